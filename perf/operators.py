@@ -1,0 +1,727 @@
+"""What fitting and serving gated efficiency heads is measured on.
+
+The operators: the gated block over feature rows (``forward``), its gradients
+for a given dz (``backward``), the loss on log eta with the gradients
+(``loss``), the AdamW step over many tensors (``adamw``), the feature rows of
+(record, spec vector) pairs (``features``), and the evaluation of records with
+gated heads (``eval``).
+
+With ``own`` false, ``run`` computes them in elementary torch operations, in 32
+bits (counts in 64-bit integers, features in float64, as their logarithms of
+large counts need); with ``own`` true it makes the calls that a program makes.
+
+Rows come grouped by kernel family (``KS_NFAM`` of them), with the family's own
+weights, like the records of an evaluation; the shares follow a decoder layer:
+GEMMs most, an embedding and an LM head per step.  Weights are N(0, 0.3^2)
+rounded to their type, features those of real records' range (0 .. 1, the last
+one 1), measured eta 1 + lognormal.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+NFAM = 10
+(GEMM, LM_HEAD, GROUPED, PREFILL, DECODE, RMSNORM, ROPE, SILU, KV_WRITE, EMBED) = range(NFAM)
+# kernels of a family per step, from a dense decoder's layers
+SHARE = (128, 1, 2, 10, 22, 64, 32, 32, 32, 1)
+EXPERTS = 8
+
+
+def _case(name, op, n, prec="f32", inp=16, hid=64, **more):
+    c = {"op": op, "n": n, "prec": prec, "inp": inp, "hid": hid, **more}
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # a scheduler prices one kernel of each family: the latency of a call
+        _case("forward, ten rows", "forward", 10, "bf16", 16, 64),
+        # a whole database of measurements against the widest head
+        _case("forward, database", "forward", 1_000_003, "f32", 32, 256),
+        # gradients for a loss of the user's own, the records of a 7B trace
+        _case("backward, 7b trace", "backward", 290_001, "bf16", 16, 128, dx=False),
+        # ... with the gradient of the rows (sensitivities), odd widths
+        _case("backward with rows'", "backward", 100_003, "f32", 32, 67, dx=True),
+        # a minibatch of a fit; a tenth of the rows was never measured
+        _case("loss, minibatch", "loss", 4099, "f32", 16, 64, huber=0.0),
+        # a full-batch pass over two million measurements (the largest)
+        _case("loss, database", "loss", 2_000_003, "bf16", 32, 256, huber=0.5),
+        # the four tensors of one small head, states in 32 bits
+        _case("adamw, one head", "adamw", 4, inp=16, hid=64, bits=32, grad="f32"),
+        # a pool of heads, one optimiser over all their tensors, states in 8 bits
+        _case("adamw, pool, 8 bits", "adamw", 600, inp=32, hid=256, bits=8, grad="f32"),
+        # the feature rows of one serving step for 64 hypothetical GPUs
+        _case("features, one step", "features", 292, "bf16", 16, specs=64, steps=1),
+        # ... of a 7B trace for two datasheets, fp32 with the squares
+        _case("features, trace", "features", 290_000, "f32", 32, specs=2, steps=1000),
+        # a serving step's kernels priced with gated heads for 16 GPUs
+        _case("eval, one step", "eval", 292, "f32", 16, 64, specs=16, steps=1),
+        # ... and a trace's, every output
+        _case("eval, trace", "eval", 290_000, "f32", 32, 128, specs=2, steps=1000),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def _cost(c):
+    w = work(c)
+    return w["bytes"] / 4e12 + w["flops"] / 1e14
+
+
+def draw(rng):
+    """One more case of the same ranges: any operator, type and width; from one
+    row to the largest listed one's work."""
+    most = max(_cost(c) for c in listed())
+    while True:
+        op = rng.choice(["forward", "backward", "loss", "adamw", "features", "eval"])
+        prec = rng.choice(["f32", "bf16"])
+        inp = rng.choice([16, 32])
+        hid = rng.choice([64, 128, 256, rng.randint(1, 256)])
+        if op == "adamw":
+            c = _case(None, op, _log_int(rng, 1, 900), "f32", inp, hid, bits=rng.choice([8, 32]),
+                      grad=rng.choice(["f32", "bf16"]))
+        elif op in ("features", "eval"):
+            steps = _log_int(rng, 1, 1000)
+            c = _case(None, op, steps * rng.choice([32, 290, 292]) + rng.randint(0, 3), "f32" if op == "eval" else prec,
+                      inp, hid, specs=_log_int(rng, 1, 64), steps=steps)
+        else:
+            c = _case(None, op, _log_int(rng, 1, 2_000_003), prec, inp, hid)
+            if op == "backward":
+                c["dx"] = rng.random() < 0.5
+            if op == "loss":
+                c["huber"] = rng.choice([0.0, 0.1, 0.5])
+        if _cost(c) <= most:
+            return c
+
+
+# ------------------------------------------------------------------ inputs
+def _split(n, g):
+    """Family offsets of n rows: the shares, jittered; below ten rows per share
+    one family after another."""
+    share = np.array(SHARE, np.float64) * (0.5 + torch.rand(NFAM, generator=g, dtype=torch.float64).numpy())
+    cut = np.floor(np.cumsum(share) / share.sum() * n).astype(np.int64)
+    if n <= 64:
+        cut = np.array([(n * (f + 1)) // NFAM for f in range(NFAM)], np.int64)
+    cut[-1] = n
+    return [0] + [int(v) for v in cut]
+
+
+def _dtype(c):
+    return torch.bfloat16 if c["prec"] == "bf16" else torch.float32
+
+
+def _weights(c, dev):
+    def w(*shape):
+        return (torch.randn(*shape, generator=dev[1], device=dev[0]) * 0.3).to(_dtype(c))
+    return {"w1": w(NFAM, c["hid"], c["inp"]), "w2": w(NFAM, c["hid"], c["inp"]), "w3": w(NFAM, c["hid"]),
+            "b3": w(NFAM)}
+
+
+def _records(c, off, host, dev):
+    """Records of every family over c["steps"] steps, with request lists, routed
+    rows and spec vectors."""
+    n, S = c["n"], c["steps"]
+
+    def ints(lo, hi, size):   # log-uniform
+        r = torch.rand(size, generator=host, dtype=torch.float64)
+        return torch.exp(r * (math.log(hi) - math.log(lo)) + math.log(lo)).floor().to(torch.int32)
+
+    step = torch.cat([torch.sort(torch.randint(0, S, (off[f + 1] - off[f],), generator=host)).values
+                      for f in range(NFAM)]).to(torch.int32)
+    tokens = ints(1, 8192, S)
+    wide = torch.tensor([1024, 2048, 4096, 5120, 8192, 11008, 28672], dtype=torch.int32)
+    m = tokens[step.long()]
+    nn = wide[torch.randint(0, len(wide), (n,), generator=host)]
+    k = wide[torch.randint(0, len(wide), (n,), generator=host)]
+    a = torch.zeros(n, dtype=torch.int32)
+    b = torch.zeros(n, dtype=torch.int32)
+    nn[off[LM_HEAD]:off[LM_HEAD + 1]] = 32000
+    for f in (PREFILL, DECODE, ROPE, KV_WRITE):
+        s = slice(off[f], off[f + 1])
+        nn[s] = 8 * torch.randint(1, 9, (off[f + 1] - off[f],), generator=host, dtype=torch.int32)
+        k[s] = 128
+        a[s] = 8
+    s = slice(off[GROUPED], off[GROUPED + 1])
+    lists = max(1, off[GROUPED + 1] - off[GROUPED])
+    a[s] = EXPERTS
+    b[s] = torch.arange(off[GROUPED + 1] - off[GROUPED], dtype=torch.int32) * EXPERTS
+    routed = ints(1, 1024, lists * EXPERTS) * torch.randint(0, 2, (lists * EXPERTS,), generator=host, dtype=torch.int32)
+    reqs = torch.randint(1, 33, (S,), generator=host, dtype=torch.int32)
+    req_off = torch.cat([torch.zeros(1, dtype=torch.int32), torch.cumsum(reqs, 0, dtype=torch.int32)])
+    R = int(req_off[-1])
+    q = torch.where(torch.rand(R, generator=host) < 0.3, ints(64, 2048, R), torch.ones(R, dtype=torch.int32))
+    h = ints(1, 32768, R)
+    ns = c["specs"]
+    spec = np.zeros(ns, np.dtype([("peak_flops", "<f8"), ("hbm_bw", "<f8"), ("t0", "<f8"), ("l2_bytes", "<f8"),
+                                  ("ar_alpha0", "<f8"), ("ar_alpha_log2p", "<f8"), ("ar_beta", "<f8"),
+                                  ("n_cu", "<u4"), ("reserved", "<u4")]))
+    u = torch.rand(4, ns, generator=host, dtype=torch.float64).numpy()
+    spec["peak_flops"] = 2e14 * 12.0 ** u[0]
+    spec["hbm_bw"] = 1e12 * 8.0 ** u[1]
+    spec["t0"] = 1e-6 + 4e-6 * u[2]
+    spec["l2_bytes"] = 4e7
+    spec["ar_beta"] = 1e11
+    spec["n_cu"] = 64 + np.floor(192 * u[3])
+    t = {"step": step, "m": m, "n": nn, "k": k, "a": a, "b": b, "req_off": req_off, "req_q": q, "req_h": h,
+         "routed": routed, "specs": torch.from_numpy(spec.view(np.uint8).copy())}
+    t = {key: v.to(dev[0]) for key, v in t.items()}
+    t["spec"] = {key: torch.from_numpy(spec[key].astype(np.float64)).to(dev[0])
+                 for key in ("peak_flops", "hbm_bw", "t0", "l2_bytes", "n_cu")}
+    return t
+
+
+def _arena(c, host, dev):
+    """Parameters, gradients and states of c["n"] tensors of a pool of heads, as
+    a program keeps them: one buffer of each, every tensor from a multiple of 64
+    elements on.  Biases and w3 take no weight decay."""
+    D, H = c["inp"], c["hid"]
+    kinds = (NFAM * H * D, NFAM * H * D, NFAM * H, NFAM)
+    odd = torch.randint(0, 40, (c["n"],), generator=host).tolist()
+    size = [max(1, kinds[i % 4] - (odd[i] if i >= 4 else 0)) for i in range(c["n"])]
+    at = np.concatenate([[0], np.cumsum([-(-s // 64) * 64 for s in size])])
+    N = int(at[-1])
+    used = torch.zeros(N, dtype=torch.bool)
+    decay = torch.zeros(N)
+    for i, s in enumerate(size):
+        used[int(at[i]):int(at[i]) + s] = True
+        decay[int(at[i]):int(at[i]) + s] = 0.01 if i % 4 < 2 else 0.0
+    used, decay = used.to(dev[0]), decay.to(dev[0])
+
+    def rnd():
+        return torch.randn(N, generator=dev[1], device=dev[0]) * used
+    scale = torch.exp2(-10 * torch.rand(N, generator=dev[1], device=dev[0]))
+    g = (rnd() * scale * 0.1).to(torch.bfloat16 if c["grad"] == "bf16" else torch.float32)
+    m, v = rnd() * scale * 0.03, (rnd() * scale * 0.1) ** 2
+    st = {"p": rnd() * 0.3, "g": g, "copy": torch.zeros(N, dtype=torch.bfloat16, device=dev[0]), "decay": decay}
+    if c["bits"] == 8:
+        st["m"], st["m_exp"] = _encode(m, torch.float8_e4m3fn)
+        st["v"], st["v_exp"] = _encode(v, torch.float8_e5m2)
+    else:
+        st["m"], st["v"] = m, v
+    st["size"], st["at"] = size, [int(x) for x in at[:-1]]
+    st["cfg"] = {"lr": 1e-3, "beta1": 0.9, "beta2": 0.999, "eps": 1e-8, "grad_scale": 0.5, "step": 7}
+    return st
+
+
+def prepare(case, seed):
+    host = torch.Generator().manual_seed(seed)
+    dev = ("cuda", torch.Generator("cuda").manual_seed(seed))
+    c = dict(case)
+    if c["op"] == "adamw":
+        st = {"case": c, **_arena(c, host, dev)}
+    else:
+        off = _split(c["n"], host)
+        st = {"case": c, "off": off}
+        if c["op"] in ("features", "eval"):
+            st |= _records(c, off, host, dev)
+            if c["op"] == "eval":
+                st |= _weights(c, dev)
+        else:
+            st |= _weights(c, dev)
+            x = torch.rand(c["n"], c["inp"], generator=dev[1], device=dev[0])
+            x[:, 15] = 1.0
+            st["x"] = x.to(_dtype(c))
+            st["fam"] = torch.repeat_interleave(torch.arange(NFAM, device=dev[0]),
+                                                torch.tensor(np.diff(off), device=dev[0]), output_size=c["n"])
+        if c["op"] == "backward":
+            st["dz"] = torch.randn(c["n"], generator=dev[1], device=dev[0]) / c["n"]
+        if c["op"] == "loss":
+            eta = 1.0 + torch.exp(0.7 * torch.randn(c["n"], generator=dev[1], device=dev[0]) - 1.0)
+            never = torch.rand(c["n"], generator=dev[1], device=dev[0])
+            st["eta"] = torch.where(never < 0.1, math.nan, eta)
+            st["weight"] = torch.where(never > 0.95, 0.0, 0.5 + torch.rand(c["n"], generator=dev[1], device=dev[0]))
+    if own:
+        _plan(st)
+    return st
+
+
+# ------------------------------------------------------------------ plain forms
+def _f32(t):
+    return t.to(torch.float32)
+
+
+def _few(s):
+    """So few rows that a product for each row, with its own copy of the weights,
+    beats one for each family."""
+    c = s["case"]
+    return c["n"] * c["hid"] * c["inp"] <= 1 << 23
+
+
+def _families(s):
+    return [(f, slice(s["off"][f], s["off"][f + 1])) for f in range(NFAM) if s["off"][f + 1] > s["off"][f]]
+
+
+def _project(s, x, w):
+    """[n][H]: each row by its family's weights."""
+    if _few(s):
+        return torch.bmm(w[s["fam"]], x.unsqueeze(2)).squeeze(2)
+    out = torch.empty(x.shape[0], w.shape[1], device=x.device)
+    for f, r in _families(s):
+        torch.mm(x[r], w[f].t(), out=out[r])
+    return out
+
+
+def _gather(s, d, x):
+    """[KS_NFAM][H][D]: sums over each family's rows of d x^T."""
+    if _few(s):
+        one = (s["fam"] == torch.arange(NFAM, device=x.device)[:, None]).to(torch.float32)
+        return (one @ (d.unsqueeze(2) * x.unsqueeze(1)).reshape(len(x), -1)).reshape(NFAM, d.shape[1], x.shape[1])
+    out = torch.zeros(NFAM, d.shape[1], x.shape[1], device=x.device)
+    for f, r in _families(s):
+        torch.mm(d[r].t(), x[r], out=out[f])
+    return out
+
+
+def _block(s, x):
+    w1, w2, w3, b3 = (_f32(s[k]) for k in ("w1", "w2", "w3", "b3"))
+    g, u = _project(s, x, w1), _project(s, x, w2)
+    sg = 1.0 / (1.0 + torch.exp(-g))
+    a = g * sg
+    z = (a * u * w3[s["fam"]]).sum(1) + b3[s["fam"]]
+    return w1, w2, w3, u, sg, a, z
+
+
+def _gradients(s, x, dz, block, dx):
+    w1, w2, w3, u, sg, a, _ = block
+    dy = dz[:, None] * w3[s["fam"]]
+    du = dy * a
+    dg = dy * u * (sg + a * (1.0 - sg))
+    out = {"w1": _gather(s, dg, x), "w2": _gather(s, du, x),
+           "w3": _gather(s, dz[:, None] * a * u, torch.ones_like(x[:, :1]))[:, :, 0],
+           "b3": _gather(s, dz[:, None], torch.ones_like(x[:, :1]))[:, 0, 0]}
+    if dx:
+        wt1, wt2 = w1.transpose(1, 2).contiguous(), w2.transpose(1, 2).contiguous()
+        out["x"] = (_project(s, dg, wt1) + _project(s, du, wt2)).to(s["x"].dtype)
+    return out
+
+
+def _per_family(s, v):
+    """Sums of v over each family's rows, in 64 bits (long sums)."""
+    c = torch.cat([v.new_zeros(1, dtype=torch.float64), torch.cumsum(v.to(torch.float64), 0)])
+    at = torch.tensor(s["off"], device=v.device)
+    return c[at[1:]] - c[at[:-1]]
+
+
+def _plain_loss(s):
+    x = _f32(s["x"])
+    block = _block(s, x)
+    z = block[-1]
+    wt = torch.where(torch.isfinite(s["eta"]) & (s["eta"] > 0) & (s["weight"] > 0), s["weight"], 0.0)
+    r = torch.clamp(-z, min=0.0) + torch.log1p(torch.exp(-z.abs())) - torch.log(torch.where(wt > 0, s["eta"], 1.0))
+    d = s["case"]["huber"] or math.inf
+    rho = torch.where(r.abs() <= d, 0.5 * r * r, 0.0 if d == math.inf else d * (r.abs() - 0.5 * d))
+    total = _per_family(s, wt)
+    loss = _per_family(s, wt * rho) / torch.where(total > 0, total, 1.0)
+    share = wt / torch.where(total > 0, total, 1.0)[s["fam"]].to(torch.float32)
+    dz = -share * torch.clamp(r, -d, d) / (1.0 + torch.exp(z))
+    return {"loss": loss.to(torch.float32), "z": z, **_gradients(s, x, dz, block, False)}
+
+
+def _ceil(a, b):
+    return torch.div(a + b - 1, b, rounding_mode="floor")
+
+
+def _counts(s):
+    """F, Bt, B, M of every record in 64-bit integers, and the K its features use."""
+    o = s["off"]
+    step, m, n, k, a, b = (s[key].long() for key in ("step", "m", "n", "k", "a", "b"))
+    q, h = s["req_q"].long(), s["req_h"].long()
+    at = s["req_off"].long()
+
+    def per_step(v):
+        t = torch.cat([v.new_zeros(1), torch.cumsum(v, 0)])
+        return (t[at[1:]] - t[at[:-1]])[step]
+
+    Q, KV, P, T = per_step(q), per_step(h + q), per_step(q * h + q * (q + 1) // 2), per_step(_ceil(q, 128))
+    F, Bt, B, M = (torch.zeros_like(m) for _ in range(4))
+
+    def put(lo, hi, f, bt, blocks, rows):
+        r = slice(o[lo], o[hi + 1])
+        F[r], Bt[r], B[r], M[r] = f(r), bt(r), blocks(r), rows(r)
+
+    put(GEMM, LM_HEAD, lambda r: 2 * m[r] * n[r] * k[r], lambda r: 2 * (m[r] * k[r] + k[r] * n[r] + m[r] * n[r]),
+        lambda r: _ceil(m[r], 128) * _ceil(n[r], 128), lambda r: m[r])
+    r = slice(o[GROUPED], o[GROUPED + 1])
+    me = s["routed"].long()[b[r][:, None] + torch.arange(EXPERTS, device=m.device)]
+    tot, act, tiles = me.sum(1), (me > 0).sum(1), _ceil(me, 128).sum(1)
+    put(GROUPED, GROUPED, lambda r: 2 * tot * n[r] * k[r], lambda r: 2 * (tot * k[r] + act * k[r] * n[r] + tot * n[r]),
+        lambda r: tiles * _ceil(n[r], 128), lambda r: tot)
+    put(PREFILL, DECODE, lambda r: 4 * n[r] * k[r] * P[r], lambda r: 4 * k[r] * (n[r] * Q[r] + a[r] * KV[r]),
+        lambda r: n[r] * T[r], lambda r: Q[r])
+    put(RMSNORM, RMSNORM, lambda r: 4 * m[r] * n[r], lambda r: 4 * m[r] * n[r] + 2 * n[r], lambda r: m[r], lambda r: m[r])
+    put(ROPE, ROPE, lambda r: 3 * m[r] * n[r] * k[r], lambda r: 4 * m[r] * n[r] * k[r] + 2 * m[r] * k[r],
+        lambda r: m[r], lambda r: m[r])
+    put(SILU, SILU, lambda r: 5 * m[r] * n[r], lambda r: 6 * m[r] * n[r], lambda r: _ceil(m[r] * n[r], 1024), lambda r: m[r])
+    put(KV_WRITE, KV_WRITE, lambda r: 0, lambda r: 8 * m[r] * n[r] * k[r], lambda r: m[r], lambda r: m[r])
+    put(EMBED, EMBED, lambda r: 0, lambda r: 4 * m[r] * n[r] + 4 * m[r], lambda r: m[r], lambda r: m[r])
+    kk = k.clone()
+    for f in (RMSNORM, SILU, EMBED):
+        kk[o[f]:o[f + 1]] = 0
+    return F, Bt, B, M, n, kk
+
+
+def _plain_features(s):
+    """[specs][n][inp] in float64, and t_roof."""
+    F, Bt, B, M, n, k = (v.to(torch.float64) for v in _counts(s))
+    sp = {key: v[:, None] for key, v in s["spec"].items()}
+    P, BW, N = sp["peak_flops"], sp["hbm_bw"], sp["n_cu"]
+    W = torch.ceil(B / N)
+    u = torch.where(B > 0, W * N / torch.clamp(B, min=1.0), 1.0)
+    tc, tm = F * u / P, Bt / BW
+    roof = torch.maximum(tc, tm)
+    log = torch.log2
+    some = torch.zeros_like(tc)
+    ai = F / torch.clamp(Bt, min=1.0)
+    blocks = torch.clamp(B, min=1.0)
+    x = [log(torch.clamp(ai, min=2.0 ** -10)) / 16 + some, log(torch.clamp(ai * BW / P, min=2.0 ** -20)) / 16,
+         log(1 + B / N) / 16, 1 / u, log(1 + W) / 16, torch.clamp(sp["l2_bytes"] / torch.clamp(Bt, min=1.0), max=1.0),
+         log(torch.clamp(roof / torch.clamp(sp["t0"], min=1e-9), min=2.0 ** -20)) / 16,
+         tc / torch.where(tc + tm > 0, tc + tm, 1.0), log(1 + F) / 64 + some, log(1 + Bt) / 48 + some,
+         log(1 + M) / 24 + some, log(1 + n) / 24 + some, log(1 + k) / 24 + some, log(1 + F / blocks) / 48 + some,
+         log(1 + Bt / blocks) / 40 + some, some + 1.0]
+    x = torch.stack(x, 2)
+    return torch.cat([x, x * x], 2) if s["case"]["inp"] == 32 else x, roof
+
+
+def _by_family(s, v):
+    """[specs][n] ... -> the pairs in the order of their families."""
+    return torch.cat([v[:, r].reshape(-1, *v.shape[2:]) for _, r in _families(s)])
+
+
+def _plain_eval(s):
+    x, roof = _plain_features(s)
+    S, n = roof.shape
+    o = s["off"]
+    pairs = {"case": dict(s["case"], n=S * n), "off": [S * v for v in o], **{k: s[k] for k in ("w1", "w2", "w3", "b3")},
+             "fam": torch.repeat_interleave(torch.arange(NFAM, device=roof.device),
+                                            torch.tensor(np.diff(o) * S, device=roof.device), output_size=S * n)}
+    z = _block(pairs, _by_family(s, _f32(x)))[-1]
+    eta = torch.cat([(1.0 + torch.exp(-z[S * r.start:S * r.stop])).reshape(S, -1) for _, r in _families(s)], 1)
+    t = torch.maximum(_f32(roof) * eta, _f32(s["spec"]["t0"])[:, None])
+    return {"t_roof": _f32(roof), "eta": eta, "t_kernel": t}
+
+
+def _encode(v, dtype):
+    """8-bit values of that type and, for each 64 elements, the power of two that
+    they stand for a multiple of (its exponent + 127): the largest finite element
+    comes to 2^7 .. 2^8 in e4m3, 2^14 .. 2^15 in e5m2.  A second moment above
+    zero never becomes zero."""
+    signed = dtype == torch.float8_e4m3fn
+    b = v.reshape(-1, 64)
+    top = torch.where(torch.isfinite(b), b.abs(), 0.0).amax(1)
+    e = torch.clamp((top.view(torch.int32) >> 23) - (7 if signed else 14), min=1)
+    q = b * ((254 - e) << 23).view(torch.float32)[:, None]
+    if not signed:
+        q = torch.where((q > 0) & (q < 2.0 ** -16), 2.0 ** -16, q)
+    return q.reshape(-1).to(dtype), e.to(torch.uint8)
+
+
+def _decode(q, e):
+    return (_f32(q).reshape(-1, 64) * (e.to(torch.int32) << 23).view(torch.float32)[:, None]).reshape(-1)
+
+
+def _plain_adamw(s):
+    o = s["cfg"]
+    eight = s["case"]["bits"] == 8
+    g = _f32(s["g"]) * o["grad_scale"]
+    m, v = (_decode(s["m"], s["m_exp"]), _decode(s["v"], s["v_exp"])) if eight else (s["m"], s["v"])
+    m = m * o["beta1"] + g * (1 - o["beta1"])
+    v = v * o["beta2"] + g * (1 - o["beta2"]) * g
+    c1, c2 = 1 - o["beta1"] ** o["step"], 1 - o["beta2"] ** o["step"]
+    p = s["p"] * (1 - o["lr"] * s["decay"]) - (o["lr"] / c1) * (m / (torch.sqrt(v) / math.sqrt(c2) + o["eps"]))
+    s["p"].copy_(p)
+    s["copy"].copy_(p)
+    if eight:
+        for key, val in (("m", m), ("v", v)):
+            q, e = _encode(val, s[key].dtype)
+            s[key].copy_(q)
+            s[key + "_exp"].copy_(e)
+    else:
+        s["m"].copy_(m)
+        s["v"].copy_(v)
+    return _adamw_out(s)
+
+
+def _adamw_out(s):
+    return {k: s[k] for k in ("p", "copy", "m", "v", "m_exp", "v_exp") if k in s}
+
+
+# ------------------------------------------------------------------ the framework's calls
+def _plan(s):
+    """What a program keeps from call to call: the structs that point at its
+    tensors, outputs and the workspace."""
+    from paper_2606_28565_amd import abi
+    c = s["case"]
+    prec = abi.KS_BF16 if c["prec"] == "bf16" else abi.KS_F32
+
+    def new(*shape, dtype=torch.float32):
+        return torch.empty(*shape, dtype=dtype, device="cuda")
+
+    h = None
+    if "w1" in s:
+        h = s["heads"] = abi.gated_heads(s["w1"], s["w2"], s["w3"], s["b3"])
+    if c["op"] in ("forward", "backward", "loss"):
+        rows = s["rows"] = abi.feature_rows(s["x"], s["off"])
+        if c["op"] == "forward":
+            s["out"] = {"z": new(c["n"])}
+            return
+        s["ws"] = new(max(1, abi.ks_gated_workspace_bytes(h, rows)), dtype=torch.uint8)
+        s["out"] = {"w1": new(*s["w1"].shape), "w2": new(*s["w2"].shape), "w3": new(*s["w3"].shape), "b3": new(NFAM)}
+        if c.get("dx"):
+            s["out"]["x"] = torch.empty_like(s["x"])
+        s["grad"] = abi.gated_grad(**{k: s["out"].get(k) for k in ("w1", "w2", "w3", "b3", "x")})
+        if c["op"] == "loss":
+            s["out"] |= {"loss": new(NFAM), "z": new(c["n"])}
+            s["target"] = abi.eta_target(s["eta"], s["weight"], c["huber"] or math.inf)
+    elif c["op"] == "adamw":
+        def part(key, i, per=1):
+            return s[key][s["at"][i] // per:s["at"][i] // per - (-s["size"][i] // per)]
+        eight = c["bits"] == 8
+        s["tensors"] = abi.adamw_tensors([
+            {"param": part("p", i), "grad": part("g", i), "m": part("m", i), "v": part("v", i), "copy": part("copy", i),
+             "m_exp": part("m_exp", i, 64) if eight else None, "v_exp": part("v_exp", i, 64) if eight else None,
+             "weight_decay": 0.01 if i % 4 < 2 else 0.0} for i in range(c["n"])])
+        s["adamw"] = abi.adamw_config(state_bits=c["bits"], **s["cfg"])
+        s["out"] = _adamw_out(s)
+    else:
+        d = abi.ks_desc()
+        d.n_rows, d.n_steps, d.n_req = c["n"], c["steps"], s["req_q"].numel()
+        for f in range(NFAM + 1):
+            d.fam_off[f] = s["off"][f]
+        for key in ("step", "m", "n", "k", "a", "b", "req_off", "req_q", "req_h"):
+            setattr(d, key, s[key].data_ptr())
+        d.expert_rows, d.n_expert_rows, d.elem_bytes = s["routed"].data_ptr(), s["routed"].numel(), 2
+        s["desc"] = d
+        s["ws"] = new(abi.ks_workspace_bytes(d, c["specs"]), dtype=torch.uint8)
+        pairs = c["specs"] * c["n"]
+        if c["op"] == "features":
+            s["out"] = {"x": new(pairs, c["inp"], dtype=_dtype(c)), "t_roof": new(pairs)}
+            s["prec"] = prec
+        else:
+            s["out"], s["kout"] = abi.kernel_outputs(c["n"], c["specs"], counts=False)
+
+
+def _own(s):
+    from paper_2606_28565_amd import abi
+    st = abi.current_stream()
+    op, o = s["case"]["op"], s["out"]
+    if op == "forward":
+        abi.ks_gated_forward(s["heads"], s["rows"], o["z"].data_ptr(), st)
+    elif op == "backward":
+        abi.ks_gated_backward(s["heads"], s["rows"], s["dz"].data_ptr(), s["grad"], s["ws"].data_ptr(), s["ws"].numel(), st)
+    elif op == "loss":
+        abi.ks_gated_loss(s["heads"], s["rows"], s["target"], o["loss"].data_ptr(), o["z"].data_ptr(), s["grad"],
+                          s["ws"].data_ptr(), s["ws"].numel(), st)
+    elif op == "adamw":
+        abi.ks_adamw(s["adamw"], s["tensors"], st)
+    elif op == "features":
+        abi.ks_features(s["desc"], s["specs"].data_ptr(), s["case"]["specs"], s["case"]["inp"], s["prec"],
+                        o["x"].data_ptr(), s["case"]["inp"], o["t_roof"].data_ptr(), s["ws"].data_ptr(), s["ws"].numel(), st)
+    else:
+        abi.ks_eval_kernels(s["desc"], s["specs"].data_ptr(), s["case"]["specs"], s["heads"], s["kout"],
+                            s["ws"].data_ptr(), s["ws"].numel(), st)
+    return o
+
+
+def run(state):
+    if own:
+        return _own(state)
+    op = state["case"]["op"]
+    if op == "forward":
+        return {"z": _block(state, _f32(state["x"]))[-1]}
+    if op == "backward":
+        # (a row whose dz is 0 contributes nothing, whatever its features)
+        x = torch.where(state["dz"][:, None] != 0, _f32(state["x"]), 0.0)
+        return _gradients(state, x, state["dz"], _block(state, x), state["case"]["dx"])
+    if op == "loss":
+        return _plain_loss(state)
+    if op == "adamw":
+        return _plain_adamw(state)
+    if op == "features":
+        x, roof = _plain_features(state)
+        return {"x": _by_family(state, x).to(_dtype(state["case"])), "t_roof": _f32(_by_family(state, roof))}
+    return _plain_eval(state)
+
+
+def work(case):
+    c = dict(case)
+    e = 2 if c["prec"] == "bf16" else 4
+    n, D, H = c["n"], c["inp"], c["hid"]
+    if c["op"] == "adamw":
+        elems = sum((NFAM * H * D, NFAM * H * D, NFAM * H, NFAM)[i % 4] for i in range(n))
+        per = 8 + (2 if c["grad"] == "bf16" else 4) + 2 + (16 if c["bits"] == 32 else 4 + 4 / 64)
+        return {"bytes": elems * per, "flops": 12.0 * elems}
+    weights = e * NFAM * (2 * H * D + H + 1)
+    if c["op"] in ("features", "eval"):
+        pairs = n * c["specs"]
+        if c["op"] == "features":
+            return {"bytes": 24.0 * n + pairs * (D * e + 4.0), "flops": 60.0 * pairs}
+        return {"bytes": 24.0 * n + pairs * 12.0 + weights, "flops": pairs * (60.0 + 4.0 * D * H)}
+    if c["op"] == "forward":
+        return {"bytes": n * (D * e + 4.0) + weights, "flops": 4.0 * n * D * H}
+    grads = 4.0 * NFAM * (2 * H * D + H + 1)
+    if c["op"] == "backward":
+        return {"bytes": n * (D * e * (2 if c["dx"] else 1) + 4.0) + weights + grads,
+                "flops": n * D * H * (12.0 if c["dx"] else 8.0)}
+    return {"bytes": n * (D * e + 12.0) + weights + grads, "flops": 8.0 * n * D * H}
+
+
+# ------------------------------------------------------------------ the definitions in 64 bits
+def _wide(t):
+    return t.to(torch.float64)
+
+
+def _exact_rows(s, given):
+    """z, and the sums of the gradients, family by family and a piece of the rows
+    at a time.  given(z, rows, f): dz of those rows, or None."""
+    D = torch.float64
+    n = s["x"].shape[0]
+    out = {"z": torch.empty(n, dtype=D, device="cuda")}
+    acc = {k: torch.zeros(s[k].shape, dtype=D, device="cuda") for k in ("w1", "w2", "w3", "b3")}
+    dx = torch.zeros(s["x"].shape, dtype=D, device="cuda")
+    for f in range(NFAM):
+        wg, wu, w3, b3 = (_wide(s[k][f]) for k in ("w1", "w2", "w3", "b3"))
+        for lo in range(s["off"][f], s["off"][f + 1], 200_000):
+            r = slice(lo, min(lo + 200_000, s["off"][f + 1]))
+            x = _wide(s["x"][r])
+            g, u = x @ wg.t(), x @ wu.t()
+            sg = torch.sigmoid(g)
+            out["z"][r] = (g * sg * u) @ w3 + b3
+            dz = given(out["z"][r], r, f)
+            if dz is None:
+                continue
+            x = torch.where(dz[:, None] != 0, x, torch.zeros_like(x))
+            dgate = dz[:, None] * w3 * u * sg * (1 + g * (1 - sg))
+            dup = dz[:, None] * w3 * g * sg
+            acc["w1"][f] += dgate.t() @ x
+            acc["w2"][f] += dup.t() @ x
+            acc["w3"][f] += dz @ (g * sg * u)
+            acc["b3"][f] += dz.sum()
+            dx[r] = dgate @ wg + dup @ wu
+    return out["z"], acc, dx
+
+
+def _exact_counts(s):
+    """[F, Bt, B, M] of each record, by numpy on the host."""
+    h = {k: s[k].cpu().numpy().astype(np.int64) for k in ("step", "m", "n", "k", "a", "b", "req_off", "req_q", "req_h",
+                                                          "routed")}
+    up = lambda v, d: -(-v // d)  # noqa: E731
+    q, hist, ro = h["req_q"], h["req_h"], h["req_off"]
+    agg = np.array([[np.sum(q[i:j]), np.sum(hist[i:j] + q[i:j]), np.sum(q[i:j] * hist[i:j] + q[i:j] * (q[i:j] + 1) // 2),
+                     np.sum(up(q[i:j], 128))] for i, j in zip(ro[:-1], ro[1:])], np.int64)
+    fam = np.repeat(np.arange(NFAM), np.diff(s["off"]))
+    m, n, k, a = h["m"], h["n"], h["k"], h["a"]
+    Q, KV, PAIRS, TILES = agg[h["step"]].T
+    me = np.where((fam == GROUPED)[:, None], h["routed"][np.where(fam == GROUPED, h["b"], 0)[:, None] + np.arange(EXPERTS)], 0)
+    E, act, et = me.sum(1), (me > 0).sum(1), up(me, 128).sum(1)
+    att, gemm = (fam == PREFILL) | (fam == DECODE), (fam == GEMM) | (fam == LM_HEAD)
+    pick = [gemm, fam == GROUPED, att, fam == RMSNORM, fam == ROPE, fam == SILU, fam == KV_WRITE, fam == EMBED]
+    F = np.select(pick, [2 * m * n * k, 2 * E * n * k, 4 * n * k * PAIRS, 4 * m * n, 3 * m * n * k, 5 * m * n, 0 * m, 0 * m])
+    Bt = 2 * np.select(pick, [m * k + k * n + m * n, E * k + act * k * n + E * n, 2 * n * k * Q + 2 * a * k * KV,
+                              2 * m * n + n, 2 * m * n * k + m * k, 3 * m * n, 4 * m * n * k, 2 * m * n + 2 * m])
+    B = np.select(pick, [up(m, 128) * up(n, 128), et * up(n, 128), n * TILES, m, m, up(m * n, 1024), m, m])
+    M = np.select(pick, [m, E, Q, m, m, m, m, m])
+    K = np.where((fam == RMSNORM) | (fam == SILU) | (fam == EMBED), 0, k)
+    return F, Bt, B, M, n, K
+
+
+def _exact_features(s):
+    F, Bt, B, M, n, k = _exact_counts(s)
+    sp = {key: v.cpu().numpy() for key, v in s["spec"].items()}
+    xs, roofs = [], []
+    with np.errstate(divide="ignore"):
+        for i in range(len(sp["n_cu"])):
+            N = int(sp["n_cu"][i])
+            W = (B + N - 1) // N
+            u = np.where(B > 0, W * N / np.maximum(B, 1), 1.0)
+            tc, tm = F * u / sp["peak_flops"][i], Bt / sp["hbm_bw"][i]
+            roof = np.maximum(tc, tm)
+            ai = F / np.maximum(Bt, 1)
+            x = np.stack([np.maximum(np.log2(ai), -10) / 16,
+                          np.maximum(np.log2(ai * sp["hbm_bw"][i] / sp["peak_flops"][i]), -20) / 16,
+                          np.log2(1 + B / N) / 16, 1 / u, np.log2(1 + W) / 16,
+                          np.minimum(1, sp["l2_bytes"][i] / np.maximum(Bt, 1)),
+                          np.maximum(np.log2(roof / max(sp["t0"][i], 1e-9)), -20) / 16,
+                          np.where(tc + tm > 0, tc / np.where(tc + tm > 0, tc + tm, 1), 0), np.log2(1 + F) / 64,
+                          np.log2(1 + Bt) / 48, np.log2(1 + M) / 24, np.log2(1 + n) / 24, np.log2(1 + k) / 24,
+                          np.log2(1 + F / np.maximum(B, 1)) / 48, np.log2(1 + Bt / np.maximum(B, 1)) / 40,
+                          np.ones(len(F))], 1)
+            xs.append(np.concatenate([x, x * x], 1) if s["case"]["inp"] == 32 else x)
+            roofs.append(roof)
+    return np.stack(xs), np.stack(roofs)
+
+
+def _exact_adamw(s):
+    o = s["cfg"]
+    eight = s["case"]["bits"] == 8
+
+    def value(key):
+        if not eight:
+            return _wide(s[key])
+        return (_wide(_f32(s[key])).reshape(-1, 64) * torch.exp2(_wide(s[key + "_exp"]) - 127)[:, None]).reshape(-1)
+
+    g = _wide(s["g"]) * o["grad_scale"]
+    m = o["beta1"] * value("m") + (1 - o["beta1"]) * g
+    v = o["beta2"] * value("v") + (1 - o["beta2"]) * g ** 2
+    hat_m, hat_v = m / (1 - o["beta1"] ** o["step"]), v / (1 - o["beta2"] ** o["step"])
+    p = _wide(s["p"])
+    p = p - o["lr"] * (hat_m / (hat_v.sqrt() + o["eps"]) + _wide(s["decay"]) * p)
+    out = {"p": p, "copy": p, "m": m, "v": v}
+    if eight:
+        for key, lift in (("m", 7), ("v", 14)):
+            b = out[key].reshape(-1, 64)
+            e = torch.clamp(torch.frexp(b.abs().amax(1))[1] - 1 - lift, min=-126)
+            out[key] = (b / torch.exp2(_wide(e))[:, None]).reshape(-1)
+            out[key + "_exp"] = None
+    return out
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    op = s["case"]["op"]
+    if op == "adamw":
+        return _exact_adamw(s)
+    if op in ("features", "eval"):
+        if s["case"]["n"] * s["case"]["specs"] > 3_000_000:
+            return None   # (minutes on the host)
+        x, roof = _exact_features(s)
+        o = s["off"]
+        order = lambda v: np.concatenate([v[:, o[f]:o[f + 1]].reshape(-1, *v.shape[2:]) for f in range(NFAM)])  # noqa: E731
+        if op == "features":
+            return {"x": order(x), "t_roof": order(roof)}
+        z = np.empty(roof.shape)
+        for f in range(NFAM):
+            wg, wu, w3, b3 = (_wide(s[key][f]).cpu().numpy() for key in ("w1", "w2", "w3", "b3"))
+            for i in range(len(roof)):
+                xf = x[i, o[f]:o[f + 1]]
+                g = xf @ wg.T
+                z[i, o[f]:o[f + 1]] = (g / (1 + np.exp(-g)) * (xf @ wu.T)) @ w3 + b3
+        eta = 1 + np.exp(-z)
+        return {"t_roof": roof, "eta": eta, "t_kernel": np.maximum(roof * eta, s["spec"]["t0"].cpu().numpy()[:, None])}
+    if op == "forward":
+        return {"z": _exact_rows(s, lambda z, r, f: None)[0]}
+    if op == "backward":
+        _, acc, dx = _exact_rows(s, lambda z, r, f: _wide(s["dz"][r]))
+        return {**acc, "x": dx} if s["case"]["dx"] else acc
+    eta, wt = _wide(s["eta"]), _wide(s["weight"])
+    wt = torch.where(torch.isfinite(eta) & (eta > 0), wt, torch.zeros_like(wt))
+    total = torch.stack([wt[s["off"][f]:s["off"][f + 1]].sum() for f in range(NFAM)])
+    loss = torch.zeros(NFAM, dtype=torch.float64, device="cuda")
+    d = s["case"]["huber"] or math.inf
+
+    def given(z, r, f):
+        if total[f] == 0:
+            return torch.zeros_like(z)
+        res = torch.logaddexp(torch.zeros_like(z), -z) - torch.log(torch.where(wt[r] > 0, eta[r], torch.ones_like(z)))
+        big = res.abs() > d
+        rho = torch.where(big, d * res.abs() - d * d / 2 if d < math.inf else res, res ** 2 / 2)
+        loss[f] += (wt[r] * rho).sum() / total[f]
+        return -wt[r] / total[f] * torch.where(big, d * torch.sign(res) if d < math.inf else res, res) * torch.sigmoid(-z)
+
+    z, acc, _ = _exact_rows(s, given)
+    return {"loss": loss, "z": z, **acc}
