@@ -417,7 +417,7 @@ def _encode(v, dtype):
     e = torch.clamp((top.view(torch.int32) >> 23) - (7 if signed else 14), min=1)
     q = b * ((254 - e) << 23).view(torch.float32)[:, None]
     if not signed:
-        q = torch.where((q > 0) & (q < 2.0 ** -16), 2.0 ** -16, q)
+        q = torch.where((b > 0) & (q < 2.0 ** -16), 2.0 ** -16, q)
     return q.reshape(-1).to(dtype), e.to(torch.uint8)
 
 
