@@ -8,8 +8,8 @@
  *   t      = max(t_roof * eta, t0),                    Eq. 2 (Sec. 5.3)
  *   t_roof = max(F * u / P_peak, Bt / BW_peak),        Eq. 2
  *   u      = ceil(B / N_cu) * N_cu / B,                Sec. 2.2
- *   eta    = 1 / sigma(z) = 1 + exp(-z), z from a per-family MLP head on
- *            dimensionless features,                   Sec. 5.3
+ *   eta    = 1 / sigma(z) = 1 + exp(-z), z from a per-family MLP head or
+ *            gated block on dimensionless features,    Sec. 5.3
  *   t_ar   = alpha0(P) + 2 (P - 1) / P * S / beta,     Eq. 3 (Sec. 5.6)
  *   t_step = max(t_gpu + n c_disp, l) + max(0, c_ovl - t_gpu) + c_tail,
  *                                                      Eq. 4 (Sec. 5.7)
@@ -119,7 +119,7 @@ typedef struct ks_spec {
 } ks_spec;
 
 enum { KS_F32 = 0, KS_BF16 = 1 };
-enum { KS_ETA_MLP = 0, KS_ETA_ONE = 1 };
+enum { KS_ETA_MLP = 0, KS_ETA_ONE = 1, KS_ETA_GATED = 2 };
 
 /*
  * Per-family efficiency heads (Sec. 5.3), device arrays, row-major [out][in]:
@@ -130,6 +130,14 @@ enum { KS_ETA_MLP = 0, KS_ETA_ONE = 1 };
  * z = w3 . relu(W2 relu(W1 x) + b2) + b3;  eta = 1 + exp(-z).
  * Supported: in_dim 16 or 32; hidden 64 or 128 (KS_F32), 64, 128 or 256
  * (KS_BF16).  mode KS_ETA_ONE: eta = 1 (the MLP fields are ignored).
+ *
+ * mode KS_ETA_GATED: a gated feed-forward block per family in the MLP's place,
+ *   w1 (gate), w2 (up) [KS_NFAM][hidden][in_dim], w3 [KS_NFAM][hidden],
+ *   b3 [KS_NFAM]; b2 is not read:
+ *   z = w3 . (silu(W1 x) * (W2 x)) + b3, silu(g) = g / (1 + exp(-g)).
+ * Supported: in_dim 16 or 32; hidden 1 .. 256, either precision.  KS_BF16 rounds
+ * x to bfloat16 before the two projections; everything after them is fp32.
+ * ks_gated_loss and ks_adamw fit such heads.
  *
  * Per-family head selection (Sec. 5.3 picks each family's head from a pool):
  * the families whose bit is set in bounded_mask (bit f = family f) take
@@ -150,7 +158,7 @@ enum { KS_ETA_MLP = 0, KS_ETA_ONE = 1 };
  * grid when its coordinates lie in the closed box and the eight corners of
  * its cell are all measured (not NaN); there eta is the trilinear
  * interpolation of the corners.  Other queries of such a family take the
- * family's other head (MLP, bounded head or eta = 1, as above).
+ * family's other head (MLP, gated block, bounded head or eta = 1, as above).
  * grid: device float array [KS_NFAM][n0][n1][n2], row-major, NaN for a node
  * never measured (rows of families outside grid_mask are not read); NULL if
  * grid_mask is 0.  n0 n1 n2 <= KS_GRID_MAX_NODES.  Computed in fp32: a query
@@ -188,7 +196,7 @@ typedef struct ks_host {
 /* Per-record and per-pair outputs (device; any pointer may be NULL = skip).
  * flops, bytes, blocks: [n_rows]; t_roof, eta, t_kernel: [n_specs][n_rows].
  * source: [n_specs][n_rows], where each pair's eta came from: 0 the head of
- * heads.mode (the MLP, or eta = 1), 1 the bounded analytical head, 2 the
+ * heads.mode (the MLP, the gated block, or eta = 1), 1 the bounded analytical head, 2 the
  * measured Tier B grid (density routing, Sec. 5.5). */
 typedef struct ks_kernel_out {
   uint64_t *flops, *bytes, *blocks;
@@ -433,6 +441,123 @@ ks_status ks_eval_steps_static(const ks_desc* desc, const ks_steps* steps,
                                const ks_heads* heads, const ks_host* host,
                                const ks_step_out* out, const ks_kernel_out* kout,
                                uint32_t* flags, hipStream_t stream);
+
+/*
+ * Fitting gated heads (Sec. 5.3: heads learn log eta of measured kernels from
+ * dimensionless features).  A fit forms the feature rows of its measurements
+ * once (ks_features), then per step takes the loss and its gradients
+ * (ks_gated_loss) and moves the parameters (ks_adamw); the fitted weights price
+ * records through the evaluation calls (mode KS_ETA_GATED).  ks_gated_forward and
+ * ks_gated_backward are the block by itself, for losses of the caller's own.
+ * None of these calls synchronizes; all can be captured into a graph.
+ */
+
+/* Feature rows, family-major: rows [fam_off[f], fam_off[f+1]) are family f's and
+ * go through its weights.  x: device [n_rows][ldx], of heads.precision's type,
+ * the first in_dim elements of each row are read; ldx >= in_dim.  Any base of its
+ * type's alignment and any stride is taken; 16-byte aligned rows are read
+ * fastest.  n_rows < 2^31. */
+typedef struct ks_rows {
+  int64_t n_rows;
+  int64_t fam_off[KS_NFAM + 1];          /* host array, fam_off[0] = 0       */
+  const void *x;
+  int64_t ldx;
+} ks_rows;
+
+/* Gradients (device, overwritten; families without rows get zeros).
+ * w1, w2: [KS_NFAM][hidden][in_dim], w3: [KS_NFAM][hidden], b3: [KS_NFAM], all
+ * fp32 whatever the heads' precision, all four or none of them NULL.
+ * x: [n_rows][ldx] of heads.precision's type, or NULL; it may not overlap the
+ * rows themselves. */
+typedef struct ks_gated_grad {
+  float *w1, *w2, *w3, *b3;
+  void *x;
+  int64_t ldx;
+} ks_gated_grad;
+
+/* Measured efficiency factors.  A row counts when its eta is finite and above 0
+ * and its weight (1 without weights) is finite and above 0; the others, whatever
+ * their features, add nothing to the loss or to any gradient. */
+typedef struct ks_eta_target {
+  const float *eta;       /* device [n_rows]                                 */
+  const float *weight;    /* device [n_rows] or NULL                         */
+  double huber;           /* d > 0 of the Huber loss; INFINITY: squares only */
+} ks_eta_target;
+
+/* z [n_rows] (device) = w3_f . (silu(W1_f x) * (W2_f x)) + b3_f of each row. */
+ks_status ks_gated_forward(const ks_heads *heads, const ks_rows *rows, float *z, hipStream_t stream);
+
+/* Bytes of device workspace ks_gated_backward and ks_gated_loss need for these
+ * rows (256-byte aligned); 0 on bad arguments.  Only sizes are read. */
+size_t ks_gated_workspace_bytes(const ks_heads *heads, const ks_rows *rows);
+
+/* Gradients of sum_i dz_i z_i (dz: device [n_rows]) for the weights and, where
+ * grad->x is set, for the rows: with g = W1 x, u = W2 x, s = sigma(g), a = g s,
+ *   dw3 = dz a u, db3 = dz, du = dz w3 a, dg = dz w3 u (s + a (1 - s)),
+ *   dW1 = dg x^T, dW2 = du x^T, dx = W1^T dg + W2^T du.
+ * A row whose dz is 0 adds nothing, whatever its features, and its dx is 0.
+ * Sums are formed in a fixed order: the same call gives the same bits. */
+ks_status ks_gated_backward(const ks_heads *heads, const ks_rows *rows, const float *dz, const ks_gated_grad *grad,
+                            void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* The loss on log eta and its gradients: with r = log(1 + exp(-z)) - log(eta),
+ *   loss[f] = sum w rho(r) / sum w over family f's rows that count,
+ *   rho(r) = r^2 / 2 for |r| <= huber, huber (|r| - huber / 2) beyond,
+ * 0 for a family without any; the gradients are those of sum_f loss[f].
+ * loss: device [KS_NFAM]; z: device [n_rows] or NULL; grad: NULL for the loss
+ * alone, else its four weight gradients (grad->x must be NULL). */
+ks_status ks_gated_loss(const ks_heads *heads, const ks_rows *rows, const ks_eta_target *target, float *loss, float *z,
+                        const ks_gated_grad *grad, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* The feature rows of every (record, spec vector) pair as the evaluation forms
+ * them: family-major over the pairs, so that with n = fam_off[f+1] - fam_off[f]
+ * record i of family f under spec s is row n_specs fam_off[f] + s n + i (a
+ * ks_rows with fam_off scaled by n_specs).  x: device [n_specs n_rows][ldx],
+ * in_dim 16 or 32 elements per row written, of precision's type; t_roof: device
+ * [n_specs n_rows] or NULL, the pairs' rooflines (a measured eta is the measured
+ * time over it).  ws as for ks_eval_kernels.  Records with bad device data get
+ * zeros and raise the flag of ks_device_status().  n_specs n_rows < 2^31. */
+ks_status ks_features(const ks_desc *desc, const ks_spec *specs, int32_t n_specs, int32_t in_dim, int32_t precision,
+                      void *x, int64_t ldx, float *t_roof, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * One AdamW step over many tensors.  Per element, in fp32, g = grad_scale grad:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + ((1 - beta2) g) g,
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps).
+ * States in 32 bits: m, v float [n].  States in 8 bits: m e4m3 [n], v e5m2 [n]
+ * (one byte each, OCP formats) and for every 64 elements one exponent byte e each
+ * (m_exp, v_exp [ceil(n / 64)]): the byte stands for its value times 2^(e - 127).
+ * The largest finite element of a block comes to 2^7 .. 2^8 (m) or 2^14 .. 2^15
+ * (v), e is 1 at least; rounding is to nearest even, a second moment above zero
+ * never rounds to zero, infinities in m become NaN.  The step itself uses the
+ * unrounded m and v.  All-zero states are those before the first step.
+ */
+typedef struct ks_tensor {
+  int64_t n;                       /* elements, 0 .. 2^35                    */
+  float *param;                    /* device [n], updated                    */
+  const void *grad;                /* device [n] of grad_type                */
+  void *m, *v;                     /* device [n], updated                    */
+  uint8_t *m_exp, *v_exp;          /* 8-bit states, else NULL                */
+  uint16_t *copy;                  /* device [n] or NULL: the updated param
+                                      in bfloat16 (what KS_BF16 heads read)  */
+  float weight_decay;
+  int32_t grad_type;               /* KS_F32 or KS_BF16                      */
+} ks_tensor;
+
+/* step: t, 1 for the first step.  step_dev: NULL, or a device counter of the
+ * steps made so far: t is then *step_dev + 1, and the call leaves *step_dev = t
+ * (so that a captured call counts its replays); step is not read. */
+typedef struct ks_adamw_config {
+  double lr, beta1, beta2, eps, grad_scale;
+  int32_t state_bits;              /* 8 or 32                                */
+  int32_t reserved;
+  int64_t step;
+  uint32_t *step_dev;
+} ks_adamw_config;
+
+/* tensors: HOST array of n_tensors (read during the call); no two may share a
+ * param.  Launches: one for every 48 tensors, one more with step_dev. */
+ks_status ks_adamw(const ks_adamw_config *config, const ks_tensor *tensors, int32_t n_tensors, hipStream_t stream);
 
 /* Synchronous device-side check of the inputs: step order within families,
  * field limits, request and expert offsets, spec sanity.  Synchronizes the

@@ -17,7 +17,7 @@ LIB_PATH = os.path.join(PKG, "libks.so")
 NFAM = 10
 KS_OK, KS_EINVAL, KS_ERANGE, KS_EHIP, KS_EWORKSPACE = range(5)
 KS_F32, KS_BF16 = 0, 1
-KS_ETA_MLP, KS_ETA_ONE = 0, 1
+KS_ETA_MLP, KS_ETA_ONE, KS_ETA_GATED = 0, 1, 2
 KS_STATIC_SCRATCH_BYTES = 64 << 20   # the allocation-free entry point's device array
 STATUS_NAMES = {0: "KS_OK", 1: "KS_EINVAL", 2: "KS_ERANGE", 3: "KS_EHIP", 4: "KS_EWORKSPACE"}
 
@@ -104,6 +104,29 @@ class ks_sim_out(C.Structure):
                 ("clock", C.c_double)]
 
 
+class ks_rows(C.Structure):
+    _fields_ = [("n_rows", C.c_int64), ("fam_off", C.c_int64 * (NFAM + 1)), ("x", P), ("ldx", C.c_int64)]
+
+
+class ks_gated_grad(C.Structure):
+    _fields_ = [("w1", P), ("w2", P), ("w3", P), ("b3", P), ("x", P), ("ldx", C.c_int64)]
+
+
+class ks_eta_target(C.Structure):
+    _fields_ = [("eta", P), ("weight", P), ("huber", C.c_double)]
+
+
+class ks_tensor(C.Structure):
+    _fields_ = [("n", C.c_int64), ("param", P), ("grad", P), ("m", P), ("v", P), ("m_exp", P), ("v_exp", P),
+                ("copy", P), ("weight_decay", C.c_float), ("grad_type", C.c_int32)]
+
+
+class ks_adamw_config(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("grad_scale", C.c_double), ("state_bits", C.c_int32), ("reserved", C.c_int32),
+                ("step", C.c_int64), ("step_dev", P)]
+
+
 assert C.sizeof(ks_spec) == 64
 
 
@@ -154,6 +177,19 @@ def load(path: str = LIB_PATH) -> C.CDLL:
                                 C.POINTER(ks_sched), C.POINTER(ks_requests), C.POINTER(ks_sim_out), P,
                                 C.c_size_t, P]
     lib.ks_simulate.restype = C.c_int
+    pr, pg = C.POINTER(ks_rows), C.POINTER(ks_gated_grad)
+    lib.ks_gated_forward.argtypes = [ph, pr, P, P]
+    lib.ks_gated_forward.restype = C.c_int
+    lib.ks_gated_workspace_bytes.argtypes = [ph, pr]
+    lib.ks_gated_workspace_bytes.restype = C.c_size_t
+    lib.ks_gated_backward.argtypes = [ph, pr, P, pg, P, C.c_size_t, P]
+    lib.ks_gated_backward.restype = C.c_int
+    lib.ks_gated_loss.argtypes = [ph, pr, C.POINTER(ks_eta_target), P, P, pg, P, C.c_size_t, P]
+    lib.ks_gated_loss.restype = C.c_int
+    lib.ks_features.argtypes = [pd, psp, C.c_int32, C.c_int32, C.c_int32, P, C.c_int64, P, P, C.c_size_t, P]
+    lib.ks_features.restype = C.c_int
+    lib.ks_adamw.argtypes = [C.POINTER(ks_adamw_config), P, C.c_int32, P]
+    lib.ks_adamw.restype = C.c_int
     lib.ks_set_timing_events.argtypes = [P, P]
     lib.ks_set_timing_events.restype = C.c_int
     lib.ks_different_families.argtypes = [C.POINTER(ks_desc), C.c_int32, C.POINTER(ks_heads), C.POINTER(ks_kernel_out),
@@ -250,6 +286,40 @@ def ks_different_families(desc, n_specs, heads, kout, ws_bytes) -> int:
     """The families of which this call evaluates the different records only."""
     return load().ks_different_families(C.byref(desc), n_specs, C.byref(heads),
                                         None if kout is None else C.byref(kout), ws_bytes)
+
+
+def ks_gated_forward(heads, rows, z_ptr, stream, check=True):
+    st = load().ks_gated_forward(C.byref(heads), C.byref(rows), z_ptr, stream)
+    return _check(st) if check else st
+
+
+def ks_gated_workspace_bytes(heads, rows) -> int:
+    return load().ks_gated_workspace_bytes(C.byref(heads), C.byref(rows))
+
+
+def ks_gated_backward(heads, rows, dz_ptr, grad, ws_ptr, ws_bytes, stream, check=True):
+    st = load().ks_gated_backward(C.byref(heads), C.byref(rows), dz_ptr, C.byref(grad), ws_ptr, ws_bytes, stream)
+    return _check(st) if check else st
+
+
+def ks_gated_loss(heads, rows, target, loss_ptr, z_ptr, grad, ws_ptr, ws_bytes, stream, check=True):
+    """grad: a ks_gated_grad, or None for the loss alone; z_ptr may be None."""
+    st = load().ks_gated_loss(C.byref(heads), C.byref(rows), C.byref(target), loss_ptr, z_ptr,
+                              None if grad is None else C.byref(grad), ws_ptr, ws_bytes, stream)
+    return _check(st) if check else st
+
+
+def ks_features(desc, specs_ptr, n_specs, in_dim, precision, x_ptr, ldx, t_roof_ptr, ws_ptr, ws_bytes, stream,
+                check=True):
+    st = load().ks_features(C.byref(desc), specs_ptr, n_specs, in_dim, precision, x_ptr, ldx, t_roof_ptr, ws_ptr,
+                            ws_bytes, stream)
+    return _check(st) if check else st
+
+
+def ks_adamw(config, tensors, stream, check=True):
+    """tensors: a ctypes array of ks_tensor (see adamw_tensors)."""
+    st = load().ks_adamw(C.byref(config), tensors, len(tensors), stream)
+    return _check(st) if check else st
 
 
 def ks_set_timing_events(before, after, check=True):
@@ -445,6 +515,105 @@ def step_outputs(n_steps: int, n_specs: int, device="cuda"):
 def current_stream() -> int:
     import torch
     return torch.cuda.current_stream().cuda_stream
+
+
+# --------------------------------------------------------------------------
+# gated heads and their fitting: torch device tensors -> ctypes structs.  The
+# structs hold addresses only: keep the tensors while the structs are used.
+# --------------------------------------------------------------------------
+def _precision(t) -> int:
+    import torch
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"{t.dtype} is neither float32 nor bfloat16")
+    return KS_BF16 if t.dtype == torch.bfloat16 else KS_F32
+
+
+def _whole(t):
+    if t is not None and not t.is_contiguous():
+        raise ValueError("a tensor is not contiguous")
+    return _ptr(t)
+
+
+def gated_heads(w1, w2, w3, b3) -> ks_heads:
+    """Gated heads (mode KS_ETA_GATED) over w1, w2 [NFAM][hidden][in_dim], w3
+    [NFAM][hidden], b3 [NFAM], all fp32 or all bf16."""
+    hd = ks_heads()
+    _, hd.hidden, hd.in_dim = w1.shape
+    want = {"w1": (NFAM, hd.hidden, hd.in_dim), "w2": (NFAM, hd.hidden, hd.in_dim), "w3": (NFAM, hd.hidden), "b3": (NFAM,)}
+    for name, t in (("w1", w1), ("w2", w2), ("w3", w3), ("b3", b3)):
+        if tuple(t.shape) != want[name] or t.dtype != w1.dtype:
+            raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}, not {w1.dtype} {want[name]}")
+        setattr(hd, name, _whole(t))
+    hd.precision, hd.mode = _precision(w1), KS_ETA_GATED
+    return hd
+
+
+def feature_rows(x, fam_off) -> ks_rows:
+    """Feature rows x [n][in_dim] (any row stride), grouped by family."""
+    r = ks_rows()
+    if x.dim() != 2 or (x.numel() and x.stride(1) != 1):
+        raise ValueError("x is not [rows][in_dim] with adjacent elements")
+    r.n_rows = x.shape[0]
+    for f in range(NFAM + 1):
+        r.fam_off[f] = int(fam_off[f])
+    r.x, r.ldx = _ptr(x) if x.numel() else None, max(x.stride(0), x.shape[1])
+    return r
+
+
+def gated_grad(w1=None, w2=None, w3=None, b3=None, x=None) -> ks_gated_grad:
+    """Where the gradients go: fp32 tensors of the weights' shapes; x [n][in_dim]
+    of the rows' type (any row stride) or None."""
+    g = ks_gated_grad()
+    for name, t in (("w1", w1), ("w2", w2), ("w3", w3), ("b3", b3)):
+        if t is not None and _precision(t) != KS_F32:
+            raise ValueError(f"the gradient of {name} is not fp32")
+        setattr(g, name, _whole(t))
+    if x is not None:
+        if x.dim() != 2 or (x.numel() and x.stride(1) != 1):
+            raise ValueError("x is not [rows][in_dim] with adjacent elements")
+        g.x, g.ldx = _ptr(x) if x.numel() else None, max(x.stride(0), x.shape[1])
+    return g
+
+
+def eta_target(eta, weight=None, huber=float("inf")) -> ks_eta_target:
+    """Measured eta (fp32) of each row and the rows' weights (fp32) or None."""
+    for t in (eta, weight):
+        if t is not None and _precision(t) != KS_F32:
+            raise ValueError("eta or weight is not fp32")
+    if weight is not None and weight.shape != eta.shape:
+        raise ValueError("weight is not of eta's shape")
+    return ks_eta_target(_whole(eta) if eta.numel() else None,
+                         None if weight is None or not weight.numel() else _whole(weight), huber)
+
+
+def adamw_tensors(tensors):
+    """tensors: dicts of param (fp32), grad (fp32 or bf16), m, v and optionally
+    m_exp, v_exp (states of 8 bits), copy (bf16), weight_decay.  Returns the
+    ctypes array ks_adamw takes."""
+    import torch
+    arr = (ks_tensor * len(tensors))()
+    for i, d in enumerate(tensors):
+        t, n = arr[i], d["param"].numel()
+        want = {"param": (torch.float32, n), "m": (None, n), "v": (None, n), "grad": (None, n), "copy": (torch.bfloat16, n),
+                "m_exp": (torch.uint8, -(-n // 64)), "v_exp": (torch.uint8, -(-n // 64))}
+        for name, (dtype, size) in want.items():
+            v = d.get(name)
+            if v is None:
+                continue
+            if v.numel() != size or (dtype is not None and v.dtype != dtype):
+                raise ValueError(f"tensor {i}: {name} is {v.dtype} of {v.numel()} elements, not {size}")
+            setattr(t, name, _whole(v) if size else None)
+        states = ((torch.float32,) * 2 if d.get("m_exp") is None else (torch.float8_e4m3fn, torch.float8_e5m2))
+        if (d["m"].dtype, d["v"].dtype) != states:
+            raise ValueError(f"tensor {i}: states of {d['m'].dtype} and {d['v'].dtype}, not {states}")
+        t.n, t.weight_decay, t.grad_type = n, d.get("weight_decay", 0.0), _precision(d["grad"])
+    return arr
+
+
+def adamw_config(lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, state_bits=32, step=1,
+                 step_dev=None) -> ks_adamw_config:
+    """step_dev: an int32 tensor of one element counting the steps made, or None."""
+    return ks_adamw_config(lr, beta1, beta2, eps, grad_scale, state_bits, 0, step, _ptr(step_dev))
 
 
 # --------------------------------------------------------------------------

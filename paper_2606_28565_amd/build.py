@@ -45,11 +45,11 @@ def build(verbose: bool = False) -> str:
     common = ["-I", INCLUDE, "-I", CSRC]
     jobs = []
     # the heads' instantiations of the evaluation kernel compile in parts
-    for heads in range(4):
+    for heads in range(5):
         jobs.append(("ks_kernels.hip", f"ks_kernels{heads}", [HIPCC, *DEVICE_FLAGS, *common, f"-DKS_HEADS={heads}"]))
-    for src in ("ks_unique.hip", "ks_finish.hip", "ks_expand.hip", "ks_static.hip"):
+    for src in ("ks_gated.hip", "ks_unique.hip", "ks_finish.hip", "ks_expand.hip", "ks_static.hip", "ks_adamw.hip"):
         jobs.append((src, os.path.splitext(src)[0], [HIPCC, *DEVICE_FLAGS, *common]))
-    for src in ("ks_api.cpp", "ks_sim.cpp"):
+    for src in ("ks_api.cpp", "ks_sim.cpp", "ks_fit.cpp"):
         jobs.append((src, os.path.splitext(src)[0], [HIPCC, *HOST_FLAGS, *common, "-D__HIP_PLATFORM_AMD__"]))
 
     def compile_one(job):

@@ -101,9 +101,12 @@ constexpr double kUniqSpreadFew = 1.5e12, kUniqSpread = 2.5e12;
 // (the most a pair can save: fp32 heads 32-128)
 constexpr double kUniqF32Rate = 1.9e14, kUniqMost = 2.0 * 128 * (32 + 128) / kUniqF32Rate;
 
-double head_rate(const ks_heads *h) {
-  if (h->precision == KS_F32) return kUniqF32Rate;
-  return h->hidden == 64 ? 0.65e15 : 1.2e15;
+// the head's seconds per pair
+double head_secs(const ks_heads *h) {
+  if (h->mode == KS_ETA_GATED)
+    return h->hidden * (h->precision == KS_BF16 ? 0.45e-12 : h->in_dim == 16 ? 0.5e-12 : 0.85e-12);
+  const double rate = h->precision == KS_F32 ? kUniqF32Rate : h->hidden == 64 ? 0.65e15 : 1.2e15;
+  return 2.0 * h->hidden * (h->in_dim + h->hidden) / rate;
 }
 
 // The different records of a call: which families, and the room for their
@@ -277,7 +280,8 @@ ks_status head_kind(const ks_heads *h, int *kind) {
   if (h->bounded_mask & ~all) return fail(KS_EINVAL, "heads.bounded_mask 0x%x has bits beyond the families",
                                           h->bounded_mask);
   if (h->bounded_mask && !h->bounded) return fail(KS_EINVAL, "heads.bounded is NULL with a nonzero mask");
-  if (h->mode != KS_ETA_ONE && h->mode != KS_ETA_MLP) return fail(KS_EINVAL, "heads.mode %d unknown", h->mode);
+  if (h->mode != KS_ETA_ONE && h->mode != KS_ETA_MLP && h->mode != KS_ETA_GATED)
+    return fail(KS_EINVAL, "heads.mode %d unknown", h->mode);
   if (h->grid_mask & ~all) return fail(KS_EINVAL, "heads.grid_mask 0x%x has bits beyond the families", h->grid_mask);
   if (h->grid_mask) {
     if (!h->grid) return fail(KS_EINVAL, "heads.grid is NULL with a nonzero mask");
@@ -300,6 +304,13 @@ ks_status head_kind(const ks_heads *h, int *kind) {
   // families, eta = 1 for the rest)
   if (h->mode == KS_ETA_ONE || h->bounded_mask == all) {
     *kind = (h->bounded_mask | h->grid_mask) ? ks::kBoundedOnly : ks::kEtaOne;
+    return KS_OK;
+  }
+  if (h->mode == KS_ETA_GATED) {
+    const ks_status st = ks::check_gated(h);
+    if (st != KS_OK) return st;
+    if (h->precision == KS_F32) *kind = h->in_dim == 16 ? ks::kGatedF32_16 : ks::kGatedF32_32;
+    else *kind = h->in_dim == 16 ? ks::kGatedBF16_16 : ks::kGatedBF16_32;
     return KS_OK;
   }
   if (!h->w1 || !h->w2 || !h->b2 || !h->w3 || !h->b3) return fail(KS_EINVAL, "a head parameter pointer is NULL");
@@ -361,24 +372,25 @@ void fill_eval(ks::EvalParams &p, const ks_desc *d, const ks_spec *specs, int32_
   p.n_tiles = t.tile_off[KS_NFAM];
   p.spec_chunk = n_specs;
   p.n_chunks = 1;
-  p.bounded_mask = h->bounded_mask;
-  p.bounded = h->bounded_mask ? h->bounded : nullptr;
-  p.grid_mask = h->grid_mask;
-  p.grid = h->grid_mask ? h->grid : nullptr;
+  p.bounded_mask = h ? h->bounded_mask : 0;
+  p.bounded = p.bounded_mask ? h->bounded : nullptr;
+  p.grid_mask = h ? h->grid_mask : 0;
+  p.grid = p.grid_mask ? h->grid : nullptr;
   p.grid_nodes = 0;
   for (int a = 0; a < 3; ++a) {
-    p.grid_axis[a] = h->grid_mask ? h->grid_axis[a] : 0;
-    p.grid_n[a] = h->grid_mask ? h->grid_n[a] : 2;
-    p.grid_lo[a] = h->grid_mask ? (float)h->grid_lo[a] : 0.0f;
-    p.grid_scale[a] = h->grid_mask ? (float)((h->grid_n[a] - 1) / (h->grid_hi[a] - h->grid_lo[a])) : 0.0f;
+    p.grid_axis[a] = p.grid_mask ? h->grid_axis[a] : 0;
+    p.grid_n[a] = p.grid_mask ? h->grid_n[a] : 2;
+    p.grid_lo[a] = p.grid_mask ? (float)h->grid_lo[a] : 0.0f;
+    p.grid_scale[a] = p.grid_mask ? (float)((h->grid_n[a] - 1) / (h->grid_hi[a] - h->grid_lo[a])) : 0.0f;
   }
-  if (h->grid_mask) p.grid_nodes = p.grid_n[0] * p.grid_n[1] * p.grid_n[2];
-  if (h->mode == KS_ETA_MLP) {
+  if (p.grid_mask) p.grid_nodes = p.grid_n[0] * p.grid_n[1] * p.grid_n[2];
+  if (h && h->mode != KS_ETA_ONE) {
     p.w1 = h->w1;
     p.w2 = h->w2;
     p.b2 = h->b2;
     p.w3 = h->w3;
     p.b3 = h->b3;
+    p.hidden = h->hidden;
   }
   if (out) {
     p.o_flops = out->flops;
@@ -401,7 +413,7 @@ bool takes_uniq(const ks_desc *d, int32_t n_specs, const ks_heads *h, int kind, 
   if ((double)d->n_rows * n_specs * kUniqMost < kUniqSecs) return false;
   *pair = kout && (kout->t_roof || kout->eta || kout->t_kernel);
   if (kout && kout->source && h->grid_mask) return false;
-  const double head = 2.0 * h->hidden * (h->in_dim + h->hidden) / head_rate(h);
+  const double head = head_secs(h);
   const int outs = kout ? (kout->t_roof != nullptr) + (kout->eta != nullptr) + (kout->t_kernel != nullptr) : 0;
   double saved = 0.0, cost = kUniqSecs + (*pair ? kUniqPairSecs : 0.0);
   if (kout && (kout->flops || kout->bytes || kout->blocks)) cost += kUniqCountSecs;
@@ -633,6 +645,30 @@ size_t ks::eval_workspace_bytes(const int64_t fam_off[KS_NFAM + 1], int64_t n_st
   d.n_rows = fam_off[KS_NFAM];
   d.n_steps = n_steps;
   return layout_of(&d, n_specs).total;
+}
+
+ks_status ks::check_gated(const ks_heads *h) {
+  if (!h) return fail(KS_EINVAL, "heads is NULL");
+  if (h->mode != KS_ETA_GATED) return fail(KS_EINVAL, "heads.mode %d not KS_ETA_GATED", h->mode);
+  if (!h->w1 || !h->w2 || !h->w3 || !h->b3) return fail(KS_EINVAL, "a head parameter pointer is NULL");
+  if (h->precision != KS_F32 && h->precision != KS_BF16) return fail(KS_EINVAL, "heads.precision %d unknown", h->precision);
+  if (h->in_dim != 16 && h->in_dim != 32) return fail(KS_EINVAL, "heads.in_dim %d not 16 or 32", h->in_dim);
+  if (h->hidden < 1 || h->hidden > 256) return fail(KS_EINVAL, "gated heads.hidden %d outside 1..256", h->hidden);
+  const uintptr_t at = reinterpret_cast<uintptr_t>(h->w1) | reinterpret_cast<uintptr_t>(h->w2) |
+                       reinterpret_cast<uintptr_t>(h->w3) | reinterpret_cast<uintptr_t>(h->b3);
+  if (at % (h->precision == KS_F32 ? 4 : 2)) return fail(KS_EINVAL, "a head parameter pointer is not aligned to its type");
+  return KS_OK;
+}
+
+ks_status ks::feature_prologue(const ks_desc *desc, const ks_spec *specs, int32_t n_specs, void *ws, size_t ws_bytes,
+                               EvalParams *p, hipStream_t stream) {
+  Layout L;
+  ks_status st = check_common(desc, specs, n_specs, ws, ws_bytes, &L);
+  if (st != KS_OK) return st;
+  st = prologue(desc, specs, n_specs, static_cast<char *>(ws), L, false, stream);
+  if (st != KS_OK) return st;
+  fill_eval(*p, desc, specs, n_specs, nullptr, nullptr, static_cast<char *>(ws), L);
+  return KS_OK;
 }
 
 // Replaced, where the kernels are linked, by the launch that does both.

@@ -1,0 +1,143 @@
+// The gated efficiency head's device code: the block that the evaluation
+// (ks_kernels.hip) and the row operators (ks_gated.hip) share.
+//
+//   z = w3 . (silu(W1 x) * (W2 x)) + b3,   silu(g) = g / (1 + exp(-g))
+//
+// A wave takes 64 rows: two column blocks of 32 on the 32x32 matrix
+// instruction, the weights its row operand from LDS.  One lane then holds 16
+// of a 32-unit block's gates and ups of one row, so the activation, the product
+// and the dot product with w3 stay in the lane's registers; one exchange of the
+// wave's halves at the end completes the sums over the units.
+#pragma once
+
+#include <stdint.h>
+
+namespace ks {
+namespace gated {
+
+typedef __bf16 gbf16x8 __attribute__((ext_vector_type(8)));
+typedef float gf32x16 __attribute__((ext_vector_type(16)));
+typedef float gf32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t gu32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kMaxHidden = 256;
+
+// 1 / (1 + exp(-g)).  exp(-g) overflows to infinity below -88: 0, as it should.
+__device__ __forceinline__ float sigmoid(float g) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504088896340736f));
+}
+
+template <bool BF16, int IN>
+struct Block {
+  static constexpr int KC = IN / 16;                  // 16-feature chunks
+  static constexpr int kFrag = BF16 ? 256 : 512;      // dwords of 32 units x 16 features
+  static constexpr int kBlk = 2 * KC * kFrag + 32;    // of 32 units: gates, ups, w3 by register and half
+  static constexpr int kLds = kMaxHidden / 32 * kBlk + 4;
+  static constexpr int OFF_B3 = kLds - 4, OFF_NB = kLds - 3;
+
+  // unit of register r in lane half h of a block's products
+  __device__ static __forceinline__ int unit_of(int h, int r) { return 8 * (r >> 2) + 4 * h + (r & 3); }
+
+  // a family's weights into LDS; units past hidden are zero (and add nothing)
+  __device__ static void stage(uint32_t *lds, const void *w1, const void *w2, const void *w3, const void *b3, int hidden,
+                               int tid, int n_threads) {
+    const int nb = (hidden + 31) / 32;
+    constexpr int E = BF16 ? 2 : 4;
+    const bool vec = ((reinterpret_cast<uintptr_t>(w1) | reinterpret_cast<uintptr_t>(w2)) & 15) == 0;
+    // one lane's 8 features of a fragment: 16 bytes of bf16, 32 of fp32
+    for (int i = tid; i < nb * 2 * KC * 64; i += n_threads) {
+      const int lane = i & 63, fr = i >> 6;
+      const int kc = fr % KC, m = (fr / KC) & 1, mb = fr / (2 * KC);
+      const int unit = mb * 32 + (lane & 31);
+      const char *src = (const char *)(m ? w2 : w1) + ((size_t)unit * IN + kc * 16 + (lane >> 5) * 8) * E;
+      uint32_t *dst = lds + mb * kBlk + (m * KC + kc) * kFrag + lane * 4;
+      gu32x4 v0 = {0, 0, 0, 0}, v1 = {0, 0, 0, 0};
+      if (unit < hidden) {
+        if (vec) {
+          v0 = *(const gu32x4 *)src;
+          if constexpr (!BF16) v1 = *(const gu32x4 *)(src + 16);
+        } else if constexpr (BF16) {
+          const uint16_t *h = (const uint16_t *)src;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v0[j] = h[2 * j] | (uint32_t)h[2 * j + 1] << 16;
+        } else {
+          const uint32_t *f = (const uint32_t *)src;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v0[j] = f[j], v1[j] = f[4 + j];
+        }
+      }
+      *(gu32x4 *)dst = v0;
+      if constexpr (!BF16) *(gu32x4 *)(dst + 256) = v1;
+    }
+    for (int i = tid; i < nb * 32; i += n_threads) {
+      const int mb = i >> 5, unit = mb * 32 + unit_of((i >> 4) & 1, i & 15);
+      float w = 0.0f;
+      if (unit < hidden)
+        w = BF16 ? __builtin_bit_cast(float, (uint32_t)((const uint16_t *)w3)[unit] << 16) : ((const float *)w3)[unit];
+      ((float *)lds)[mb * kBlk + 2 * KC * kFrag + (i & 31)] = w;
+    }
+    if (tid == 0) {
+      ((float *)lds)[OFF_B3] = BF16 ? __builtin_bit_cast(float, (uint32_t)*(const uint16_t *)b3 << 16) : *(const float *)b3;
+      lds[OFF_NB] = (uint32_t)nb;
+    }
+  }
+
+  // the column operand of 64 rows: a lane holds, of row (lane mod 32) of each
+  // column block, the eight features of its half
+  struct Rows {
+    gu32x4 v[2][KC][BF16 ? 1 : 2];
+  };
+
+  __device__ static __forceinline__ void products(const uint32_t *frag, int lane, const Rows &x, int kc, gf32x16 (&c)[2]) {
+    if constexpr (BF16) {
+      const gbf16x8 a = __builtin_bit_cast(gbf16x8, *(const gu32x4 *)(frag + lane * 4));
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        c[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(gbf16x8, x.v[i][kc][0]), c[i], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        // (whole vectors cast: a cast of one element of a vector in memory reads its first)
+        const gf32x4 a = __builtin_bit_cast(gf32x4, *(const gu32x4 *)(frag + h * 256 + lane * 4));
+        const gf32x4 b0 = __builtin_bit_cast(gf32x4, x.v[0][kc][h]), b1 = __builtin_bit_cast(gf32x4, x.v[1][kc][h]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          c[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b0[j], c[0], 0, 0, 0);
+          c[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b1[j], c[1], 0, 0, 0);
+        }
+      }
+    }
+  }
+
+  // z of row (lane) of the 64
+  __device__ static __forceinline__ float z_of(const Rows &x, const uint32_t *lds) {
+    const int lane = threadIdx.x & 63;
+    const int nb = __builtin_amdgcn_readfirstlane(lds[OFF_NB]);
+    float z[2] = {0.0f, 0.0f};
+#pragma unroll 1
+    for (int mb = 0; mb < nb; ++mb) {
+      const uint32_t *blk = lds + mb * kBlk;
+      gf32x16 g[2] = {gf32x16{}, gf32x16{}}, u[2] = {gf32x16{}, gf32x16{}};
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc) {
+        products(blk + kc * kFrag, lane, x, kc, g);
+        products(blk + (KC + kc) * kFrag, lane, x, kc, u);
+      }
+      const float *w3 = (const float *)blk + 2 * KC * kFrag + (lane >> 5) * 16;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float w = w3[r];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) z[i] = fmaf(w, g[i][r] * sigmoid(g[i][r]) * u[i][r], z[i]);
+      }
+    }
+    // lanes 32.. of the first block's sums for lanes ..31 of the second's
+    const auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, z[0]), __builtin_bit_cast(uint32_t, z[1]),
+                                                    false, false);
+    return __builtin_bit_cast(float, (uint32_t)s[0]) + __builtin_bit_cast(float, (uint32_t)s[1]) +
+           ((const float *)lds)[OFF_B3];
+  }
+};
+
+}  // namespace gated
+}  // namespace ks

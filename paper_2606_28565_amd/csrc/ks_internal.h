@@ -30,6 +30,7 @@ enum HeadKind : int {
   kEtaOne = 0,
   kF32_16_64, kF32_16_128, kF32_32_64, kF32_32_128,
   kBF16_16_64, kBF16_16_128, kBF16_16_256, kBF16_32_64, kBF16_32_128, kBF16_32_256,
+  kGatedF32_16, kGatedF32_32, kGatedBF16_16, kGatedBF16_32,   // any hidden up to 256
   kBoundedOnly,   // no MLP: bounded-head and grid families, eta = 1 for the rest
   kNumKinds
 };
@@ -111,6 +112,7 @@ struct EvalParams {
   int32_t spec_chunk, n_chunks;
   // heads
   const void *w1, *w2, *b2, *w3, *b3;
+  int32_t hidden;              // of the gated heads (the others' kind says it)
   uint32_t bounded_mask;       // families that take the bounded analytical head
   const float *bounded;        // [KS_NFAM][2][16]: g then a
   uint32_t grid_mask;          // families with a measured eta grid (Tier B)
@@ -242,6 +244,15 @@ size_t eval_workspace_bytes(const int64_t fam_off[KS_NFAM + 1], int64_t n_steps,
 // the thread-local message ks_last_error() reports; returns st
 ks_status set_error(ks_status st, const char *fmt, ...);
 
+// checks, workspace and prologue of an evaluation call without heads or outputs
+// (ks_features); on KS_OK p is what its kernel takes
+ks_status feature_prologue(const ks_desc *desc, const ks_spec *specs, int32_t n_specs, void *ws, size_t ws_bytes,
+                           EvalParams *p, hipStream_t stream);
+hipError_t launch_features(const EvalParams &p, int in_dim, bool bf16, void *x, int64_t ldx, float *t_roof,
+                           hipStream_t s);
+// checks of a gated head's fields, weights included
+ks_status check_gated(const ks_heads *h);
+
 hipError_t launch_clear(uint32_t *err, uint32_t *range, int64_t n_range, hipStream_t s);
 hipError_t launch_spec_prep(const ks_spec *specs, int32_t n_specs, SpecC *out, uint32_t *err, hipStream_t s);
 // launch_clear, then the spec constants of launch_spec_prep (in the same
@@ -275,5 +286,71 @@ hipError_t launch_finish(const FinishParams &p, hipStream_t s);
 // per-pair eta source of a call without a grid (p.o_src, families' bounded bit)
 hipError_t launch_fill_source(const EvalParams &p, hipStream_t s);
 hipError_t launch_validate(const ValidateParams &p, hipStream_t s);
+
+// ---- gated heads over rows (ks_gated.hip)
+// A forward workgroup takes fwd_tiles 64-row tiles of one family, a backward
+// workgroup bwd_rows rows of one (a multiple of 16 per row group).
+struct GatedParams {
+  const void *x;
+  int64_t ldx;
+  bool vec;                          // rows are 16-byte aligned
+  int64_t fam_off[KS_NFAM + 1];
+  int32_t in_dim, hidden;
+  bool bf16;
+  const void *w1, *w2, *w3, *b3;
+  int32_t fwd_tiles, bwd_rows;
+  int32_t fwd_wg[KS_NFAM + 1], bwd_wg[KS_NFAM + 1];
+  float *z;                          // nullable
+  // the loss (eta null: none)
+  const float *eta, *weight;
+  float huber;
+  float *dz_out;                     // w rho'(r) dr/dz, not yet over sum w; null: the loss alone
+  double *loss_part;                 // [forward workgroups][2]: sum w rho, sum w
+  float *loss;                       // [KS_NFAM]
+  // gradients
+  const float *dz;
+  float *part;                       // [backward workgroups][gated_part_size()]
+  float *g_w1, *g_w2, *g_w3, *g_b3;  // null: none
+  void *g_x;                         // nullable
+  int64_t g_ldx;
+  bool g_vec;
+};
+constexpr int kGatedGroup = 64;      // units per wave of the backward kernel
+constexpr int gated_groups(int hidden) { return (hidden + kGatedGroup - 1) / kGatedGroup; }
+// floats of a backward workgroup's sums: per group of 64 units dW1, dW2 and dw3; db3
+constexpr int gated_part_size(int hidden, int in_dim) {
+  return gated_groups(hidden) * kGatedGroup * (2 * in_dim + 1) + 1;
+}
+hipError_t launch_gated_forward(const GatedParams &p, hipStream_t s);
+hipError_t launch_gated_backward(const GatedParams &p, hipStream_t s);
+hipError_t launch_gated_rows(const GatedParams &p, hipStream_t s);     // g_x
+hipError_t launch_gated_reduce(const GatedParams &p, hipStream_t s);   // gradients and the loss
+
+// ---- AdamW (ks_adamw.hip)
+constexpr int kAdamTensors = 48;     // per launch: their table travels in the kernel arguments
+constexpr int kAdamChunk = 4096;     // elements per workgroup
+struct AdamTensor {
+  float *p;
+  const void *g;
+  void *m, *v;
+  uint8_t *m_exp, *v_exp;
+  uint16_t *copy;
+  int64_t n;
+  float decay;                       // 1 - lr weight_decay
+  uint32_t flags;                    // kAdam...
+};
+enum : uint32_t { kAdamVec = 1u, kAdamGrad16 = 2u };
+struct AdamParams {
+  AdamTensor t[kAdamTensors];
+  uint32_t chunk_off[kAdamTensors + 1];
+  int32_t n_tensors;
+  float b1, c1, b2, c2, eps, grad_scale;   // c = 1 - beta
+  float lr, step_size, inv_sqrt;     // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+  float log_b1, log_b2;              // for a step counted on the device
+  const uint32_t *step_dev;
+};
+static_assert(sizeof(AdamParams) <= 4096, "the table fits the kernel arguments");
+hipError_t launch_adamw(const AdamParams &p, bool eight, hipStream_t s);
+hipError_t launch_adamw_count(uint32_t *step_dev, hipStream_t s);
 
 }  // namespace ks

@@ -26,6 +26,7 @@
 #include <utility>
 
 #include "ks_agg.h"
+#include "ks_gated.h"
 #include "ks_internal.h"
 
 namespace ks {
@@ -1396,6 +1397,49 @@ struct HeadF32 {
   }
 };
 
+// The gated block (ks_gated.h) as a head: a lane's row of features becomes the
+// column operand by exchanging the wave's halves.
+template <bool BF16, int IN>
+struct HeadGated {
+  using G = gated::Block<BF16, IN>;
+  static constexpr bool kRaw = false;
+  static constexpr int LDS_DW = G::kLds;
+  static constexpr bool kMlp = true;
+
+  __device__ static void stage(uint32_t *lds, int fam, const EvalParams &p) {
+    constexpr int E = BF16 ? 2 : 4;
+    const size_t w = (size_t)fam * p.hidden * IN * E;
+    G::stage(lds, (const char *)p.w1 + w, (const char *)p.w2 + w, (const char *)p.w3 + (size_t)fam * p.hidden * E,
+             (const char *)p.b3 + fam * E, p.hidden, (int)threadIdx.x, kWgThreads);
+  }
+
+  __device__ static __forceinline__ float mlp(const float (&x)[IN], const uint32_t *lds) {
+    typename G::Rows r;
+#pragma unroll
+    for (int kc = 0; kc < G::KC; ++kc) {
+      if constexpr (BF16) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t lo = pack_bf16(x[16 * kc + 2 * q], x[16 * kc + 2 * q + 1]);
+          uint32_t hi = pack_bf16(x[16 * kc + 8 + 2 * q], x[16 * kc + 9 + 2 * q]);
+          swap32(lo, hi);
+          r.v[0][kc][0][q] = lo;
+          r.v[1][kc][0][q] = hi;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          uint32_t lo = __builtin_bit_cast(uint32_t, x[16 * kc + j]), hi = __builtin_bit_cast(uint32_t, x[16 * kc + 8 + j]);
+          swap32(lo, hi);
+          r.v[0][kc][j >> 2][j & 3] = lo;
+          r.v[1][kc][j >> 2][j & 3] = hi;
+        }
+      }
+    }
+    return G::z_of(r, lds);
+  }
+};
+
 struct HeadOne {
   static constexpr int LDS_DW = 1;
   static constexpr bool kMlp = false;
@@ -1419,6 +1463,10 @@ template <> struct KindOf<kBF16_16_256> { using H = HeadBF16<16, 256>; static co
 template <> struct KindOf<kBF16_32_64> { using H = HeadBF16<32, 64>; static constexpr int IN = 32; };
 template <> struct KindOf<kBF16_32_128> { using H = HeadBF16<32, 128>; static constexpr int IN = 32; };
 template <> struct KindOf<kBF16_32_256> { using H = HeadBF16<32, 256>; static constexpr int IN = 32; };
+template <> struct KindOf<kGatedF32_16> { using H = HeadGated<false, 16>; static constexpr int IN = 16; };
+template <> struct KindOf<kGatedF32_32> { using H = HeadGated<false, 32>; static constexpr int IN = 32; };
+template <> struct KindOf<kGatedBF16_16> { using H = HeadGated<true, 16>; static constexpr int IN = 16; };
+template <> struct KindOf<kGatedBF16_32> { using H = HeadGated<true, 32>; static constexpr int IN = 32; };
 
 // ------------------------------------------------------------ segmented scan
 // Inclusive scan of a wave's 64 values, segmented by sorted keys, with DPP
@@ -1486,6 +1534,10 @@ template <> struct MinWg<kBF16_16_64> { static constexpr int value = 2; };
 template <> struct MinWg<kBF16_16_128> { static constexpr int value = 2; };
 template <> struct MinWg<kBF16_32_64> { static constexpr int value = 2; };
 template <> struct MinWg<kBF16_32_128> { static constexpr int value = 2; };
+template <> struct MinWg<kGatedF32_16> { static constexpr int value = 2; };
+template <> struct MinWg<kGatedF32_32> { static constexpr int value = 2; };
+template <> struct MinWg<kGatedBF16_16> { static constexpr int value = 2; };
+template <> struct MinWg<kGatedBF16_32> { static constexpr int value = 2; };
 
 // One wave's tile: 64 consecutive records of one family (nvalid = 0 for an
 // idle wave of a family's last workgroup tile).
@@ -2776,6 +2828,63 @@ __global__ void k_validate(ValidateParams p) {
 }
 #endif
 
+// ------------------------------------------------------------ feature rows
+// The features of every (record, spec) pair as k_eval forms them, stored: a wave
+// takes 64 records of one family and spec_chunk specs, a lane its record's row
+// of IN features per spec.  Written bytes bound it.
+#if KS_HEADS == 0
+template <int IN, bool BF16>
+__global__ __launch_bounds__(kWgThreads) void k_features(EvalParams p, char *x, int64_t ldx, float *t_roof, bool vec) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wt = item_tile((int)blockIdx.x, p.n_chunks), s_lo = item_range((int)blockIdx.x, p.n_chunks) * p.spec_chunk;
+  const Tile t = locate(p, wt, wave, 0);
+  if (t.nvalid == 0) return;
+  const Fields f = load_fields<false, true>(p, t, lane);
+  const bool valid = lane < t.nvalid;
+  uint32_t bad = (int64_t)f.st >= p.n_steps ? kErrStep : 0u;
+  const CntF c = record_counts_f(t.fam, f.m, f.n, f.k, f.a, f.b, f.st, p, bad);
+  const RowC rc = row_consts(c.B, c.F, c.Bt, c.M, f.n, f.k);
+  if (valid && bad) atomicOr(p.err, bad);
+  const bool small = __ballot(rc.B >= kSmallB) == 0;
+  const int64_t n_fam = t.fam_hi - t.fam_lo;
+  for (int s = s_lo; s < min(s_lo + p.spec_chunk, p.n_specs); ++s) {
+    const SpecC sc = spec_at(p.spec_c, s);
+    const Roof o = small ? roofline<true>(rc, sc) : roofline<false>(rc, sc);
+    float v[IN];
+    features<IN>(rc, sc, o, v);
+    if (!valid) continue;
+    const int64_t pair = p.n_specs * t.fam_lo + s * n_fam + (t.row0 - t.fam_lo) + lane;
+    if (bad) {
+#pragma unroll
+      for (int i = 0; i < IN; ++i) v[i] = 0.0f;
+    }
+    if (t_roof) t_roof[pair] = bad ? 0.0f : o.t_roof;
+    char *dst = x + pair * ldx * (BF16 ? 2 : 4);
+    if constexpr (BF16) {
+      uint32_t b[IN / 2];
+#pragma unroll
+      for (int i = 0; i < IN / 2; ++i) b[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+      if (vec) {
+#pragma unroll
+        for (int i = 0; i < IN / 8; ++i) ((u32x4 *)dst)[i] = u32x4{b[4 * i], b[4 * i + 1], b[4 * i + 2], b[4 * i + 3]};
+      } else {
+#pragma unroll
+        for (int i = 0; i < IN; ++i) ((uint16_t *)dst)[i] = (uint16_t)(b[i / 2] >> (16 * (i & 1)));
+      }
+    } else {
+      if (vec) {
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int i = 0; i < IN / 4; ++i) ((f32x4 *)dst)[i] = f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+      } else {
+#pragma unroll
+        for (int i = 0; i < IN; ++i) ((float *)dst)[i] = v[i];
+      }
+    }
+  }
+}
+#endif
+
 // ------------------------------------------------------------ launchers
 // The persistent grid: as many workgroups as are resident at once (the
 // occupancy the compiled kernel's registers and LDS allow, times the CU
@@ -2858,7 +2967,7 @@ hipError_t launch_uniq(const EvalParams &p, hipStream_t s) {
 }
 
 // This file is compiled once per KS_HEADS (in parallel): 1 the fp32 heads, 2 the
-// bf16 heads up to hidden 128, 3 those of 256, 0 everything else.
+// bf16 heads up to hidden 128, 3 those of 256, 4 the gated heads, 0 everything else.
 #if KS_HEADS == 1
 template hipError_t launch_kind<kF32_16_64>(const EvalParams &, hipStream_t);
 template hipError_t launch_uniq<kF32_16_64>(const EvalParams &, hipStream_t);
@@ -2885,6 +2994,16 @@ template hipError_t launch_uniq<kBF16_16_256>(const EvalParams &, hipStream_t);
 template hipError_t launch_kind<kBF16_32_256>(const EvalParams &, hipStream_t);
 template hipError_t launch_uniq<kBF16_32_256>(const EvalParams &, hipStream_t);
 #endif
+#if KS_HEADS == 4
+template hipError_t launch_kind<kGatedF32_16>(const EvalParams &, hipStream_t);
+template hipError_t launch_uniq<kGatedF32_16>(const EvalParams &, hipStream_t);
+template hipError_t launch_kind<kGatedF32_32>(const EvalParams &, hipStream_t);
+template hipError_t launch_uniq<kGatedF32_32>(const EvalParams &, hipStream_t);
+template hipError_t launch_kind<kGatedBF16_16>(const EvalParams &, hipStream_t);
+template hipError_t launch_uniq<kGatedBF16_16>(const EvalParams &, hipStream_t);
+template hipError_t launch_kind<kGatedBF16_32>(const EvalParams &, hipStream_t);
+template hipError_t launch_uniq<kGatedBF16_32>(const EvalParams &, hipStream_t);
+#endif
 #if KS_HEADS == 0
 extern template hipError_t launch_kind<kF32_16_64>(const EvalParams &, hipStream_t);
 extern template hipError_t launch_uniq<kF32_16_64>(const EvalParams &, hipStream_t);
@@ -2906,6 +3025,14 @@ extern template hipError_t launch_kind<kBF16_16_256>(const EvalParams &, hipStre
 extern template hipError_t launch_uniq<kBF16_16_256>(const EvalParams &, hipStream_t);
 extern template hipError_t launch_kind<kBF16_32_256>(const EvalParams &, hipStream_t);
 extern template hipError_t launch_uniq<kBF16_32_256>(const EvalParams &, hipStream_t);
+extern template hipError_t launch_kind<kGatedF32_16>(const EvalParams &, hipStream_t);
+extern template hipError_t launch_uniq<kGatedF32_16>(const EvalParams &, hipStream_t);
+extern template hipError_t launch_kind<kGatedF32_32>(const EvalParams &, hipStream_t);
+extern template hipError_t launch_uniq<kGatedF32_32>(const EvalParams &, hipStream_t);
+extern template hipError_t launch_kind<kGatedBF16_16>(const EvalParams &, hipStream_t);
+extern template hipError_t launch_uniq<kGatedBF16_16>(const EvalParams &, hipStream_t);
+extern template hipError_t launch_kind<kGatedBF16_32>(const EvalParams &, hipStream_t);
+extern template hipError_t launch_uniq<kGatedBF16_32>(const EvalParams &, hipStream_t);
 
 static int grid_for(int64_t n, int block, int cap) {
   int64_t g = (n + block - 1) / block;
@@ -3048,6 +3175,10 @@ static hipError_t launch_direct(int kind, const EvalParams &p, hipStream_t s) {
     case kBF16_32_64: return launch_kind<kBF16_32_64>(p, s);
     case kBF16_32_128: return launch_kind<kBF16_32_128>(p, s);
     case kBF16_32_256: return launch_kind<kBF16_32_256>(p, s);
+    case kGatedF32_16: return launch_kind<kGatedF32_16>(p, s);
+    case kGatedF32_32: return launch_kind<kGatedF32_32>(p, s);
+    case kGatedBF16_16: return launch_kind<kGatedBF16_16>(p, s);
+    case kGatedBF16_32: return launch_kind<kGatedBF16_32>(p, s);
     default: return hipErrorInvalidValue;
   }
 }
@@ -3064,6 +3195,10 @@ static hipError_t launch_uniq_kind(int kind, const EvalParams &p, hipStream_t s)
     case kBF16_32_64: return launch_uniq<kBF16_32_64>(p, s);
     case kBF16_32_128: return launch_uniq<kBF16_32_128>(p, s);
     case kBF16_32_256: return launch_uniq<kBF16_32_256>(p, s);
+    case kGatedF32_16: return launch_uniq<kGatedF32_16>(p, s);
+    case kGatedF32_32: return launch_uniq<kGatedF32_32>(p, s);
+    case kGatedBF16_16: return launch_uniq<kGatedBF16_16>(p, s);
+    case kGatedBF16_32: return launch_uniq<kGatedBF16_32>(p, s);
     default: return hipErrorInvalidValue;
   }
 }
@@ -3084,6 +3219,29 @@ hipError_t launch_fill_source(const EvalParams &p, hipStream_t s) {
   const int64_t total = (int64_t)p.n_specs * p.fam_off[KS_NFAM];
   if (!p.o_src || total == 0) return hipSuccess;
   hipLaunchKernelGGL(k_fill_source, dim3(grid_for(total, 256, 8192)), dim3(256), 0, s, p.o_src, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_features(const EvalParams &p, int in_dim, bool bf16, void *x, int64_t ldx, float *t_roof,
+                           hipStream_t s) {
+  EvalParams q = p;
+  const int n_wgt = p.wgt_off[KS_NFAM];
+  if (n_wgt == 0) return hipSuccess;
+  // enough workgroups for the chip where the record tiles alone are too few
+  const int want = 1024 / n_wgt + 1;
+  q.n_chunks = want < p.n_specs ? want : p.n_specs;
+  q.spec_chunk = (p.n_specs + q.n_chunks - 1) / q.n_chunks;
+  q.n_chunks = (p.n_specs + q.spec_chunk - 1) / q.spec_chunk;
+  const bool vec = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && (ldx * (bf16 ? 2 : 4)) % 16 == 0;
+  const dim3 grid((unsigned)n_wgt * (unsigned)q.n_chunks), block(kWgThreads);
+  char *o = static_cast<char *>(x);
+  if (bf16) {
+    if (in_dim == 16) hipLaunchKernelGGL((k_features<16, true>), grid, block, 0, s, q, o, ldx, t_roof, vec);
+    else hipLaunchKernelGGL((k_features<32, true>), grid, block, 0, s, q, o, ldx, t_roof, vec);
+  } else {
+    if (in_dim == 16) hipLaunchKernelGGL((k_features<16, false>), grid, block, 0, s, q, o, ldx, t_roof, vec);
+    else hipLaunchKernelGGL((k_features<32, false>), grid, block, 0, s, q, o, ldx, t_roof, vec);
+  }
   return hipGetLastError();
 }
 

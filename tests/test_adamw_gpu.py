@@ -1,0 +1,220 @@
+"""The AdamW step over many tensors (ks_adamw) against the fp64 oracle.
+
+fp32 states: m and v come from two products and a sum, each rounded (3 half steps
+of the larger terms); the parameter's update adds the roundings of the quotient
+(square root, product, sum, quotient and product: 8 half steps of the update) and
+two of the parameter; a step counted on the device forms 1 - beta^t there, another
+12 half steps of the update.  States in 8 bits are compared with the oracle's, which
+rounds the same fp32 moments: equal to the bit."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+from oracle import ks_fit as o
+from paper_2606_28565_amd import abi
+
+pytestmark = pytest.mark.gpu
+CFG = {"lr": 1e-2, "beta1": 0.9, "beta2": 0.999, "eps": 1e-8, "grad_scale": 0.5}
+SIZES = [1, 2, 3, 63, 64, 65, 127, 1000, 4095, 4096, 4097, 9001]
+
+
+def make(sizes, bits, grad16=False, copy=True, shift=0, seed=1, zero_state=False):
+    """Host (float32 numpy) and device tensors; every array starts ``shift``
+    elements into its allocation and has a guard behind it."""
+    import torch
+    rng = np.random.default_rng(seed)
+    host, dev = [], []
+    for i, n in enumerate(sizes):
+        spread = 10.0 ** rng.uniform(-4, 0, n)
+        p, g = rng.normal(size=n), rng.normal(size=n) * spread
+        m, v = (np.zeros(n), np.zeros(n)) if zero_state else (rng.normal(size=n) * spread, (rng.normal(size=n) * spread) ** 2)
+        p, g, m, v = (a.astype(np.float32) for a in (p, g, m, v))
+        if grad16:
+            g = torch.from_numpy(g).bfloat16().float().numpy()
+        h = {"p": p, "g": g, "wd": 0.01 * (i % 3), "n": n}
+
+        def put(a, dtype):
+            t = torch.zeros(n + shift + 3, dtype=dtype, device="cuda")
+            t[shift:shift + n] = torch.from_numpy(np.ascontiguousarray(a)).to("cuda").to(dtype)
+            return t[shift:shift + n]
+        d = {"param": put(p, torch.float32), "grad": put(g, torch.bfloat16 if grad16 else torch.float32),
+             "weight_decay": h["wd"], "copy": put(p, torch.bfloat16) if copy else None}
+        if bits == 8:
+            h["qm"], h["em"] = o.encode(m, False)
+            h["qv"], h["ev"] = o.encode(v, True)
+            for key, q, e, dt in (("m", h["qm"], h["em"], torch.float8_e4m3fn), ("v", h["qv"], h["ev"], torch.float8_e5m2)):
+                d[key] = put(q.astype(np.float32), dt)
+                d[key + "_exp"] = torch.from_numpy(e.astype(np.uint8)).cuda()
+            h["m"] = o.decode(h["qm"], h["em"], n).astype(np.float32)
+            h["v"] = o.decode(h["qv"], h["ev"], n).astype(np.float32)
+        else:
+            h["m"], h["v"] = m, v
+            d["m"], d["v"] = put(m, torch.float32), put(v, torch.float32)
+        host.append(h)
+        dev.append(d)
+    return host, dev
+
+
+def values(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def check(host, dev, bits, t, cfg=CFG, counted=False):
+    for i, (h, d) in enumerate(zip(host, dev)):
+        m, v = o.moments32(h["m"], h["v"], h["g"], cfg["grad_scale"], cfg["beta1"], cfg["beta2"])
+        want = o.step(h["p"], m, v, cfg["lr"], h["wd"], cfg["beta1"], cfg["beta2"], cfg["eps"], t)
+        up = np.abs(want - h["p"].astype(np.float64) * (1 - cfg["lr"] * h["wd"]))
+        bound = (24 if counted else 12) * o.EPS * up + 3 * o.EPS * (np.abs(h["p"]) + np.abs(want))
+        got = values(d["param"])
+        assert (np.abs(got - want) <= bound).all(), (i, np.max(np.abs(got - want) / np.maximum(bound, 1e-300)))
+        if d["copy"] is not None:
+            assert (d["copy"] == d["param"].bfloat16()).all(), i
+        if bits == 32:
+            assert (values(d["m"]) == m).all() and (values(d["v"]) == v).all(), i
+        else:
+            for key, val, second in (("m", m, False), ("v", v, True)):
+                q, e = o.encode(val, second)
+                assert (d[key + "_exp"].cpu().numpy() == e).all(), (i, key)
+                assert np.array_equal(values(d[key]), q, equal_nan=True), (i, key)
+
+
+def run(dev, bits, step=3, step_dev=None, cfg=CFG):
+    import torch
+    abi.ks_adamw(abi.adamw_config(state_bits=bits, step=step, step_dev=step_dev, **cfg), abi.adamw_tensors(dev),
+                 abi.current_stream())
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("grad16", [False, True])
+@pytest.mark.parametrize("shift", [0, 1, 4])
+def test_sizes(bits, grad16, shift):
+    """Odd sizes, whole and partial blocks of 64; aligned or not."""
+    host, dev = make(SIZES, bits, grad16, shift=shift)
+    run(dev, bits)
+    check(host, dev, bits, 3)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_many_tensors(bits):
+    """More tensors than one launch takes, empty ones among them, no copies."""
+    sizes = [(7 * i) % 150 for i in range(130)]
+    host, dev = make(sizes, bits, copy=False)
+    run(dev, bits)
+    check(host, dev, bits, 3)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_large_tensor(bits):
+    host, dev = make([1_000_003, 64], bits)
+    run(dev, bits)
+    check(host, dev, bits, 3)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_nothing_behind_the_end(bits):
+    """Elements behind a tensor's last stay as they were."""
+    import torch
+    n = 70
+    host, dev = make([n], bits)
+    big = {}
+    for key, t in list(dev[0].items()):
+        if isinstance(t, torch.Tensor) and not key.endswith("_exp"):
+            b = torch.ones(256, device="cuda").to(t.dtype)
+            b[:n] = t
+            big[key], dev[0][key] = b, b[:n]
+    run(dev, bits)
+    check(host, dev, bits, 3)
+    for key, b in big.items():
+        assert (b[n:].float() == 1).all(), key
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_first_step_from_zero_states(bits):
+    host, dev = make([300], bits, zero_state=True)
+    run(dev, bits, step=1)
+    check(host, dev, bits, 1)
+
+
+def test_small_gradients_beside_large_ones():
+    """Elements 2^-30 below their block's largest: the second moment stays above
+    zero, so no update explodes."""
+    host, dev = make([64], 8, zero_state=True)
+    import torch
+    g = np.full(64, 1.0, np.float32)
+    g[1:] = np.float32(2.0) ** -np.arange(1, 64)
+    host[0]["g"] = g
+    dev[0]["grad"].copy_(torch.from_numpy(g))
+    for t in range(1, 4):
+        run(dev, 8, step=t)
+        assert (values(dev[0]["v"]) > 0).all()
+        check(host, dev, 8, t)
+        host[0]["p"] = dev[0]["param"].cpu().numpy()
+        for key in ("m", "v"):
+            host[0][key] = o.decode(values(dev[0][key]), dev[0][key + "_exp"].cpu().numpy(), 64).astype(np.float32)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_infinities_and_nan_stay_where_they_are(bits):
+    import torch
+    host, dev = make([200], bits)
+    for i, v in ((5, np.nan), (70, np.inf), (130, -np.inf)):
+        dev[0]["grad"][i] = float(v)
+    clean = np.ones(200, bool)
+    clean[[5, 70, 130]] = False
+    run(dev, bits)
+    m, v = o.moments32(host[0]["m"], host[0]["v"], host[0]["g"], CFG["grad_scale"], CFG["beta1"], CFG["beta2"])
+    want = o.step(host[0]["p"], m, v, CFG["lr"], 0.0, CFG["beta1"], CFG["beta2"], CFG["eps"], 3)
+    got = values(dev[0]["param"])
+    assert np.abs(got - want)[clean].max() <= 1e-6
+    assert np.isfinite(values(dev[0]["m"]))[clean].all()
+    assert not np.isfinite(values(dev[0]["m"]))[~clean].any()
+    assert not np.isfinite(values(dev[0]["v"]))[~clean].any()
+    assert torch.isfinite(dev[0]["param"].cpu()[torch.from_numpy(clean)]).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_counted_on_the_device_and_captured(bits):
+    """step_dev: a captured call counts its replays; eager calls go on from there."""
+    import torch
+    host, dev = make([500, 77], bits, zero_state=True)
+    count = torch.zeros(1, dtype=torch.int32, device="cuda")
+    cfg = abi.adamw_config(state_bits=bits, step=0, step_dev=count, **CFG)
+    arr = abi.adamw_tensors(dev)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        abi.ks_adamw(cfg, arr, abi.current_stream())
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+
+    def follow(t):
+        check(host, dev, bits, t, counted=True)
+        assert int(count) == t
+        for h, d in zip(host, dev):
+            h["p"] = d["param"].cpu().numpy()
+            for key in ("m", "v"):
+                h[key] = (values(d[key]).astype(np.float32) if bits == 32 else
+                          o.decode(values(d[key]), d[key + "_exp"].cpu().numpy(), h["n"]).astype(np.float32))
+
+    follow(1)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        abi.ks_adamw(cfg, arr, abi.current_stream())
+    torch.cuda.synchronize()
+    for t in range(2, 6):
+        if t == 4:
+            abi.ks_adamw(cfg, arr, abi.current_stream())   # eager, between the replays
+        else:
+            g.replay()
+        torch.cuda.synchronize()
+        follow(t)
+
+
+def test_no_tensors():
+    import torch
+    count = torch.zeros(1, dtype=torch.int32, device="cuda")
+    abi.ks_adamw(abi.adamw_config(1e-3, step_dev=count), (abi.ks_tensor * 0)(), abi.current_stream())
+    torch.cuda.synchronize()
+    assert int(count) == 1

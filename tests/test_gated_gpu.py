@@ -1,0 +1,426 @@
+"""Gated heads over feature rows (ks_gated_forward, ks_gated_backward,
+ks_gated_loss) against the fp64 oracle: types, widths, lengths, empty families,
+strides and alignments, rows that do not count, streams and captured graphs.
+
+Tolerances are the oracle's bounds on fp32 arithmetic, times 1 (they bound any
+order of the sums); a bf16 result adds half a step, 2^-8."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+from oracle import ks_fit as o
+from paper_2606_28565_amd import abi
+
+pytestmark = pytest.mark.gpu
+NFAM = abi.NFAM
+
+
+def offsets(n, kind="mixed"):
+    """Family offsets: "mixed" leaves families 1 and 7 empty, "one" puts every row
+    into family 4, "last" into the last."""
+    if kind == "one":
+        return [0] * 5 + [n] * 6
+    if kind == "last":
+        return [0] * 10 + [n]
+    share = np.array([5, 0, 1, 2, 2, 4, 1, 0, 1, 1], np.float64)
+    cut = np.floor(np.cumsum(share) / share.sum() * n).astype(int)
+    cut[-1] = n
+    return [0] + [int(v) for v in cut]
+
+
+def make(n, prec, inp, hid, kind="mixed", seed=1, scale=0.3, ldx=None, shift=0):
+    """Inputs on the device: x may have row stride ldx and start ``shift``
+    elements into an allocation."""
+    import torch
+    dt = torch.bfloat16 if prec == "bf16" else torch.float32
+    g = torch.Generator().manual_seed(seed)
+    ldx = ldx or inp
+    buf = torch.full((n * ldx + shift + 16,), float("nan"), dtype=dt)
+    x = buf[shift:shift + n * ldx].view(n, ldx)[:, :inp]
+    x.copy_(torch.rand(n, inp, generator=g))
+    if n:
+        x[:, 15] = 1.0
+    w = {"w1": torch.randn(NFAM, hid, inp, generator=g), "w2": torch.randn(NFAM, hid, inp, generator=g),
+         "w3": torch.randn(NFAM, hid, generator=g), "b3": torch.randn(NFAM, generator=g)}
+    w = {k: (v * scale).to(dt) for k, v in w.items()}
+    dbuf = buf.cuda()
+    d = {"x": dbuf[shift:shift + n * ldx].view(n, ldx)[:, :inp], "buf": dbuf, **{k: v.cuda() for k, v in w.items()}}
+    h = {"x": x.double().numpy(), **{k: v.double().numpy() for k, v in w.items()}}
+    return d, h, offsets(n, kind)
+
+
+def heads_of(d):
+    return abi.gated_heads(d["w1"], d["w2"], d["w3"], d["b3"])
+
+
+def forward(d, off, stream=None):
+    import torch
+    n = d["x"].shape[0]
+    z = torch.full((n + 7,), -77.0, device="cuda")
+    abi.ks_gated_forward(heads_of(d), abi.feature_rows(d["x"], off), z.data_ptr(), stream or abi.current_stream())
+    torch.cuda.synchronize()
+    assert (z[n:] == -77.0).all()      # rows behind the last stay as they were
+    return z[:n].double().cpu().numpy()
+
+
+def families(h, off):
+    for f in range(NFAM):
+        r = slice(off[f], off[f + 1])
+        if r.stop > r.start:
+            z, k = o.block(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], h["b3"][f])
+            yield f, r, z, k
+
+
+def check_forward(d, h, off, z):
+    for _, r, want, k in families(h, off):
+        assert (np.abs(z[r] - want) <= k["err"]["z"]).all(), np.max(np.abs(z[r] - want) / k["err"]["z"])
+
+
+@pytest.mark.parametrize("prec", ["f32", "bf16"])
+@pytest.mark.parametrize("inp", [16, 32])
+@pytest.mark.parametrize("hid", [1, 31, 64, 65, 200, 256])
+def test_forward_widths(prec, inp, hid):
+    d, h, off = make(301, prec, inp, hid)
+    check_forward(d, h, off, forward(d, off))
+
+
+@pytest.mark.parametrize("prec", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [0, 1, 2, 31, 33, 63, 64, 65, 255, 257, 5003])
+@pytest.mark.parametrize("kind", ["mixed", "one", "last"])
+def test_forward_lengths(prec, n, kind):
+    d, h, off = make(n, prec, 16, 64, kind)
+    check_forward(d, h, off, forward(d, off))
+
+
+@pytest.mark.parametrize("prec", ["f32", "bf16"])
+@pytest.mark.parametrize("inp,ldx,shift", [(16, 17, 0), (16, 16, 1), (32, 40, 0), (32, 48, 3), (32, 33, 5), (16, 64, 8)])
+def test_forward_strides(prec, inp, ldx, shift):
+    """Row strides and bases that leave no, some or every row 16-byte aligned."""
+    d, h, off = make(130, prec, inp, 96, ldx=ldx, shift=shift)
+    check_forward(d, h, off, forward(d, off))
+
+
+def test_forward_many_rows_per_workgroup():
+    """More rows than one pass of the workgroups takes."""
+    d, h, off = make(300_011, "bf16", 16, 32)
+    check_forward(d, h, off, forward(d, off))
+
+
+def test_forward_large_gates():
+    """Gates of hundreds both ways: silu(g) is g or 0 there, never NaN."""
+    d, h, off = make(200, "f32", 16, 64, scale=60.0)
+    z = forward(d, off)
+    assert np.isfinite(z).all()
+    check_forward(d, h, off, z)
+
+
+def test_weights_off_the_16_byte_grid():
+    import torch
+    for prec in ("f32", "bf16"):
+        d, h, off = make(100, prec, 16, 40)
+        for k in ("w1", "w2", "w3", "b3"):
+            t = torch.zeros(d[k].numel() + 1, dtype=d[k].dtype, device="cuda")
+            t[1:] = d[k].reshape(-1)
+            d[k] = t[1:].view(d[k].shape)
+        check_forward(d, h, off, forward(d, off))
+        dz = torch.randn(100, generator=torch.Generator().manual_seed(3))
+        check_grads(h, off, dz.numpy(), backward(d, off, dz.cuda()), prec)
+
+
+# ------------------------------------------------------------------ backward
+def backward(d, off, dz, dx=True, ldg=None, repeat=1):
+    import torch
+    n, inp = d["x"].shape
+    ldg = ldg or inp
+    hd, rows = heads_of(d), abi.feature_rows(d["x"], off)
+    out = {k: torch.full(d[k].shape, float("nan"), device="cuda") for k in ("w1", "w2", "w3", "b3")}
+    gx = torch.full((n, ldg), -77.0, dtype=d["x"].dtype, device="cuda")
+    g = abi.gated_grad(**out, x=gx[:, :inp] if dx and n else None)
+    wsb = abi.ks_gated_workspace_bytes(hd, rows)
+    ws = torch.full((wsb,), 255, dtype=torch.uint8, device="cuda")
+    for _ in range(repeat):
+        abi.ks_gated_backward(hd, rows, dz.data_ptr() if n else None, g, ws.data_ptr(), wsb, abi.current_stream())
+    torch.cuda.synchronize()
+    if n:
+        assert (gx[:, inp:].float() == -77.0).all()
+    r = {k: v.double().cpu().numpy() for k, v in out.items()}
+    if dx:
+        r["x"] = gx[:, :inp].double().cpu().numpy()
+    return r
+
+
+def check_grads(h, off, dz, got, prec, dx=True):
+    with np.errstate(invalid="ignore"):
+        for f in range(NFAM):
+            r = slice(off[f], off[f + 1])
+            if r.start == r.stop:
+                for k in ("w1", "w2", "w3", "b3"):
+                    assert (got[k][f] == 0).all(), (k, f)
+                continue
+            _, k = o.block(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], h["b3"][f])
+            want, err = o.gradients(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], dz[r], k, 16 + len(dz) // 128)
+            for key in ("w1", "w2", "w3", "b3"):
+                off_by = np.abs(got[key][f] - want[key])
+                assert (off_by <= err[key]).all(), (key, f, np.max(off_by / np.maximum(err[key], 1e-300)))
+            if dx:
+                half = 2.0 ** -8 if prec == "bf16" else 0.0
+                bound = err["x"] + half * (np.abs(want["x"]) + err["x"])
+                assert (np.abs(got["x"][r] - want["x"]) <= bound).all(), f
+
+
+@pytest.mark.parametrize("prec", ["f32", "bf16"])
+@pytest.mark.parametrize("inp", [16, 32])
+@pytest.mark.parametrize("hid", [1, 63, 64, 65, 128, 150, 256])
+def test_backward_widths(prec, inp, hid):
+    """One to four groups of 64 units, whole and not."""
+    import torch
+    d, h, off = make(403, prec, inp, hid)
+    dz = torch.randn(403, generator=torch.Generator().manual_seed(5))
+    check_grads(h, off, dz.numpy(), backward(d, off, dz.cuda()), prec)
+
+
+@pytest.mark.parametrize("prec", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [0, 1, 15, 16, 17, 33, 65, 1000])
+@pytest.mark.parametrize("kind", ["mixed", "one"])
+def test_backward_lengths(prec, n, kind):
+    import torch
+    d, h, off = make(n, prec, 32, 64, kind)
+    dz = torch.randn(n, generator=torch.Generator().manual_seed(5))
+    check_grads(h, off, dz.numpy(), backward(d, off, dz.cuda()), prec)
+
+
+@pytest.mark.parametrize("prec", ["f32", "bf16"])
+@pytest.mark.parametrize("ldx,shift,ldg", [(17, 0, 16), (16, 1, 19), (24, 0, 24), (40, 3, 18)])
+def test_backward_strides(prec, ldx, shift, ldg):
+    import torch
+    d, h, off = make(150, prec, 16, 70, ldx=ldx, shift=shift)
+    dz = torch.randn(150, generator=torch.Generator().manual_seed(5))
+    check_grads(h, off, dz.numpy(), backward(d, off, dz.cuda(), ldg=ldg), prec)
+
+
+@pytest.mark.parametrize("prec", ["f32", "bf16"])
+def test_backward_long_sums(prec):
+    """Several tiles per wave, and many workgroups per family."""
+    import torch
+    d, h, off = make(150_007, prec, 16, 20)
+    dz = torch.randn(150_007, generator=torch.Generator().manual_seed(5))
+    check_grads(h, off, dz.numpy(), backward(d, off, dz.cuda(), dx=False), prec, dx=False)
+
+
+@pytest.mark.parametrize("prec", ["f32", "bf16"])
+def test_rows_with_dz_zero_add_nothing(prec):
+    """dz = 0 rows may hold anything: NaN and infinities in them reach no output."""
+    import torch
+    d, h, off = make(260, prec, 16, 64)
+    dz = torch.randn(260, generator=torch.Generator().manual_seed(5))
+    dz[::3] = 0.0
+    dz[100:140] = 0.0
+    d["x"][::3] = float("nan")
+    d["x"][100:140] = float("inf")
+    got = backward(d, off, dz.cuda())
+    assert all(np.isfinite(v).all() for v in got.values())
+    assert (got["x"][::3] == 0).all() and (got["x"][100:140] == 0).all()
+    check_grads(h, off, dz.numpy(), got, prec)
+    none = backward(d, off, torch.zeros(260, device="cuda"))
+    assert all((v == 0).all() for v in none.values())
+
+
+def test_backward_gives_the_same_bits_again():
+    import torch
+    d, _, off = make(20_000, "f32", 32, 128)
+    dz = torch.randn(20_000, generator=torch.Generator().manual_seed(5)).cuda()
+    a = backward(d, off, dz)
+    b = backward(d, off, dz, repeat=3)
+    for k in a:
+        assert (a[k] == b[k]).all(), k
+
+
+def test_only_the_rows_gradient():
+    """grad.x alone: no weight gradient is formed or written."""
+    import torch
+    d, h, off = make(90, "f32", 16, 64)
+    dz = torch.randn(90, generator=torch.Generator().manual_seed(5)).cuda()
+    want = backward(d, off, dz)["x"]
+    hd, rows = heads_of(d), abi.feature_rows(d["x"], off)
+    gx = torch.empty(90, 16, device="cuda")
+    ws = torch.empty(abi.ks_gated_workspace_bytes(hd, rows), dtype=torch.uint8, device="cuda")
+    abi.ks_gated_backward(hd, rows, dz.data_ptr(), abi.gated_grad(x=gx), ws.data_ptr(), ws.numel(), abi.current_stream())
+    torch.cuda.synchronize()
+    assert (gx.double().cpu().numpy() == want).all()
+
+
+# ------------------------------------------------------------------ loss
+def run_loss(d, off, eta, weight, huber, grad=True, with_z=True):
+    import torch
+    n = d["x"].shape[0]
+    hd, rows = heads_of(d), abi.feature_rows(d["x"], off)
+    out = {k: torch.full(d[k].shape, float("nan"), device="cuda") for k in ("w1", "w2", "w3", "b3")}
+    loss = torch.full((NFAM,), float("nan"), device="cuda")
+    z = torch.empty(n, device="cuda")
+    wsb = abi.ks_gated_workspace_bytes(hd, rows)
+    ws = torch.full((wsb,), 255, dtype=torch.uint8, device="cuda")
+    abi.ks_gated_loss(hd, rows, abi.eta_target(eta, weight, huber), loss.data_ptr(), z.data_ptr() if with_z else None,
+                      abi.gated_grad(**out) if grad else None, ws.data_ptr(), wsb, abi.current_stream())
+    torch.cuda.synchronize()
+    return loss.double().cpu().numpy(), z.double().cpu().numpy(), {k: v.double().cpu().numpy() for k, v in out.items()}
+
+
+def check_loss(h, off, eta, weight, huber, got, grad=True):
+    """dz's own error: log(1 + e^-z) and log eta are within 4 steps of their sizes
+    and carry z's error (slope <= 1), sigma(-z) likewise (slope <= 1/4)."""
+    loss, z, grads = got
+    eta = eta.double().numpy()
+    weight = None if weight is None else weight.double().numpy()
+    for f in range(NFAM):
+        r = slice(off[f], off[f + 1])
+        if r.start == r.stop:
+            assert loss[f] == 0 and all((grads[k][f] == 0).all() for k in grads) if grad else loss[f] == 0
+            continue
+        zf, k = o.block(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], h["b3"][f])
+        w = o.counted(eta[r], None if weight is None else weight[r])
+        on = w > 0
+        assert (np.abs(z[r] - zf)[on] <= k["err"]["z"][on]).all()
+        want, dz = o.eta_loss(zf, eta[r], None if weight is None else weight[r], huber)
+        if not on.any():
+            assert loss[f] == 0
+            if grad:
+                assert all((grads[key][f] == 0).all() for key in grads)
+            continue
+        zo = np.where(on, zf, 0.0)
+        ez = np.where(on, k["err"]["z"], 0.0)
+        size = np.logaddexp(0, -zo) + np.abs(np.log(np.where(on, eta[r], 1.0)))
+        er = ez + 8 * o.EPS * (size + np.minimum(1, np.exp(-np.abs(zo))))
+        res = np.abs(np.logaddexp(0, -zo) - np.log(np.where(on, eta[r], 1.0)))
+        share = w / w.sum()
+        slope = np.minimum(res + er, huber)
+        assert abs(loss[f] - want) <= (share * (slope * er + 8 * o.EPS * slope * (res + er))).sum() + 4 * o.EPS * want
+        if not grad:
+            continue
+        sg = o.sigmoid(-zo)
+        edz = share * (er * (sg + ez / 4) + slope * (ez / 4 + 8 * o.EPS * sg)) + 8 * o.EPS * np.abs(dz)
+        val, err = o.gradients(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], dz, k, 16 + len(eta) // 128)
+        # what an error of dz makes of the sums: their derivative by dz
+        x = np.where(on[:, None], h["x"][r], 0.0)
+        t = np.abs(k["s"] + k["a"] * (1 - k["s"])) * np.abs(k["u"]) * np.abs(h["w3"][f])
+        more = {"w1": (edz[:, None] * np.where(on[:, None], t, 0)).T @ np.abs(x),
+                "w2": (edz[:, None] * np.where(on[:, None], np.abs(k["a"] * h["w3"][f]), 0)).T @ np.abs(x),
+                "w3": (edz[:, None] * np.where(on[:, None], np.abs(k["y"]), 0)).sum(0), "b3": edz.sum()}
+        for key in ("w1", "w2", "w3", "b3"):
+            off_by = np.abs(grads[key][f] - val[key])
+            bound = (err[key] + more[key]) * 1.01 + 2 * o.EPS * np.abs(val[key])
+            assert (off_by <= bound).all(), (key, f, np.max(off_by / np.maximum(bound, 1e-300)))
+
+
+def targets(n, seed=9):
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    eta = 1 + torch.exp(0.7 * torch.randn(n, generator=g) - 1)
+    weight = 0.5 + torch.rand(n, generator=g)
+    return eta, weight
+
+
+@pytest.mark.parametrize("prec", ["f32", "bf16"])
+@pytest.mark.parametrize("inp,hid", [(16, 64), (32, 128), (16, 33), (32, 256), (16, 180)])
+@pytest.mark.parametrize("huber", [float("inf"), 0.2])
+def test_loss_widths(prec, inp, hid, huber):
+    d, h, off = make(700, prec, inp, hid)
+    eta, weight = targets(700)
+    check_loss(h, off, eta, weight, huber, run_loss(d, off, eta.cuda(), weight.cuda(), huber))
+
+
+@pytest.mark.parametrize("n", [0, 1, 16, 65, 3000])
+def test_loss_lengths_without_weights(n):
+    d, h, off = make(n, "f32", 16, 64, "mixed")
+    eta, _ = targets(n)
+    check_loss(h, off, eta, None, float("inf"), run_loss(d, off, eta.cuda(), None, float("inf")))
+
+
+@pytest.mark.parametrize("prec,hid", [("f32", 64), ("bf16", 128), ("f32", 192)])
+def test_rows_that_do_not_count(prec, hid):
+    """NaN, infinite, zero and negative eta, zero, negative, NaN and infinite
+    weights, and whatever features such rows have; a family with none that counts."""
+    d, h, off = make(800, prec, 16, hid)
+    eta, weight = targets(800)
+    inf, nan = float("inf"), float("nan")
+    for i, v in enumerate([nan, inf, -inf, 0.0, -1.0]):
+        eta[i::17] = v
+    for i, v in enumerate([0.0, -0.0, -2.0, nan, inf]):
+        weight[7 + i::19] = v
+    eta[off[3]:off[4]] = nan
+    out = o.counted(eta.numpy(), weight.numpy()) == 0
+    assert out.sum() > 300
+    import torch
+    d["x"][torch.from_numpy(np.nonzero(out)[0]).cuda()] = nan
+    got = run_loss(d, off, eta.cuda(), weight.cuda(), 0.5)
+    assert np.isfinite(got[0]).all() and all(np.isfinite(v).all() for v in got[2].values())
+    assert got[0][3] == 0 and (got[2]["w1"][3] == 0).all()
+    check_loss(h, off, eta, weight, 0.5, got)
+
+
+def test_loss_alone_is_the_same_loss():
+    d, h, off = make(1000, "f32", 32, 64)
+    eta, weight = targets(1000)
+    a = run_loss(d, off, eta.cuda(), weight.cuda(), 0.3)
+    b = run_loss(d, off, eta.cuda(), weight.cuda(), 0.3, grad=False, with_z=False)
+    assert (a[0] == b[0]).all()
+    check_loss(h, off, eta, weight, 0.3, b[:1] + a[1:], grad=True)
+
+
+def test_far_targets_do_not_overflow():
+    """eta up to 1e30 against z of either sign: the loss and its gradient stay
+    finite."""
+    import torch
+    d, h, off = make(300, "f32", 16, 64, scale=3.0)
+    eta = torch.logspace(-30, 30, 300)
+    got = run_loss(d, off, eta.cuda(), None, 1.0)
+    assert np.isfinite(got[0]).all() and all(np.isfinite(v).all() for v in got[2].values())
+    check_loss(h, off, eta, None, 1.0, got)
+
+
+# ------------------------------------------------------------------ streams, graphs
+def test_other_stream():
+    import torch
+    d, h, off = make(500, "bf16", 32, 96)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        z = forward(d, off, s.cuda_stream)
+    check_forward(d, h, off, z)
+
+
+def test_captured_loss_replays():
+    """A captured pass replayed with other weights in place between the replays."""
+    import torch
+    n = 3000
+    d, h, off = make(n, "f32", 16, 128)
+    eta, weight = targets(n)
+    eta_d, weight_d = eta.cuda(), weight.cuda()
+    hd, rows, tgt = heads_of(d), abi.feature_rows(d["x"], off), abi.eta_target(eta_d, weight_d, 0.5)
+    out = {k: torch.zeros(d[k].shape, device="cuda") for k in ("w1", "w2", "w3", "b3")}
+    grad = abi.gated_grad(**out)
+    loss, z = torch.zeros(NFAM, device="cuda"), torch.zeros(n, device="cuda")
+    ws = torch.empty(abi.ks_gated_workspace_bytes(hd, rows), dtype=torch.uint8, device="cuda")
+
+    def call():
+        abi.ks_gated_loss(hd, rows, tgt, loss.data_ptr(), z.data_ptr(), grad, ws.data_ptr(), ws.numel(), abi.current_stream())
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call()
+    torch.cuda.current_stream().wait_stream(s)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for i in range(4):
+        d["w1"].mul_(0.9)
+        g.replay()
+        torch.cuda.synchronize()
+        seen = loss.clone(), {k: v.clone() for k, v in out.items()}
+        call()   # eager, between the replays
+        torch.cuda.synchronize()
+        assert (seen[0] == loss).all() and all((seen[1][k] == out[k]).all() for k in out), i
+    h["w1"] = d["w1"].double().cpu().numpy()
+    check_loss(h, off, eta, weight, 0.5, (loss.double().cpu().numpy(), z.double().cpu().numpy(),
+                                          {k: v.double().cpu().numpy() for k, v in out.items()}))
