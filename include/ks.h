@@ -456,7 +456,7 @@ ks_status ks_eval_steps_static(const ks_desc* desc, const ks_steps* steps,
  * go through its weights.  x: device [n_rows][ldx], of heads.precision's type,
  * the first in_dim elements of each row are read; ldx >= in_dim.  Any base of its
  * type's alignment and any stride is taken; 16-byte aligned rows are read
- * fastest.  n_rows < 2^31. */
+ * fastest.  n_rows < 2^31, ldx <= 2^20. */
 typedef struct ks_rows {
   int64_t n_rows;
   int64_t fam_off[KS_NFAM + 1];          /* host array, fam_off[0] = 0       */

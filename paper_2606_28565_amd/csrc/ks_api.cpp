@@ -309,7 +309,9 @@ ks_status head_kind(const ks_heads *h, int *kind) {
   if (h->mode == KS_ETA_GATED) {
     const ks_status st = ks::check_gated(h);
     if (st != KS_OK) return st;
-    if (h->precision == KS_F32) *kind = h->in_dim == 16 ? ks::kGatedF32_16 : ks::kGatedF32_32;
+    // (up to 128 units of 32 features leave room in LDS for two workgroups per CU)
+    if (h->precision == KS_F32)
+      *kind = h->in_dim == 16 ? ks::kGatedF32_16 : h->hidden <= 128 ? ks::kGatedF32_32 : ks::kGatedF32_32_256;
     else *kind = h->in_dim == 16 ? ks::kGatedBF16_16 : ks::kGatedBF16_32;
     return KS_OK;
   }

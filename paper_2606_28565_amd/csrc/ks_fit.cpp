@@ -34,8 +34,8 @@ ks_status check_rows(const ks_heads *h, const ks_rows *r) {
   if (r->fam_off[KS_NFAM] != r->n_rows)
     return set_error(KS_EINVAL, "rows.fam_off[KS_NFAM] = %lld != n_rows = %lld", (long long)r->fam_off[KS_NFAM],
                      (long long)r->n_rows);
-  if (r->ldx < h->in_dim || r->ldx > (int64_t(1) << 31))
-    return set_error(KS_EINVAL, "rows.ldx %lld outside in_dim %d .. 2^31", (long long)r->ldx, h->in_dim);
+  if (r->ldx < h->in_dim || r->ldx > (int64_t(1) << 20))
+    return set_error(KS_EINVAL, "rows.ldx %lld outside in_dim %d .. 2^20", (long long)r->ldx, h->in_dim);
   return KS_OK;
 }
 
@@ -43,14 +43,14 @@ ks_status check_rows(const ks_heads *h, const ks_rows *r) {
 // workgroups (two per CU and one to follow each), so that the weights' way into
 // LDS is paid for by several tiles where there are many, and one pass of the four
 // waves each where there are few.  Backward: about 512 workgroups (two per CU are
-// resident), each at least one 16-row tile per row group.  The split depends on
+// resident), each at least the rows it takes at a time.  The split depends on
 // sizes alone, so results do not depend on the device.
 constexpr int64_t kFwdWgs = 1024, kBwdWgs = 512;
 
 void plan(ks::GatedParams &p, const ks_heads *h, const ks_rows *r) {
   const int64_t tiles = (r->n_rows + 63) / 64;
   p.fwd_tiles = (int32_t)(4 * std::max<int64_t>(1, (tiles + 4 * kFwdWgs - 1) / (4 * kFwdWgs)));
-  const int64_t unit = 16 * (4 / ks::gated_groups(h->hidden));
+  const int64_t unit = ks::gated_rows(h->precision == KS_BF16, h->in_dim, h->hidden);
   p.bwd_rows = (int32_t)(unit * std::max<int64_t>(1, (r->n_rows + unit * kBwdWgs - 1) / (unit * kBwdWgs)));
   p.fwd_wg[0] = p.bwd_wg[0] = 0;
   for (int f = 0; f < KS_NFAM; ++f) {
@@ -60,16 +60,15 @@ void plan(ks::GatedParams &p, const ks_heads *h, const ks_rows *r) {
   }
 }
 
-// Workspace: the backward workgroups' sums, then (the loss) the forward
-// workgroups' sums and each row's dz.
+// Workspace: the backward workgroups' gradient sums, then either kernel's
+// workgroups' loss sums.
 struct Room {
-  size_t loss, dz, total;
+  size_t loss, total;
 };
-Room room_of(const ks::GatedParams &p, int64_t n_rows) {
+Room room_of(const ks::GatedParams &p) {
   Room o;
   o.loss = align256((size_t)p.bwd_wg[KS_NFAM] * ks::gated_part_size(p.hidden, p.in_dim) * sizeof(float));
-  o.dz = o.loss + align256((size_t)p.fwd_wg[KS_NFAM] * 2 * sizeof(double));
-  o.total = o.dz + align256((size_t)n_rows * sizeof(float));
+  o.total = o.loss + align256((size_t)std::max(p.fwd_wg[KS_NFAM], p.bwd_wg[KS_NFAM]) * 2 * sizeof(double));
   return o;
 }
 
@@ -100,8 +99,8 @@ ks_status check_all(const ks_heads *h, const ks_rows *r) {
   return KS_OK;
 }
 
-ks_status check_room(const ks::GatedParams &p, int64_t n_rows, void *ws, size_t ws_bytes, Room *room) {
-  *room = room_of(p, n_rows);
+ks_status check_room(const ks::GatedParams &p, void *ws, size_t ws_bytes, Room *room) {
+  *room = room_of(p);
   if (!ws) return set_error(KS_EWORKSPACE, "workspace is NULL");
   if (ws_bytes < room->total)
     return set_error(KS_EWORKSPACE, "workspace %zu bytes < %zu required", ws_bytes, room->total);
@@ -150,7 +149,7 @@ size_t ks_gated_workspace_bytes(const ks_heads *heads, const ks_rows *rows) {
   if (check_rows(heads, rows) != KS_OK) return 0;
   ks::GatedParams p;
   fill(p, heads, rows);
-  const size_t n = room_of(p, rows->n_rows).total;
+  const size_t n = room_of(p).total;
   return n ? n : 256;
 }
 
@@ -165,7 +164,7 @@ ks_status ks_gated_backward(const ks_heads *heads, const ks_rows *rows, const fl
   st = take_grad(p, grad);
   if (st != KS_OK) return st;
   Room room;
-  st = check_room(p, rows->n_rows, ws, ws_bytes, &room);
+  st = check_room(p, ws, ws_bytes, &room);
   if (st != KS_OK) return st;
   if (grad->x) {
     const int64_t e = p.bf16 ? 2 : 4;
@@ -182,7 +181,7 @@ ks_status ks_gated_backward(const ks_heads *heads, const ks_rows *rows, const fl
   p.dz = dz;
   p.part = static_cast<float *>(ws);
   if (p.g_w1) {
-    hipError_t e = ks::launch_gated_backward(p, stream);
+    hipError_t e = ks::launch_gated_fit(p, stream);
     if (e == hipSuccess) e = ks::launch_gated_reduce(p, stream);
     if (e != hipSuccess) return hip_error(e, "gated backward launch");
   }
@@ -208,7 +207,7 @@ ks_status ks_gated_loss(const ks_heads *heads, const ks_rows *rows, const ks_eta
     if (st != KS_OK) return st;
   }
   Room room;
-  st = check_room(p, rows->n_rows, ws, ws_bytes, &room);
+  st = check_room(p, ws, ws_bytes, &room);
   if (st != KS_OK) return st;
   char *w = static_cast<char *>(ws);
   p.z = z;
@@ -220,10 +219,7 @@ ks_status ks_gated_loss(const ks_heads *heads, const ks_rows *rows, const ks_eta
   p.loss = loss;
   p.loss_part = reinterpret_cast<double *>(w + room.loss);
   p.part = reinterpret_cast<float *>(w);
-  if (p.g_w1) p.dz_out = reinterpret_cast<float *>(w + room.dz);
-  p.dz = p.dz_out;
-  hipError_t e = ks::launch_gated_forward(p, stream);
-  if (e == hipSuccess && p.g_w1) e = ks::launch_gated_backward(p, stream);
+  hipError_t e = p.g_w1 ? ks::launch_gated_fit(p, stream) : ks::launch_gated_forward(p, stream);
   if (e == hipSuccess) e = ks::launch_gated_reduce(p, stream);
   return hip_error(e, "gated loss launch");
 }

@@ -3,11 +3,20 @@
 //
 //   z = w3 . (silu(W1 x) * (W2 x)) + b3,   silu(g) = g / (1 + exp(-g))
 //
-// A wave takes 64 rows: two column blocks of 32 on the 32x32 matrix
+// A wave takes 64 rows: two column blocks of 32 on the 32x32x16 matrix
 // instruction, the weights its row operand from LDS.  One lane then holds 16
 // of a 32-unit block's gates and ups of one row, so the activation, the product
 // and the dot product with w3 stay in the lane's registers; one exchange of the
 // wave's halves at the end completes the sums over the units.
+//
+// fp32 operands are split into three bf16 pieces that sum to them exactly (from
+// 2^-102 up; below, what is lost is under 2^-126) and the six products of the
+// largest pieces are taken: the three left out are below 2^-25 of the product.
+// The bf16 instruction runs beside other waves' vector work; the fp32 one does not
+// (measured on pairs of waves: bf16 32x32x16 with FMAs takes the longer of the two,
+// fp32 32x32x2 the sum of both), and the vector work is what bounds this block: an
+// exponential and a reciprocal per gate.  (1M rows of 32-256: 305 us on the fp32
+// instruction.)
 #pragma once
 
 #include <stdint.h>
@@ -27,16 +36,49 @@ __device__ __forceinline__ float sigmoid(float g) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504088896340736f));
 }
 
-template <bool BF16, int IN>
+// two floats -> packed bfloat16 pair, round to nearest even
+typedef __bf16 gbf16x2 __attribute__((ext_vector_type(2)));
+typedef float gf32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((gf32x2{lo, hi}), gbf16x2));
+}
+// a pair of values as three packed pairs of pieces
+__device__ __forceinline__ void split2(float a, float b, uint32_t &p0, uint32_t &p1, uint32_t &p2) {
+  p0 = pack2(a, b);
+  a -= __builtin_bit_cast(float, p0 << 16);
+  b -= __builtin_bit_cast(float, p0 & 0xFFFF0000u);
+  p1 = pack2(a, b);
+  a -= __builtin_bit_cast(float, p1 << 16);
+  b -= __builtin_bit_cast(float, p1 & 0xFFFF0000u);
+  p2 = pack2(a, b);
+}
+
+// HID: the widest block that fits the LDS room (any narrower one too)
+template <bool BF16, int IN, int HID>
 struct Block {
   static constexpr int KC = IN / 16;                  // 16-feature chunks
-  static constexpr int kFrag = BF16 ? 256 : 512;      // dwords of 32 units x 16 features
+  static constexpr int NP = BF16 ? 1 : 3;             // pieces of an operand
+  static constexpr int kFrag = NP * 256;              // dwords of 32 units x 16 features
   static constexpr int kBlk = 2 * KC * kFrag + 32;    // of 32 units: gates, ups, w3 by register and half
-  static constexpr int kLds = kMaxHidden / 32 * kBlk + 4;
+  static constexpr int kLds = HID / 32 * kBlk + 4;
   static constexpr int OFF_B3 = kLds - 4, OFF_NB = kLds - 3;
 
   // unit of register r in lane half h of a block's products
   __device__ static __forceinline__ int unit_of(int h, int r) { return 8 * (r >> 2) + 4 * h + (r & 3); }
+
+  // eight values as packed pieces
+  __device__ static __forceinline__ void split8(const gf32x4 &a, const gf32x4 &b, gu32x4 (&p)[NP]) {
+    if constexpr (!BF16) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t p0, p1, p2;
+        split2(j < 2 ? a[2 * j] : b[2 * j - 4], j < 2 ? a[2 * j + 1] : b[2 * j - 3], p0, p1, p2);
+        p[0][j] = p0;
+        p[1][j] = p1;
+        p[2][j] = p2;
+      }
+    }
+  }
 
   // a family's weights into LDS; units past hidden are zero (and add nothing)
   __device__ static void stage(uint32_t *lds, const void *w1, const void *w2, const void *w3, const void *b3, int hidden,
@@ -66,8 +108,14 @@ struct Block {
           for (int j = 0; j < 4; ++j) v0[j] = f[j], v1[j] = f[4 + j];
         }
       }
-      *(gu32x4 *)dst = v0;
-      if constexpr (!BF16) *(gu32x4 *)(dst + 256) = v1;
+      if constexpr (BF16) {
+        *(gu32x4 *)dst = v0;
+      } else {
+        gu32x4 p[NP];
+        split8(__builtin_bit_cast(gf32x4, v0), __builtin_bit_cast(gf32x4, v1), p);
+#pragma unroll
+        for (int j = 0; j < NP; ++j) *(gu32x4 *)(dst + 256 * j) = p[j];
+      }
     }
     for (int i = tid; i < nb * 32; i += n_threads) {
       const int mb = i >> 5, unit = mb * 32 + unit_of((i >> 4) & 1, i & 15);
@@ -85,28 +133,27 @@ struct Block {
   // the column operand of 64 rows: a lane holds, of row (lane mod 32) of each
   // column block, the eight features of its half
   struct Rows {
-    gu32x4 v[2][KC][BF16 ? 1 : 2];
+    gu32x4 v[2][KC][NP];
   };
 
+  // c += W x for the two column blocks in turn (neither instruction waits for the
+  // one before it), small pieces first
   __device__ static __forceinline__ void products(const uint32_t *frag, int lane, const Rows &x, int kc, gf32x16 (&c)[2]) {
-    if constexpr (BF16) {
-      const gbf16x8 a = __builtin_bit_cast(gbf16x8, *(const gu32x4 *)(frag + lane * 4));
+    gbf16x8 a[NP];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        c[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(gbf16x8, x.v[i][kc][0]), c[i], 0, 0, 0);
-    } else {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        // (whole vectors cast: a cast of one element of a vector in memory reads its first)
-        const gf32x4 a = __builtin_bit_cast(gf32x4, *(const gu32x4 *)(frag + h * 256 + lane * 4));
-        const gf32x4 b0 = __builtin_bit_cast(gf32x4, x.v[0][kc][h]), b1 = __builtin_bit_cast(gf32x4, x.v[1][kc][h]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          c[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b0[j], c[0], 0, 0, 0);
-          c[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b1[j], c[1], 0, 0, 0);
-        }
-      }
+    for (int j = 0; j < NP; ++j) a[j] = __builtin_bit_cast(gbf16x8, *(const gu32x4 *)(frag + 256 * j + lane * 4));
+    auto both = [&](int i, int j) {
+      c[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], __builtin_bit_cast(gbf16x8, x.v[0][kc][j]), c[0], 0, 0, 0);
+      c[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], __builtin_bit_cast(gbf16x8, x.v[1][kc][j]), c[1], 0, 0, 0);
+    };
+    if constexpr (!BF16) {
+      both(2, 0);
+      both(1, 1);
+      both(0, 2);
+      both(1, 0);
+      both(0, 1);
     }
+    both(0, 0);
   }
 
   // z of row (lane) of the 64

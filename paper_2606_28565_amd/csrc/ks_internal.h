@@ -30,7 +30,8 @@ enum HeadKind : int {
   kEtaOne = 0,
   kF32_16_64, kF32_16_128, kF32_32_64, kF32_32_128,
   kBF16_16_64, kBF16_16_128, kBF16_16_256, kBF16_32_64, kBF16_32_128, kBF16_32_256,
-  kGatedF32_16, kGatedF32_32, kGatedBF16_16, kGatedBF16_32,   // any hidden up to 256
+  // any hidden up to 256 (kGatedF32_32: 128)
+  kGatedF32_16, kGatedF32_32, kGatedF32_32_256, kGatedBF16_16, kGatedBF16_32,
   kBoundedOnly,   // no MLP: bounded-head and grid families, eta = 1 for the rest
   kNumKinds
 };
@@ -289,7 +290,7 @@ hipError_t launch_validate(const ValidateParams &p, hipStream_t s);
 
 // ---- gated heads over rows (ks_gated.hip)
 // A forward workgroup takes fwd_tiles 64-row tiles of one family, a backward
-// workgroup bwd_rows rows of one (a multiple of 16 per row group).
+// workgroup bwd_rows rows of one (a multiple of gated_rows()).
 struct GatedParams {
   const void *x;
   int64_t ldx;
@@ -304,8 +305,7 @@ struct GatedParams {
   // the loss (eta null: none)
   const float *eta, *weight;
   float huber;
-  float *dz_out;                     // w rho'(r) dr/dz, not yet over sum w; null: the loss alone
-  double *loss_part;                 // [forward workgroups][2]: sum w rho, sum w
+  double *loss_part;                 // [workgroups of the kernel that forms it][2]: sum w rho, sum w
   float *loss;                       // [KS_NFAM]
   // gradients
   const float *dz;
@@ -315,14 +315,20 @@ struct GatedParams {
   int64_t g_ldx;
   bool g_vec;
 };
-constexpr int kGatedGroup = 64;      // units per wave of the backward kernel
-constexpr int gated_groups(int hidden) { return (hidden + kGatedGroup - 1) / kGatedGroup; }
-// floats of a backward workgroup's sums: per group of 64 units dW1, dW2 and dw3; db3
+constexpr int gated_groups(int hidden, int group) { return (hidden + group - 1) / group; }
+// k_gated_fit's unit groups and waves by kind, and the rows its workgroup takes at a
+// time (row groups x rows in hand)
+constexpr int gated_rows(bool bf16, int in_dim, int hidden) {
+  const bool wide = !bf16 && in_dim == 32;
+  return (wide ? 16 : 32) * ((wide ? 8 : 4) / gated_groups(hidden, wide ? 32 : 64));
+}
+// floats of its sums: dW1 and dW2 by groups of 64 units (the last one whole); db3
+constexpr int kGatedGroup = 64;
 constexpr int gated_part_size(int hidden, int in_dim) {
-  return gated_groups(hidden) * kGatedGroup * (2 * in_dim + 1) + 1;
+  return gated_groups(hidden, kGatedGroup) * kGatedGroup * 2 * in_dim + 1;
 }
 hipError_t launch_gated_forward(const GatedParams &p, hipStream_t s);
-hipError_t launch_gated_backward(const GatedParams &p, hipStream_t s);
+hipError_t launch_gated_fit(const GatedParams &p, hipStream_t s);      // sums of a given dz, or of the loss
 hipError_t launch_gated_rows(const GatedParams &p, hipStream_t s);     // g_x
 hipError_t launch_gated_reduce(const GatedParams &p, hipStream_t s);   // gradients and the loss
 

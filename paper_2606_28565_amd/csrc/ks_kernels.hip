@@ -1399,9 +1399,9 @@ struct HeadF32 {
 
 // The gated block (ks_gated.h) as a head: a lane's row of features becomes the
 // column operand by exchanging the wave's halves.
-template <bool BF16, int IN>
+template <bool BF16, int IN, int HID>
 struct HeadGated {
-  using G = gated::Block<BF16, IN>;
+  using G = gated::Block<BF16, IN, HID>;
   static constexpr bool kRaw = false;
   static constexpr int LDS_DW = G::kLds;
   static constexpr bool kMlp = true;
@@ -1415,27 +1415,23 @@ struct HeadGated {
 
   __device__ static __forceinline__ float mlp(const float (&x)[IN], const uint32_t *lds) {
     typename G::Rows r;
+    uint32_t P[IN / 2][3];
 #pragma unroll
-    for (int kc = 0; kc < G::KC; ++kc) {
-      if constexpr (BF16) {
+    for (int c = 0; c < IN / 2; ++c) {
+      if constexpr (BF16) P[c][0] = pack_bf16(x[2 * c], x[2 * c + 1]);
+      else gated::split2(x[2 * c], x[2 * c + 1], P[c][0], P[c][1], P[c][2]);
+    }
+#pragma unroll
+    for (int kc = 0; kc < G::KC; ++kc)
+#pragma unroll
+      for (int i = 0; i < G::NP; ++i)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          uint32_t lo = pack_bf16(x[16 * kc + 2 * q], x[16 * kc + 2 * q + 1]);
-          uint32_t hi = pack_bf16(x[16 * kc + 8 + 2 * q], x[16 * kc + 9 + 2 * q]);
+          uint32_t lo = P[8 * kc + q][i], hi = P[8 * kc + 4 + q][i];
           swap32(lo, hi);
-          r.v[0][kc][0][q] = lo;
-          r.v[1][kc][0][q] = hi;
+          r.v[0][kc][i][q] = lo;
+          r.v[1][kc][i][q] = hi;
         }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          uint32_t lo = __builtin_bit_cast(uint32_t, x[16 * kc + j]), hi = __builtin_bit_cast(uint32_t, x[16 * kc + 8 + j]);
-          swap32(lo, hi);
-          r.v[0][kc][j >> 2][j & 3] = lo;
-          r.v[1][kc][j >> 2][j & 3] = hi;
-        }
-      }
-    }
     return G::z_of(r, lds);
   }
 };
@@ -1463,10 +1459,11 @@ template <> struct KindOf<kBF16_16_256> { using H = HeadBF16<16, 256>; static co
 template <> struct KindOf<kBF16_32_64> { using H = HeadBF16<32, 64>; static constexpr int IN = 32; };
 template <> struct KindOf<kBF16_32_128> { using H = HeadBF16<32, 128>; static constexpr int IN = 32; };
 template <> struct KindOf<kBF16_32_256> { using H = HeadBF16<32, 256>; static constexpr int IN = 32; };
-template <> struct KindOf<kGatedF32_16> { using H = HeadGated<false, 16>; static constexpr int IN = 16; };
-template <> struct KindOf<kGatedF32_32> { using H = HeadGated<false, 32>; static constexpr int IN = 32; };
-template <> struct KindOf<kGatedBF16_16> { using H = HeadGated<true, 16>; static constexpr int IN = 16; };
-template <> struct KindOf<kGatedBF16_32> { using H = HeadGated<true, 32>; static constexpr int IN = 32; };
+template <> struct KindOf<kGatedF32_16> { using H = HeadGated<false, 16, 256>; static constexpr int IN = 16; };
+template <> struct KindOf<kGatedF32_32> { using H = HeadGated<false, 32, 128>; static constexpr int IN = 32; };
+template <> struct KindOf<kGatedF32_32_256> { using H = HeadGated<false, 32, 256>; static constexpr int IN = 32; };
+template <> struct KindOf<kGatedBF16_16> { using H = HeadGated<true, 16, 256>; static constexpr int IN = 16; };
+template <> struct KindOf<kGatedBF16_32> { using H = HeadGated<true, 32, 256>; static constexpr int IN = 32; };
 
 // ------------------------------------------------------------ segmented scan
 // Inclusive scan of a wave's 64 values, segmented by sorted keys, with DPP
@@ -2999,6 +2996,8 @@ template hipError_t launch_kind<kGatedF32_16>(const EvalParams &, hipStream_t);
 template hipError_t launch_uniq<kGatedF32_16>(const EvalParams &, hipStream_t);
 template hipError_t launch_kind<kGatedF32_32>(const EvalParams &, hipStream_t);
 template hipError_t launch_uniq<kGatedF32_32>(const EvalParams &, hipStream_t);
+template hipError_t launch_kind<kGatedF32_32_256>(const EvalParams &, hipStream_t);
+template hipError_t launch_uniq<kGatedF32_32_256>(const EvalParams &, hipStream_t);
 template hipError_t launch_kind<kGatedBF16_16>(const EvalParams &, hipStream_t);
 template hipError_t launch_uniq<kGatedBF16_16>(const EvalParams &, hipStream_t);
 template hipError_t launch_kind<kGatedBF16_32>(const EvalParams &, hipStream_t);
@@ -3029,6 +3028,8 @@ extern template hipError_t launch_kind<kGatedF32_16>(const EvalParams &, hipStre
 extern template hipError_t launch_uniq<kGatedF32_16>(const EvalParams &, hipStream_t);
 extern template hipError_t launch_kind<kGatedF32_32>(const EvalParams &, hipStream_t);
 extern template hipError_t launch_uniq<kGatedF32_32>(const EvalParams &, hipStream_t);
+extern template hipError_t launch_kind<kGatedF32_32_256>(const EvalParams &, hipStream_t);
+extern template hipError_t launch_uniq<kGatedF32_32_256>(const EvalParams &, hipStream_t);
 extern template hipError_t launch_kind<kGatedBF16_16>(const EvalParams &, hipStream_t);
 extern template hipError_t launch_uniq<kGatedBF16_16>(const EvalParams &, hipStream_t);
 extern template hipError_t launch_kind<kGatedBF16_32>(const EvalParams &, hipStream_t);
@@ -3177,6 +3178,7 @@ static hipError_t launch_direct(int kind, const EvalParams &p, hipStream_t s) {
     case kBF16_32_256: return launch_kind<kBF16_32_256>(p, s);
     case kGatedF32_16: return launch_kind<kGatedF32_16>(p, s);
     case kGatedF32_32: return launch_kind<kGatedF32_32>(p, s);
+    case kGatedF32_32_256: return launch_kind<kGatedF32_32_256>(p, s);
     case kGatedBF16_16: return launch_kind<kGatedBF16_16>(p, s);
     case kGatedBF16_32: return launch_kind<kGatedBF16_32>(p, s);
     default: return hipErrorInvalidValue;
@@ -3197,6 +3199,7 @@ static hipError_t launch_uniq_kind(int kind, const EvalParams &p, hipStream_t s)
     case kBF16_32_256: return launch_uniq<kBF16_32_256>(p, s);
     case kGatedF32_16: return launch_uniq<kGatedF32_16>(p, s);
     case kGatedF32_32: return launch_uniq<kGatedF32_32>(p, s);
+    case kGatedF32_32_256: return launch_uniq<kGatedF32_32_256>(p, s);
     case kGatedBF16_16: return launch_uniq<kGatedBF16_16>(p, s);
     case kGatedBF16_32: return launch_uniq<kGatedBF16_32>(p, s);
     default: return hipErrorInvalidValue;

@@ -359,11 +359,15 @@ def test_rows_that_do_not_count(prec, hid):
 
 
 def test_loss_alone_is_the_same_loss():
+    """The loss without gradients comes from another kernel, which adds a row's units
+    in another order (32 of a lane's registers at a time instead of 16 lanes): each sum
+    of H products is off by up to (H + 2) 2^-24 of its magnitudes whatever its order, so
+    both are held to that bound (check_loss), not to the same bits."""
     d, h, off = make(1000, "f32", 32, 64)
     eta, weight = targets(1000)
     a = run_loss(d, off, eta.cuda(), weight.cuda(), 0.3)
     b = run_loss(d, off, eta.cuda(), weight.cuda(), 0.3, grad=False, with_z=False)
-    assert (a[0] == b[0]).all()
+    check_loss(h, off, eta, weight, 0.3, a)
     check_loss(h, off, eta, weight, 0.3, b[:1] + a[1:], grad=True)
 
 
