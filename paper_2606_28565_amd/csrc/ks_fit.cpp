@@ -50,7 +50,7 @@ constexpr int64_t kFwdWgs = 1024, kBwdWgs = 512;
 void plan(ks::GatedParams &p, const ks_heads *h, const ks_rows *r) {
   const int64_t tiles = (r->n_rows + 63) / 64;
   p.fwd_tiles = (int32_t)(4 * std::max<int64_t>(1, (tiles + 4 * kFwdWgs - 1) / (4 * kFwdWgs)));
-  const int64_t unit = ks::gated_rows(h->precision == KS_BF16, h->in_dim, h->hidden);
+  const int64_t unit = ks::kGatedStep;
   p.bwd_rows = (int32_t)(unit * std::max<int64_t>(1, (r->n_rows + unit * kBwdWgs - 1) / (unit * kBwdWgs)));
   p.fwd_wg[0] = p.bwd_wg[0] = 0;
   for (int f = 0; f < KS_NFAM; ++f) {
@@ -60,15 +60,16 @@ void plan(ks::GatedParams &p, const ks_heads *h, const ks_rows *r) {
   }
 }
 
-// Workspace: the backward workgroups' gradient sums, then either kernel's
-// workgroups' loss sums.
+// Workspace: the backward workgroups' sums, then (the loss) the forward
+// workgroups' sums and each row's dz.
 struct Room {
-  size_t loss, total;
+  size_t loss, dz, total;
 };
 Room room_of(const ks::GatedParams &p) {
   Room o;
   o.loss = align256((size_t)p.bwd_wg[KS_NFAM] * ks::gated_part_size(p.hidden, p.in_dim) * sizeof(float));
-  o.total = o.loss + align256((size_t)std::max(p.fwd_wg[KS_NFAM], p.bwd_wg[KS_NFAM]) * 2 * sizeof(double));
+  o.dz = o.loss + align256((size_t)p.fwd_wg[KS_NFAM] * 2 * sizeof(double));
+  o.total = o.dz + align256((size_t)p.fam_off[KS_NFAM] * sizeof(float));
   return o;
 }
 
@@ -181,7 +182,7 @@ ks_status ks_gated_backward(const ks_heads *heads, const ks_rows *rows, const fl
   p.dz = dz;
   p.part = static_cast<float *>(ws);
   if (p.g_w1) {
-    hipError_t e = ks::launch_gated_fit(p, stream);
+    hipError_t e = ks::launch_gated_sums(p, stream);
     if (e == hipSuccess) e = ks::launch_gated_reduce(p, stream);
     if (e != hipSuccess) return hip_error(e, "gated backward launch");
   }
@@ -219,7 +220,10 @@ ks_status ks_gated_loss(const ks_heads *heads, const ks_rows *rows, const ks_eta
   p.loss = loss;
   p.loss_part = reinterpret_cast<double *>(w + room.loss);
   p.part = reinterpret_cast<float *>(w);
-  hipError_t e = p.g_w1 ? ks::launch_gated_fit(p, stream) : ks::launch_gated_forward(p, stream);
+  if (p.g_w1) p.dz_out = reinterpret_cast<float *>(w + room.dz);
+  p.dz = p.dz_out;
+  hipError_t e = ks::launch_gated_forward(p, stream);
+  if (e == hipSuccess && p.g_w1) e = ks::launch_gated_sums(p, stream);
   if (e == hipSuccess) e = ks::launch_gated_reduce(p, stream);
   return hip_error(e, "gated loss launch");
 }

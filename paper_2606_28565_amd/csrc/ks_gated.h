@@ -42,7 +42,9 @@ typedef float gf32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((gf32x2{lo, hi}), gbf16x2));
 }
-// a pair of values as three packed pairs of pieces
+// a pair of values as three packed pairs of pieces.  (A piece could be taken off in one
+// instruction, the dot product with (-1, 0) or (0, -1), but that one waits for the
+// matrix instructions of every wave, as the shift or mask and the subtraction do not.)
 __device__ __forceinline__ void split2(float a, float b, uint32_t &p0, uint32_t &p1, uint32_t &p2) {
   p0 = pack2(a, b);
   a -= __builtin_bit_cast(float, p0 << 16);
@@ -51,6 +53,12 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t &p0, uint32_t 
   a -= __builtin_bit_cast(float, p1 << 16);
   b -= __builtin_bit_cast(float, p1 & 0xFFFF0000u);
   p2 = pack2(a, b);
+}
+
+// ... as two, to within 2^-18 of each (half a step of a half step, 2^-9 2^-9)
+__device__ __forceinline__ void split2(float a, float b, uint32_t &p0, uint32_t &p1) {
+  p0 = pack2(a, b);
+  p1 = pack2(a - __builtin_bit_cast(float, p0 << 16), b - __builtin_bit_cast(float, p0 & 0xFFFF0000u));
 }
 
 // HID: the widest block that fits the LDS room (any narrower one too)

@@ -1,15 +1,14 @@
 // Gated heads over feature rows: the block, its gradients and the loss on
 // log eta (ks.h).  Rows are grouped by family; a workgroup works on rows of one.
 //
-//   k_gated_forward   z, or the loss alone
-//   k_gated_fit       weight gradients of a workgroup's rows, held in registers: of
-//                     a given dz, or of the loss, whose dz it forms on the way
+//   k_gated_forward   z, and for a fit the loss sums and dz of each row
+//   k_gated_sums      weight gradients of a workgroup's rows, held in registers
 //   k_gated_rows      gradients of the rows
 //   k_gated_reduce    sums of the workgroups' gradients in a fixed order
 //
 // The derivative at a row, with s = sigma(g), a = g s:
 //   du = dz w3 a,  dg = dz w3 u silu'(g),  silu'(g) = s + s (g - a),  dw3 += dz a u.
-// w3 is one factor of a unit over all rows, so k_gated_fit leaves it out and
+// w3 is one factor of a unit over all rows, so k_gated_sums leaves it out and
 // k_gated_reduce multiplies the finished sums by it.  dz is one factor of a row
 // over all units, so it goes to the rows' side of the product, dW = (..)^T (dz x).
 // And u = W2 x, so sum dz a u = W2 . (sum dz a x): dw3 follows from the finished
@@ -23,12 +22,12 @@ namespace ks {
 
 using gated::Block;
 using gated::gbf16x8;
+using gated::gf32x16;
 using gated::gf32x4;
 using gated::gu32x4;
 using gated::sigmoid;
 using gated::split2;
 
-typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 namespace {
@@ -139,10 +138,12 @@ __global__ __launch_bounds__(64 * N, 2) void k_gated_forward(GatedParams p) {
       if constexpr (LOSS) {
         const float eta = p.eta[row], wt = p.weight ? p.weight[row] : 1.0f;
         const bool counts = eta > 0.0f && eta < __builtin_inff() && wt > 0.0f && wt < __builtin_inff();
+        const EtaTerm e = eta_term(z, eta, wt, p.huber);
         if (counts) {
-          sum += (double)eta_term(z, eta, wt, p.huber).loss;
+          sum += (double)e.loss;
           total += (double)wt;
         }
+        if (p.dz_out) p.dz_out[row] = counts ? e.dz : 0.0f;
       }
     }
   }
@@ -167,417 +168,260 @@ __global__ __launch_bounds__(64 * N, 2) void k_gated_forward(GatedParams p) {
 }
 
 // ------------------------------------------------------------ gradients
-// A wave takes 16 NB units (their weights and gradients in its registers) and 16 T
-// rows at a time on the 16x16x32 instruction: the rows as the row operand, so a
-// lane holds the gates and ups of one unit for four rows of a tile, and what it makes
-// of them is the row operand of the next product, dW (units x features), without
-// any exchange between lanes.  The workgroup's W waves are the unit groups times row
-// groups; for the loss, the unit groups exchange their parts of each row's z through
-// LDS (one barrier per 16 T rows, two buffers); row groups are joined in LDS at the
-// end.
+// dW1 = sum (u silu'(g)) (dz x)^T, dW2 = sum a (dz x)^T over a workgroup's rows.  A
+// wave takes 32 units (their weights and gradients in its registers) and 32 rows at a
+// time on the 32x32x16 instruction: the rows as the row operand of the projections,
+// so a lane holds the gates and ups of one unit for 16 of the rows, and what it makes
+// of them is the row operand of the next product, units x features, without any
+// exchange between lanes.  The eight waves are the unit groups (HG) times row groups
+// (RG).  What depends on the rows alone is made once for all of them: each wave
+// brings 16 rows a step, as the projections' operand and as dz x in three bf16 pieces,
+// and leaves both in LDS.  What a unit makes of a row is three pieces too for fp32
+// heads (gradients are then sums of unrounded terms); for bf16 heads, whose features
+// and weights are rounded to 2^-9, two, within 2^-18 of each term (5 instructions
+// fewer of 19 per gate; 2M rows of 32-256: 437 us, with three 530).
 //
-// Which eight of the instruction's 32 inner indices a lane holds is free, as long as
-// both operands agree: of a tile's 16 rows (or 16 fp32 features) a lane has four, so
-// one instruction takes two of the six products of pieces.  dz x is split for either
-// precision: gradients are sums of unrounded terms, to 2^-25 of each.
+// Which rows a lane's eight inner indices of dW stand for is free, as long as both
+// operands agree: those it has, 8 (i / 4) + 4 (its half) + i mod 4 of each 16.  With 16
+// inputs the instruction's 32 columns are the features twice, against the first and
+// the second piece of dz x (then the third and nothing): a unit's gradient is the sum
+// of the two halves.
+//
+// Vector work bounds it: 8 instructions, an exponential and a reciprocal for each gate
+// and 7 to split what it makes.  A wave alone issues a vector instruction every 7.5
+// cycles, four per SIMD one every 2.7 (FMA) to 4.4, hence 128 registers and 32 units per
+// wave; and the 32x32x16 instruction runs beside them where 16x16x32 does not (two
+// waves of each kind per SIMD: 678 cycles where one kind alone takes 647 and 367;
+// 16x16x32 625, of 322 and 367).  (2M rows of 32-256 in bf16, loss and gradients: 64
+// units per wave, z exchanged between them and dz formed on the way took 776 us, this
+// and k_gated_forward take 437 and 175.)
 template <bool BF16, int IN>
 struct Back {
-  static constexpr int KC = IN / 16;
-  static constexpr bool kWide = !BF16 && IN == 32;   // most registers per unit: fewer units, one tile
-  static constexpr int NB = kWide ? 2 : 4, W = kWide ? 8 : 4, T = kWide ? 1 : 2;
-  static constexpr int kGroup = 16 * NB;
-  // a lane's part of a row (or of a unit's weights): features 4 q .. 4 q + 3 for 16
-  // inputs, 8 q .. 8 q + 7 for 32, as read
-  static constexpr int kRaw = BF16 ? IN / 8 : IN / 4;
-  struct Raw {
-    uint32_t v[kRaw];
-  };
-  __device__ static __forceinline__ Raw load(const char *x, int q, bool vec) {
-    constexpr int kBytes = 4 * kRaw;
-    Raw o;
-    const char *p = x + q * kBytes;
-    if (vec) {
-      if constexpr (kBytes == 8) {
-        const u32x2 t = *(const u32x2 *)p;
-        o.v[0] = t[0], o.v[1] = t[1];
-      } else {
-#pragma unroll
-        for (int i = 0; i < kRaw / 4; ++i) {
-          const gu32x4 t = *(const gu32x4 *)(p + 16 * i);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o.v[4 * i + j] = t[j];
-        }
-      }
-    } else if constexpr (BF16) {
-      const uint16_t *h = (const uint16_t *)p;
-#pragma unroll
-      for (int j = 0; j < kRaw; ++j) o.v[j] = h[2 * j] | (uint32_t)h[2 * j + 1] << 16;
-    } else {
-#pragma unroll
-      for (int j = 0; j < kRaw; ++j) o.v[j] = ((const uint32_t *)p)[j];
-    }
-    return o;
+  static constexpr int KC = IN / 16, W = 8;
+  static constexpr int NP = BF16 ? 1 : 3;      // pieces of the projections' operands
+  static constexpr int NQ = IN == 16 ? 2 : 3;  // column operands of dW
+  static constexpr int NA = BF16 ? 2 : 3;      // pieces of its row operands
+  // eight consecutive values as pieces
+  __device__ static __forceinline__ void pieces(const gu32x4 (&raw)[BF16 ? 1 : 2], gu32x4 (&x)[NP]) {
+    if constexpr (BF16) x[0] = raw[0];
+    else Block<false, IN, 32>::split8(__builtin_bit_cast(gf32x4, raw[0]), __builtin_bit_cast(gf32x4, raw[1]), x);
   }
-  __device__ static __forceinline__ void keep(Raw &o, bool k) {
-#pragma unroll
-    for (auto &v : o.v) v = k ? v : 0u;
-  }
-  // the operands of the projections.  fp32: with 16 inputs two pieces at a time (X0 X2,
-  // X1 X1, X0 X0 against W2 W0, W0 W1, W0 W1), with 32 one piece (0, 1, 2)
-  static constexpr int kX = BF16 ? 1 : 3, kW = BF16 ? 1 : IN == 16 ? 2 : 3;
-  struct Rows {
-    gu32x4 v[kX];
-  };
-  struct Units {
-    gu32x4 v[kW];
-  };
-  __device__ static __forceinline__ void pieces(const Raw &o, uint32_t (&p)[3][kRaw / 2 > 0 ? kRaw / 2 : 1]) {
-#pragma unroll
-    for (int j = 0; j < kRaw / 2; ++j)
-      split2(__builtin_bit_cast(float, o.v[2 * j]), __builtin_bit_cast(float, o.v[2 * j + 1]), p[0][j], p[1][j], p[2][j]);
-  }
-  __device__ static __forceinline__ Rows rows(const Raw &o) {
-    Rows r;
-    if constexpr (BF16) {
-      r.v[0] = gu32x4{o.v[0], o.v[1], IN == 16 ? 0u : o.v[kRaw - 2], IN == 16 ? 0u : o.v[kRaw - 1]};
-    } else {
-      uint32_t p[3][kRaw / 2];
-      pieces(o, p);
-      if constexpr (IN == 16) {
-        r.v[0] = gu32x4{p[0][0], p[0][1], p[2][0], p[2][1]};
-        r.v[1] = gu32x4{p[1][0], p[1][1], p[1][0], p[1][1]};
-        r.v[2] = gu32x4{p[0][0], p[0][1], p[0][0], p[0][1]};
-      } else {
-#pragma unroll
-        for (int i = 0; i < 3; ++i) r.v[i] = gu32x4{p[i][0], p[i][1], p[i][kRaw / 2 - 2], p[i][kRaw / 2 - 1]};
-      }
-    }
-    return r;
-  }
-  __device__ static __forceinline__ Units units(const Raw &o) {
-    Units r;
-    if constexpr (BF16) {
-      r.v[0] = rows(o).v[0];
-    } else {
-      uint32_t p[3][kRaw / 2];
-      pieces(o, p);
-      if constexpr (IN == 16) {
-        r.v[0] = gu32x4{p[2][0], p[2][1], p[0][0], p[0][1]};
-        r.v[1] = gu32x4{p[0][0], p[0][1], p[1][0], p[1][1]};
-      } else {
-#pragma unroll
-        for (int i = 0; i < 3; ++i) r.v[i] = gu32x4{p[i][0], p[i][1], p[i][kRaw / 2 - 2], p[i][kRaw / 2 - 1]};
-      }
-    }
-    return r;
-  }
-  __device__ static __forceinline__ gf32x4 mfma(const gu32x4 &a, const gu32x4 &b, const gf32x4 &c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(gbf16x8, a), __builtin_bit_cast(gbf16x8, b), c, 0, 0, 0);
-  }
-  // rows x units (a lane: rows 4 q .. 4 q + 3 of unit c)
-  __device__ static __forceinline__ gf32x4 product(const Rows &x, const Units &w) {
-    gf32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
-    if constexpr (BF16 && IN == 16) {
-      c = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, u32x2{x.v[0][0], x.v[0][1]}),
-                                                    __builtin_bit_cast(s16x4, u32x2{w.v[0][0], w.v[0][1]}), c, 0, 0, 0);
-    } else if constexpr (BF16) {
-      c = mfma(x.v[0], w.v[0], c);
-    } else if constexpr (IN == 16) {
-      c = mfma(x.v[0], w.v[0], c);
-      c = mfma(x.v[1], w.v[1], c);
-      c = mfma(x.v[2], w.v[1], c);
-    } else {
-      c = mfma(x.v[2], w.v[0], c);
-      c = mfma(x.v[1], w.v[1], c);
-      c = mfma(x.v[0], w.v[2], c);
-      c = mfma(x.v[1], w.v[0], c);
-      c = mfma(x.v[0], w.v[1], c);
-      c = mfma(x.v[0], w.v[0], c);
-    }
-    return c;
+  __device__ static __forceinline__ gf32x16 mfma(const gu32x4 &a, const gu32x4 &b, const gf32x16 &c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(gbf16x8, a), __builtin_bit_cast(gbf16x8, b), c, 0, 0, 0);
   }
 };
 
-// the sum of a row of 16 lanes, in each of them
-template <int CTRL>
-__device__ __forceinline__ float row_add(float v) {
-  const int o = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true);
-  return v + __builtin_bit_cast(float, o);
-}
-__device__ __forceinline__ float row_sum(float v) {
-  v = row_add<0x128>(v);   // row_ror:8, 4, 2, 1
-  v = row_add<0x124>(v);
-  v = row_add<0x122>(v);
-  return row_add<0x121>(v);
-}
-
-template <bool BF16, int IN, bool LOSS>
-__global__ __launch_bounds__((64 * Back<BF16, IN>::W), 2) void k_gated_fit(GatedParams p) {
+template <bool BF16, int IN>
+__global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(GatedParams p) {
   using K = Back<BF16, IN>;
-  using Raw = typename K::Raw;
-  constexpr int KC = K::KC, NB = K::NB, T = K::T, W = K::W, R = 16 * T;
-  constexpr int kWords = 2 * NB * KC * 4 + 1;
-  __shared__ float join[W - 1][kWords][64];
-  __shared__ __align__(16) float zbuf[2][W][R];   // a wave's part of z of the rows in hand
-  __shared__ __align__(16) float dzbuf[W][R];
-  const int lane = threadIdx.x & 63, q = lane >> 4, c = lane & 15;
+  constexpr int KC = K::KC, W = K::W, NP = K::NP, NQ = K::NQ, NA = K::NA, R = 16 * W;   // rows of a step
+  constexpr int kTiles = R / 32;
+  constexpr int kX = kTiles * KC * NP * 64 * 4, kQ = kTiles * 2 * NQ * 64 * 4, kJoin = (W - 1) * 16 * 64;
+  __shared__ __align__(16) uint32_t lds[kX + kQ > kJoin ? kX + kQ : kJoin];
+  gu32x4(*lx)[KC][NP][64] = reinterpret_cast<gu32x4(*)[KC][NP][64]>(lds);          // [tile]: rows
+  gu32x4(*lq)[2][NQ][64] = reinterpret_cast<gu32x4(*)[2][NQ][64]>(lds + kX);       // [tile][16 rows]: dz x
+  const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int HG = gated_groups(p.hidden, K::kGroup), RG = W / HG;
+  const int HG = (p.hidden + kGatedGroup - 1) / kGatedGroup, RG = HG > 4 ? 1 : HG > 2 ? 2 : 4;   // (four tiles)
   const int hg = wave % HG, rg = wave / HG;
-  const int wg = blockIdx.x, f = family_of(p.bwd_wg, wg);
   const bool works = rg < RG;
+  const int wg = blockIdx.x, f = family_of(p.bwd_wg, wg);
   const int64_t begin = p.fam_off[f] + (int64_t)(wg - p.bwd_wg[f]) * p.bwd_rows;
   const int64_t fam_end = p.fam_off[f + 1];
   const int64_t end = begin + p.bwd_rows < fam_end ? begin + p.bwd_rows : fam_end;
-  const int steps = (int)((end - begin + R * RG - 1) / (R * RG));   // the same for every wave
-  gf32x4 dw[2][NB][KC] = {};
+  gf32x16 dw[2] = {gf32x16{}, gf32x16{}};
   float d0 = 0.0f;
-  double sum = 0.0, total = 0.0;
-  typename K::Units wgt[2][NB];
-  float w3[NB] = {};
+  gu32x4 wgt[2][KC][NP];
   {
-    constexpr int E = BF16 ? 2 : 4;
     const bool vec = ((reinterpret_cast<uintptr_t>(p.w1) | reinterpret_cast<uintptr_t>(p.w2)) & 15) == 0;
+    const int unit = hg * kGatedGroup + n;
+    const bool there = works && unit < p.hidden;
+    const int64_t at = ((int64_t)f * p.hidden + (there ? unit : 0)) * IN + 8 * h;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int unit = hg * K::kGroup + 16 * b + c;
-      const bool there = works && unit < p.hidden;
-      const size_t at = ((size_t)f * p.hidden + (there ? unit : 0)) * IN * E;
-      Raw a1 = K::load((const char *)p.w1 + at, q, vec), a2 = K::load((const char *)p.w2 + at, q, vec);
-      K::keep(a1, there);
-      K::keep(a2, there);
-      wgt[0][b] = K::units(a1);
-      wgt[1][b] = K::units(a2);
-      if (LOSS && there) w3[b] = element<BF16>(p.w3, (int64_t)f * p.hidden + unit);
-    }
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int k = 0; k < KC; ++k) {
+        gu32x4 raw[BF16 ? 1 : 2];
+        load8<BF16>(raw, m ? p.w2 : p.w1, at + 16 * k, vec);
+#pragma unroll
+        for (auto &v : raw) v = there ? v : gu32x4{0, 0, 0, 0};
+        K::pieces(raw, wgt[m][k]);
+      }
   }
-  const float b3 = LOSS ? element<BF16>(p.b3, f) : 0.0f;
-  // Rows row0 .. row0 + R - 1 of a step; past the last row a lane reads the last.
-  const uint32_t ld = (uint32_t)p.ldx * (BF16 ? 2 : 4);
-  const int i_row = lane & (R - 1);   // the row whose loss (or dz) the lane forms
-  const uint32_t off_a = __umul24(c, ld), off_b = __umul24(4 * q, ld) + c * (BF16 ? 2 : 4);
-  Raw xa[T];
-  float in0 = 0.0f, in1 = 1.0f, dza[T];
-  auto fetch = [&](int64_t row0) {
-    const int64_t base = row0 < end ? row0 : end - 1;
-    const int left = end - base < R ? (int)(end - base) : R;   // rows there
-    const char *x = (const char *)p.x + base * ld;
-#pragma unroll
-    for (int t = 0; t < T; ++t) {
-      const uint32_t r = min(16 * t + c, left - 1);
-      xa[t] = K::load(left == R ? x + (size_t)(16 * t) * ld + off_a : x + __umul24(r, ld), q, p.vec);
-      if (!LOSS) dza[t] = p.dz[base + r];
-    }
-    const int64_t mine = base + min(i_row, left - 1);
-    if (LOSS) {
-      in0 = p.eta[mine];
-      if (p.weight) in1 = p.weight[mine];
-    } else {
-      in0 = p.dz[mine];
-    }
-  };
-  int64_t row0 = begin + R * rg;
-  if (works) fetch(row0);
+  // the wave's 16 rows of a step: 16 of tile wave / 2
+  const int tile = wave >> 1, half = wave & 1;
+  const uint32_t ld = (uint32_t)p.ldx;
+  const int oct = lane >> 4;                       // the eight features a lane brings of row c
+  const bool brings = IN == 32 || oct < 2;
+  const int col = IN == 32 ? n : c;                // ... and the feature of its rows
+  constexpr int E = BF16 ? 2 : 4;
+  const uint32_t off_row = __umul24(c, ld * E) + (brings ? 8 * E * oct : 0), off_col = __umul24(4 * h, ld * E) + col * E;
 #pragma unroll 1
-  for (int step = 0; step < steps; ++step, row0 += R * RG) {
-    float av[T][NB][4], gv[T][NB][4], zp[T][4] = {};
-    float xb[T][4][KC];
-    const float cur0 = in0, cur1 = in1;
-    if (works) {
-      typename K::Rows xc[T];
+  for (int64_t row0 = begin; row0 < end; row0 += R) {
+    const int64_t mine = row0 + 16 * wave;
+    const int there = end - mine < 16 ? (int)(end - mine) - 1 : 15;   // the last of the wave's rows; below 0: none
+    gu32x4 raw[BF16 ? 1 : 2];
+    float v[8], dz[8], dzc;
+    if (there == 15) {
+      const char *x = (const char *)p.x + mine * ld * E;
+      const float *z = p.dz + mine;
+      load8<BF16>(raw, x + off_row, 0, p.vec);
+      dzc = z[c];
 #pragma unroll
-      for (int t = 0; t < T; ++t) {
-        // (a row whose dz is 0 adds nothing, whatever it holds)
-        if (!LOSS) K::keep(xa[t], dza[t] != 0.0f && row0 + 16 * t + c < end);
-        xc[t] = K::rows(xa[t]);
-      }
-      if (row0 + R <= end) {
-        const char *x = (const char *)p.x + row0 * ld;
-#pragma unroll
-        for (int t = 0; t < T; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int k = 0; k < KC; ++k)
-              xb[t][r][k] = element<BF16>(x + (size_t)(16 * t + r) * ld + off_b, 16 * k);
-      } else {
-        const int64_t base = row0 < end ? row0 : end - 1;
-        const int last = (int)(end - base) - 1;
-        const char *x = (const char *)p.x + base * ld;
-#pragma unroll
-        for (int t = 0; t < T; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int k = 0; k < KC; ++k)
-              xb[t][r][k] = element<BF16>(x + __umul24(min(16 * t + 4 * q + r, last), ld), 16 * k + c);
-      }
-      fetch(row0 + R * RG);
-#pragma unroll
-      for (int t = 0; t < T; ++t)
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          const gf32x4 g = K::product(xc[t], wgt[0][b]), u = K::product(xc[t], wgt[1][b]);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float s = sigmoid(g[r]), a = g[r] * s;
-            av[t][b][r] = a;
-            gv[t][b][r] = u[r] * fmaf(s, g[r] - a, s);   // u silu'(g)
-            if (LOSS) zp[t][r] = fmaf(w3[b], a * u[r], zp[t][r]);
-          }
-        }
-    }
-    float dz = 0.0f;
-    if constexpr (LOSS) {
-#pragma unroll
-      for (int t = 0; t < T; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) zp[t][r] = row_sum(zp[t][r]);
-      float(*zb)[R] = zbuf[step & 1];
-      if (works && c == 0) {
-#pragma unroll
-        for (int t = 0; t < T; ++t) *(gf32x4 *)&zb[wave][16 * t + 4 * q] = gf32x4{zp[t][0], zp[t][1], zp[t][2], zp[t][3]};
-      }
-      if (HG > 1) __syncthreads();
-      else __builtin_amdgcn_wave_barrier();
-      if (works) {
-        float z = b3;
-        for (int h = 0; h < HG; ++h) z += zb[rg * HG + h][i_row];
-        const int64_t row = row0 + i_row;
-        const bool there = row < end;
-        const bool counts = there && cur0 > 0.0f && cur0 < __builtin_inff() && cur1 > 0.0f && cur1 < __builtin_inff();
-        const EtaTerm e = eta_term(z, cur0, cur1, p.huber);
-        if (counts) dz = e.dz;
-        if (hg == 0 && lane < R && there) {
-          if (p.z) p.z[row] = z;
-          if (counts) {
-            sum += (double)e.loss;
-            total += (double)cur1;
-          }
-        }
+      for (int i = 0; i < 8; ++i) {
+        const int row = 8 * (i >> 2) + (i & 3);
+        v[i] = element<BF16>(x + (size_t)row * ld * E + off_col, 0);
+        dz[i] = z[4 * h + row];
       }
     } else {
-      if (row0 + i_row < end) dz = cur0;
-    }
-    if (works) {
-      if (hg == 0 && lane < R) d0 += dz;
-      dzbuf[wave][i_row] = dz;
-      __builtin_amdgcn_wave_barrier();
+      const int64_t base = mine < end ? mine : end - 1;
+      const int last = there < 0 ? 0 : there;
+      load8<BF16>(raw, p.x, (base + min(c, last)) * ld + (brings ? 8 * oct : 0), p.vec);
+      dzc = p.dz[base + min(c, last)];
 #pragma unroll
-      for (int t = 0; t < T; ++t) {
-        const gf32x4 d = *(const gf32x4 *)&dzbuf[wave][16 * t + 4 * q];
-        if constexpr (LOSS) {
-          // A row that does not count may hold anything: where its z is not finite,
-          // neither need be what is made of it (z is, only if all of it is).
-          bool odd = false;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) odd = odd || (d[r] == 0.0f && !(fabsf(zp[t][r]) < __builtin_inff()));
-          if (__ballot(odd)) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-              for (int b = 0; b < NB; ++b) {
-                if (d[r] == 0.0f) av[t][b][r] = gv[t][b][r] = 0.0f;
-              }
-          }
-        }
-        // the features' operand: Q0 Q2, Q1 Q1, Q0 Q0 of dz x against P2 P0, P1 P0, P1 P0
-        gu32x4 xq[KC][3];
-#pragma unroll
-        for (int k = 0; k < KC; ++k) {
-          float v[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) v[r] = d[r] != 0.0f ? d[r] * xb[t][r][k] : 0.0f;
-          uint32_t a[3], b[3];
-          split2(v[0], v[1], a[0], a[1], a[2]);
-          split2(v[2], v[3], b[0], b[1], b[2]);
-          xq[k][0] = gu32x4{a[0], b[0], a[2], b[2]};
-          xq[k][1] = gu32x4{a[1], b[1], a[1], b[1]};
-          xq[k][2] = gu32x4{a[0], b[0], a[0], b[0]};
-        }
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int m = 0; m < 2; ++m) {
-            const float(&v)[4] = m ? av[t][b] : gv[t][b];
-            uint32_t a0[3], a1[3];
-            split2(v[0], v[1], a0[0], a0[1], a0[2]);
-            split2(v[2], v[3], a1[0], a1[1], a1[2]);
-            const gu32x4 lo = {a0[2], a1[2], a0[0], a1[0]}, hi = {a0[1], a1[1], a0[0], a1[0]};
-#pragma unroll
-            for (int k = 0; k < KC; ++k) dw[m][b][k] = K::mfma(lo, xq[k][0], dw[m][b][k]);
-#pragma unroll
-            for (int k = 0; k < KC; ++k) dw[m][b][k] = K::mfma(hi, xq[k][1], dw[m][b][k]);
-#pragma unroll
-            for (int k = 0; k < KC; ++k) dw[m][b][k] = K::mfma(hi, xq[k][2], dw[m][b][k]);
-          }
+      for (int i = 0; i < 8; ++i) {
+        const int row = 8 * (i >> 2) + 4 * h + (i & 3);
+        const int64_t at = base + min(row, last);
+        v[i] = element<BF16>(p.x, at * ld + col);
+        dz[i] = row <= there ? p.dz[at] : 0.0f;
       }
-      __builtin_amdgcn_wave_barrier();
+      if (c > there) dzc = 0.0f;
     }
-  }
+    __syncthreads();   // (the step before is done with the room)
+    {
+      // (a row whose dz is 0 adds nothing, whatever it holds)
+      const bool on = dzc != 0.0f;
+      if (oct == 0) d0 += dzc;
+      if (brings) {
 #pragma unroll
-  for (int d = 1; d < R; d *= 2) d0 += __shfl_xor(d0, d);
-  if constexpr (LOSS) {
+        for (auto &r : raw) r = on ? r : gu32x4{0, 0, 0, 0};
+        gu32x4 x[NP];
+        K::pieces(raw, x);
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      sum += __shfl_xor(sum, d);
-      total += __shfl_xor(total, d);
-    }
-    __shared__ double part[W][2];
-    if (lane == 0) {
-      part[wave][0] = sum;
-      part[wave][1] = total;
+        for (int i = 0; i < NP; ++i) lx[tile][oct >> 1][i][16 * half + c + 32 * (oct & 1)] = x[i];
+      }
+      gu32x4 qp[3];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t p0, p1, p2;
+        const float a = dz[2 * i] != 0.0f ? dz[2 * i] * v[2 * i] : 0.0f;
+        const float b = dz[2 * i + 1] != 0.0f ? dz[2 * i + 1] * v[2 * i + 1] : 0.0f;
+        split2(a, b, p0, p1, p2);
+        qp[0][i] = p0, qp[1][i] = p1, qp[2][i] = p2;
+      }
+      if constexpr (IN == 32) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i) lq[tile][half][i][lane] = qp[i];
+      } else {
+        lq[tile][half][0][lane] = n < 16 ? qp[0] : qp[1];
+        lq[tile][half][1][lane] = n < 16 ? qp[2] : gu32x4{0, 0, 0, 0};
+      }
     }
     __syncthreads();
-    if (threadIdx.x < 2) {
-      double v = 0.0;
-      for (int i = 0; i < W; ++i) v += part[i][threadIdx.x];
-      p.loss_part[2 * wg + threadIdx.x] = v;
+    if (works) {
+#pragma unroll 1
+      for (int t = rg; t < kTiles; t += RG) {
+        if (row0 + 32 * t >= end) break;
+        gf32x16 g = {}, u = {};
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+          gu32x4 x[NP];
+#pragma unroll
+          for (int i = 0; i < NP; ++i) x[i] = lx[t][k][i][lane];
+          auto both = [&](int i, int j) {
+            g = K::mfma(x[i], wgt[0][k][j], g);
+            u = K::mfma(x[i], wgt[1][k][j], u);
+          };
+          if constexpr (!BF16) {
+            both(2, 0);
+            both(1, 1);
+            both(0, 2);
+            both(1, 0);
+            both(0, 1);
+          }
+          both(0, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          gu32x4 w[2][NA];   // pieces of what the unit makes of 8 rows: for dW1, dW2
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float a[2], e[2];
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+              const float gr = g[8 * j + 2 * i + o], s = sigmoid(gr);
+              a[o] = gr * s;
+              e[o] = u[8 * j + 2 * i + o] * fmaf(s, gr - a[o], s);   // u silu'(g)
+            }
+            uint32_t p0, p1, p2;
+            if constexpr (NA == 3) split2(e[0], e[1], p0, p1, p2);
+            else split2(e[0], e[1], p0, p1);
+            w[0][0][i] = p0, w[0][1][i] = p1;
+            if constexpr (NA == 3) w[0][2][i] = p2;
+            if constexpr (NA == 3) split2(a[0], a[1], p0, p1, p2);
+            else split2(a[0], a[1], p0, p1);
+            w[1][0][i] = p0, w[1][1][i] = p1;
+            if constexpr (NA == 3) w[1][2][i] = p2;
+          }
+          gu32x4 x[NQ];
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) x[i] = lq[t][j][i][lane];
+          auto add = [&](int i, int k) {
+            dw[0] = K::mfma(w[0][i], x[k], dw[0]);
+            dw[1] = K::mfma(w[1][i], x[k], dw[1]);
+          };
+          if constexpr (IN == 32) {
+            if constexpr (NA == 3) add(2, 0);
+            add(1, 1);
+            add(0, 2);
+            add(1, 0);
+            add(0, 1);
+          } else {
+            add(0, 1);
+            if constexpr (NA == 3) add(2, 0);
+            add(1, 0);
+          }
+          add(0, 0);
+        }
+      }
     }
   }
-  // the row groups' sums onto the first's, in order
-  if (works && rg > 0) {
-    float(*o)[64] = join[(rg - 1) * HG + hg];
-    int n = 0;
+  // db3, and the row groups' sums onto the first's in order (in the same room)
+  __shared__ float d0s[W];
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+  for (int d = 1; d < 64; d *= 2) d0 += __shfl_xor(d0, d);
+  if (lane == 0) d0s[wave] = d0;
+  float(*join)[16][64] = reinterpret_cast<float(*)[16][64]>(lds);
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+  for (int m = 0; m < 2; ++m) {
+    __syncthreads();
+    if (works && rg > 0) {
 #pragma unroll
-        for (int k = 0; k < KC; ++k)
+      for (int i = 0; i < 16; ++i) join[(rg - 1) * HG + hg][i][lane] = dw[m][i];
+    }
+    __syncthreads();
+    if (works && rg == 0) {
+      for (int g = 1; g < RG; ++g)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[n++][lane] = dw[m][b][k][i];
-    o[n][lane] = d0;
+        for (int i = 0; i < 16; ++i) dw[m][i] += join[(g - 1) * HG + hg][i][lane];
+    }
   }
-  __syncthreads();
   if (!works || rg > 0) return;
-  for (int g = 1; g < RG; ++g) {
-    const float(*o)[64] = join[(g - 1) * HG + hg];
-    int n = 0;
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int k = 0; k < KC; ++k)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) dw[m][b][k][i] += o[n++][lane];
-    d0 += o[n][lane];
-  }
   float *out = p.part + (size_t)wg * gated_part_size(p.hidden, IN);
+  float *own = out + hg * kGatedGroup * 2 * IN;
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int unit0 = hg * K::kGroup + 16 * b;
-    float *mine = out + (unit0 / kGatedGroup) * kGatedGroup * 2 * IN;
+  for (int m = 0; m < 2; ++m)
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int k = 0; k < KC; ++k)
-          mine[(m * kGatedGroup + unit0 % kGatedGroup + 4 * q + i) * IN + 16 * k + c] = dw[m][b][k][i];
+    for (int i = 0; i < 16; ++i) {
+      float v = dw[m][i];
+      if constexpr (IN == 16) v += __shfl_xor(v, 16);   // the features' second half of the columns
+      if (n < IN) own[(m * kGatedGroup + 8 * (i >> 2) + 4 * h + (i & 3)) * IN + n] = v;
+    }
+  if (hg == 0 && lane == 0) {
+    float v = 0.0f;
+    for (int i = 0; i < W; ++i) v += d0s[i];
+    out[gated_part_size(p.hidden, IN) - 1] = v;
   }
-  if (hg == 0 && lane == 0) out[gated_part_size(p.hidden, IN) - 1] = d0;
 }
 
 // ------------------------------------------------------------ rows' gradients
@@ -705,8 +549,7 @@ __global__ __launch_bounds__(kThreads) void k_gated_reduce(GatedParams p, int ch
   if (p.eta) {
     __shared__ double ls[kThreads][2];
     double a = 0.0, b = 0.0;
-    const int32_t *wgs = p.g_w1 ? p.bwd_wg : p.fwd_wg;   // of the kernel that summed the loss
-    for (int w = wgs[f] + (int)threadIdx.x; w < wgs[f + 1]; w += kThreads) {
+    for (int w = p.fwd_wg[f] + (int)threadIdx.x; w < p.fwd_wg[f + 1]; w += kThreads) {
       a += p.loss_part[2 * w];
       b += p.loss_part[2 * w + 1];
     }
@@ -789,20 +632,16 @@ hipError_t launch_gated_forward(const GatedParams &p, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <bool BF16, int IN, bool LOSS>
-static void fit_kind(const GatedParams &p, hipStream_t s) {
-  hipLaunchKernelGGL((k_gated_fit<BF16, IN, LOSS>), dim3(p.bwd_wg[KS_NFAM]), dim3(64 * Back<BF16, IN>::W), 0, s, p);
-}
-template <bool LOSS>
-static void fit_of(const GatedParams &p, hipStream_t s) {
-  if (p.bf16) p.in_dim == 16 ? fit_kind<true, 16, LOSS>(p, s) : fit_kind<true, 32, LOSS>(p, s);
-  else p.in_dim == 16 ? fit_kind<false, 16, LOSS>(p, s) : fit_kind<false, 32, LOSS>(p, s);
-}
-
-hipError_t launch_gated_fit(const GatedParams &p, hipStream_t s) {
-  if (p.bwd_wg[KS_NFAM] == 0) return hipSuccess;
-  if (p.eta) fit_of<true>(p, s);
-  else fit_of<false>(p, s);
+hipError_t launch_gated_sums(const GatedParams &p, hipStream_t s) {
+  const dim3 grid(p.bwd_wg[KS_NFAM]), block(512);
+  if (grid.x == 0) return hipSuccess;
+  if (p.bf16) {
+    if (p.in_dim == 16) hipLaunchKernelGGL((k_gated_sums<true, 16>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((k_gated_sums<true, 32>), grid, block, 0, s, p);
+  } else {
+    if (p.in_dim == 16) hipLaunchKernelGGL((k_gated_sums<false, 16>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((k_gated_sums<false, 32>), grid, block, 0, s, p);
+  }
   return hipGetLastError();
 }
 

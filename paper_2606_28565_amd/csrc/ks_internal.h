@@ -290,7 +290,7 @@ hipError_t launch_validate(const ValidateParams &p, hipStream_t s);
 
 // ---- gated heads over rows (ks_gated.hip)
 // A forward workgroup takes fwd_tiles 64-row tiles of one family, a backward
-// workgroup bwd_rows rows of one (a multiple of gated_rows()).
+// workgroup bwd_rows rows of one (a multiple of kGatedStep).
 struct GatedParams {
   const void *x;
   int64_t ldx;
@@ -305,7 +305,8 @@ struct GatedParams {
   // the loss (eta null: none)
   const float *eta, *weight;
   float huber;
-  double *loss_part;                 // [workgroups of the kernel that forms it][2]: sum w rho, sum w
+  float *dz_out;                     // w drho/dz, not yet over sum w; null: the loss alone
+  double *loss_part;                 // [forward workgroups][2]: sum w rho, sum w
   float *loss;                       // [KS_NFAM]
   // gradients
   const float *dz;
@@ -315,20 +316,14 @@ struct GatedParams {
   int64_t g_ldx;
   bool g_vec;
 };
-constexpr int gated_groups(int hidden, int group) { return (hidden + group - 1) / group; }
-// k_gated_fit's unit groups and waves by kind, and the rows its workgroup takes at a
-// time (row groups x rows in hand)
-constexpr int gated_rows(bool bf16, int in_dim, int hidden) {
-  const bool wide = !bf16 && in_dim == 32;
-  return (wide ? 16 : 32) * ((wide ? 8 : 4) / gated_groups(hidden, wide ? 32 : 64));
-}
-// floats of its sums: dW1 and dW2 by groups of 64 units (the last one whole); db3
-constexpr int kGatedGroup = 64;
+// k_gated_sums: rows a workgroup takes at a time, units per wave; floats of its sums:
+// by groups of 32 units dW1 and dW2 (the last group whole), then db3
+constexpr int kGatedStep = 128, kGatedGroup = 32;
 constexpr int gated_part_size(int hidden, int in_dim) {
-  return gated_groups(hidden, kGatedGroup) * kGatedGroup * 2 * in_dim + 1;
+  return (hidden + kGatedGroup - 1) / kGatedGroup * kGatedGroup * 2 * in_dim + 1;
 }
 hipError_t launch_gated_forward(const GatedParams &p, hipStream_t s);
-hipError_t launch_gated_fit(const GatedParams &p, hipStream_t s);      // sums of a given dz, or of the loss
+hipError_t launch_gated_sums(const GatedParams &p, hipStream_t s);
 hipError_t launch_gated_rows(const GatedParams &p, hipStream_t s);     // g_x
 hipError_t launch_gated_reduce(const GatedParams &p, hipStream_t s);   // gradients and the loss
 

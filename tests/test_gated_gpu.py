@@ -150,6 +150,12 @@ def backward(d, off, dz, dx=True, ldg=None, repeat=1):
     return r
 
 
+def bits(prec):
+    """bf16 heads sum what a unit makes of a row to 2^-18 of it, fp32 heads unrounded
+    (three exact pieces; the products left out are below 2^-25)."""
+    return 18 if prec == "bf16" else 25
+
+
 def check_grads(h, off, dz, got, prec, dx=True):
     with np.errstate(invalid="ignore"):
         for f in range(NFAM):
@@ -159,7 +165,7 @@ def check_grads(h, off, dz, got, prec, dx=True):
                     assert (got[k][f] == 0).all(), (k, f)
                 continue
             _, k = o.block(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], h["b3"][f])
-            want, err = o.gradients(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], dz[r], k, 16 + len(dz) // 128)
+            want, err = o.gradients(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], dz[r], k, 16 + len(dz) // 128, bits(prec))
             for key in ("w1", "w2", "w3", "b3"):
                 off_by = np.abs(got[key][f] - want[key])
                 assert (off_by <= err[key]).all(), (key, f, np.max(off_by / np.maximum(err[key], 1e-300)))
@@ -266,7 +272,7 @@ def run_loss(d, off, eta, weight, huber, grad=True, with_z=True):
     return loss.double().cpu().numpy(), z.double().cpu().numpy(), {k: v.double().cpu().numpy() for k, v in out.items()}
 
 
-def check_loss(h, off, eta, weight, huber, got, grad=True):
+def check_loss(h, off, eta, weight, huber, got, grad=True, prec="f32"):
     """dz's own error: log(1 + e^-z) and log eta are within 4 steps of their sizes
     and carry z's error (slope <= 1), sigma(-z) likewise (slope <= 1/4)."""
     loss, z, grads = got
@@ -299,7 +305,7 @@ def check_loss(h, off, eta, weight, huber, got, grad=True):
             continue
         sg = o.sigmoid(-zo)
         edz = share * (er * (sg + ez / 4) + slope * (ez / 4 + 8 * o.EPS * sg)) + 8 * o.EPS * np.abs(dz)
-        val, err = o.gradients(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], dz, k, 16 + len(eta) // 128)
+        val, err = o.gradients(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], dz, k, 16 + len(eta) // 128, bits(prec))
         # what an error of dz makes of the sums: their derivative by dz
         x = np.where(on[:, None], h["x"][r], 0.0)
         t = np.abs(k["s"] + k["a"] * (1 - k["s"])) * np.abs(k["u"]) * np.abs(h["w3"][f])
@@ -326,7 +332,7 @@ def targets(n, seed=9):
 def test_loss_widths(prec, inp, hid, huber):
     d, h, off = make(700, prec, inp, hid)
     eta, weight = targets(700)
-    check_loss(h, off, eta, weight, huber, run_loss(d, off, eta.cuda(), weight.cuda(), huber))
+    check_loss(h, off, eta, weight, huber, run_loss(d, off, eta.cuda(), weight.cuda(), huber), prec=prec)
 
 
 @pytest.mark.parametrize("n", [0, 1, 16, 65, 3000])
@@ -355,7 +361,7 @@ def test_rows_that_do_not_count(prec, hid):
     got = run_loss(d, off, eta.cuda(), weight.cuda(), 0.5)
     assert np.isfinite(got[0]).all() and all(np.isfinite(v).all() for v in got[2].values())
     assert got[0][3] == 0 and (got[2]["w1"][3] == 0).all()
-    check_loss(h, off, eta, weight, 0.5, got)
+    check_loss(h, off, eta, weight, 0.5, got, prec=prec)
 
 
 def test_loss_alone_is_the_same_loss():
