@@ -533,7 +533,7 @@ ks_status ks_features(const ks_desc *desc, const ks_spec *specs, int32_t n_specs
  * unrounded m and v.  All-zero states are those before the first step.
  */
 typedef struct ks_tensor {
-  int64_t n;                       /* elements, 0 .. 2^35                    */
+  int64_t n;                       /* elements, 0 .. 2^33                    */
   float *param;                    /* device [n], updated                    */
   const void *grad;                /* device [n] of grad_type                */
   void *m, *v;                     /* device [n], updated                    */
@@ -556,7 +556,7 @@ typedef struct ks_adamw_config {
 } ks_adamw_config;
 
 /* tensors: HOST array of n_tensors (read during the call); no two may share a
- * param.  Launches: one for every 48 tensors, one more with step_dev. */
+ * param.  Launches: one for every 200 tensors, one more with step_dev. */
 ks_status ks_adamw(const ks_adamw_config *config, const ks_tensor *tensors, int32_t n_tensors, hipStream_t stream);
 
 /* Synchronous device-side check of the inputs: step order within families,

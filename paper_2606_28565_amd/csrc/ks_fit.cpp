@@ -261,7 +261,7 @@ ks_status ks_adamw(const ks_adamw_config *c, const ks_tensor *tensors, int32_t n
   const bool eight = c->state_bits == 8;
   for (int i = 0; i < n_tensors; ++i) {
     const ks_tensor &t = tensors[i];
-    if (t.n < 0 || t.n > (int64_t(1) << 35)) return set_error(KS_ERANGE, "tensor %d: n %lld outside 0..2^35", i, (long long)t.n);
+    if (t.n < 0 || t.n > (int64_t(1) << 33)) return set_error(KS_ERANGE, "tensor %d: n %lld outside 0..2^33", i, (long long)t.n);
     if (t.grad_type != KS_F32 && t.grad_type != KS_BF16) return set_error(KS_EINVAL, "tensor %d: grad_type %d unknown", i, t.grad_type);
     if (!std::isfinite(t.weight_decay)) return set_error(KS_EINVAL, "tensor %d: weight_decay not finite", i);
     if (t.n == 0) continue;

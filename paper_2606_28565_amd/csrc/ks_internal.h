@@ -328,8 +328,8 @@ hipError_t launch_gated_rows(const GatedParams &p, hipStream_t s);     // g_x
 hipError_t launch_gated_reduce(const GatedParams &p, hipStream_t s);   // gradients and the loss
 
 // ---- AdamW (ks_adamw.hip)
-constexpr int kAdamTensors = 48;     // per launch: their table travels in the kernel arguments
-constexpr int kAdamChunk = 4096;     // elements per workgroup
+constexpr int kAdamTensors = 200;     // per launch: their table travels in the kernel arguments
+constexpr int kAdamChunk = 1024;     // elements per workgroup
 struct AdamTensor {
   float *p;
   const void *g;
@@ -350,7 +350,7 @@ struct AdamParams {
   float log_b1, log_b2;              // for a step counted on the device
   const uint32_t *step_dev;
 };
-static_assert(sizeof(AdamParams) <= 4096, "the table fits the kernel arguments");
+static_assert(sizeof(AdamParams) <= 16384, "the table fits the kernel arguments");
 hipError_t launch_adamw(const AdamParams &p, bool eight, hipStream_t s);
 hipError_t launch_adamw_count(uint32_t *step_dev, hipStream_t s);
 

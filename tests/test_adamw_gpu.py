@@ -99,7 +99,7 @@ def test_sizes(bits, grad16, shift):
 @pytest.mark.parametrize("bits", [32, 8])
 def test_many_tensors(bits):
     """More tensors than one launch takes, empty ones among them, no copies."""
-    sizes = [(7 * i) % 150 for i in range(130)]
+    sizes = [(7 * i) % 150 for i in range(430)]
     host, dev = make(sizes, bits, copy=False)
     run(dev, bits)
     check(host, dev, bits, 3)
