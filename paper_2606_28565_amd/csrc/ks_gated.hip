@@ -109,28 +109,34 @@ __global__ __launch_bounds__(64 * N, 2) void k_gated_forward(GatedParams p) {
   constexpr int E = BF16 ? 2 : 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wg = blockIdx.x, f = family_of(p.fwd_wg, wg);
-  const size_t w = (size_t)f * p.hidden * IN * E;
-  G::stage(lds, (const char *)p.w1 + w, (const char *)p.w2 + w, (const char *)p.w3 + (size_t)f * p.hidden * E,
-           (const char *)p.b3 + f * E, p.hidden, (int)threadIdx.x, 64 * N);
-  __syncthreads();
   const int64_t begin = p.fam_off[f] + (int64_t)(wg - p.fwd_wg[f]) * p.fwd_tiles * 64;
   const int64_t fam_end = p.fam_off[f + 1];
   const int64_t end = begin + (int64_t)p.fwd_tiles * 64 < fam_end ? begin + (int64_t)p.fwd_tiles * 64 : fam_end;
-  double sum = 0.0, total = 0.0;
-  for (int64_t row0 = begin + 64 * wave; row0 < end; row0 += 64 * N) {
-    typename G::Rows x;
+  gu32x4 raw[2][G::KC][BF16 ? 1 : 2];
+  auto fetch = [&](int64_t row0) {   // past the last row a lane reads the last
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int64_t r = row0 + 32 * i + (lane & 31);
       const int64_t at = (r < end ? r : end - 1) * p.ldx + (lane >> 5) * 8;
 #pragma unroll
-      for (int kc = 0; kc < G::KC; ++kc) {
-        gu32x4 raw[BF16 ? 1 : 2];
-        load8<BF16>(raw, p.x, at + 16 * kc, p.vec);
-        if constexpr (BF16) x.v[i][kc][0] = raw[0];
-        else G::split8(__builtin_bit_cast(gf32x4, raw[0]), __builtin_bit_cast(gf32x4, raw[1]), x.v[i][kc]);
-      }
+      for (int kc = 0; kc < G::KC; ++kc) load8<BF16>(raw[i][kc], p.x, at + 16 * kc, p.vec);
     }
+  };
+  fetch(begin + 64 * wave);   // (with the weights on their way too)
+  const size_t w = (size_t)f * p.hidden * IN * E;
+  G::stage(lds, (const char *)p.w1 + w, (const char *)p.w2 + w, (const char *)p.w3 + (size_t)f * p.hidden * E,
+           (const char *)p.b3 + f * E, p.hidden, (int)threadIdx.x, 64 * N);
+  __syncthreads();
+  double sum = 0.0, total = 0.0;
+  for (int64_t row0 = begin + 64 * wave; row0 < end; row0 += 64 * N) {
+    typename G::Rows x;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int kc = 0; kc < G::KC; ++kc) {
+        if constexpr (BF16) x.v[i][kc][0] = raw[i][kc][0];
+        else G::split8(__builtin_bit_cast(gf32x4, raw[i][kc][0]), __builtin_bit_cast(gf32x4, raw[i][kc][1]), x.v[i][kc]);
+      }
     const float z = G::z_of(x, lds);
     const int64_t row = row0 + lane;
     if (row < end) {
@@ -146,6 +152,7 @@ __global__ __launch_bounds__(64 * N, 2) void k_gated_forward(GatedParams p) {
         if (p.dz_out) p.dz_out[row] = counts ? e.dz : 0.0f;
       }
     }
+    fetch(row0 + 64 * N);
   }
   if constexpr (LOSS) {
     __shared__ double part[N][2];
@@ -218,6 +225,7 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
   constexpr int kTiles = R / 32;
   constexpr int kX = kTiles * KC * NP * 64 * 4, kQ = kTiles * 2 * NQ * 64 * 4, kJoin = (W - 1) * 16 * 64;
   __shared__ __align__(16) uint32_t lds[kX + kQ > kJoin ? kX + kQ : kJoin];
+  __shared__ __align__(16) float dzs[W][16];
   gu32x4(*lx)[KC][NP][64] = reinterpret_cast<gu32x4(*)[KC][NP][64]>(lds);          // [tile]: rows
   gu32x4(*lq)[2][NQ][64] = reinterpret_cast<gu32x4(*)[2][NQ][64]>(lds + kX);       // [tile][16 rows]: dz x
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, c = lane & 15;
@@ -256,42 +264,40 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
   const int col = IN == 32 ? n : c;                // ... and the feature of its rows
   constexpr int E = BF16 ? 2 : 4;
   const uint32_t off_row = __umul24(c, ld * E) + (brings ? 8 * E * oct : 0), off_col = __umul24(4 * h, ld * E) + col * E;
-#pragma unroll 1
-  for (int64_t row0 = begin; row0 < end; row0 += R) {
-    const int64_t mine = row0 + 16 * wave;
-    const int there = end - mine < 16 ? (int)(end - mine) - 1 : 15;   // the last of the wave's rows; below 0: none
-    gu32x4 raw[BF16 ? 1 : 2];
-    float v[8], dz[8], dzc;
-    if (there == 15) {
+  gu32x4 raw[BF16 ? 1 : 2];
+  float v[8], dzc;
+  auto fetch = [&](int64_t mine) {
+    if (mine + 16 <= end) {
       const char *x = (const char *)p.x + mine * ld * E;
-      const float *z = p.dz + mine;
       load8<BF16>(raw, x + off_row, 0, p.vec);
-      dzc = z[c];
+      dzc = p.dz[mine + c];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int row = 8 * (i >> 2) + (i & 3);
-        v[i] = element<BF16>(x + (size_t)row * ld * E + off_col, 0);
-        dz[i] = z[4 * h + row];
-      }
-    } else {
+      for (int i = 0; i < 8; ++i) v[i] = element<BF16>(x + (size_t)(8 * (i >> 2) + (i & 3)) * ld * E + off_col, 0);
+    } else {   // past the last row a lane reads the last
       const int64_t base = mine < end ? mine : end - 1;
-      const int last = there < 0 ? 0 : there;
+      const int last = (int)(end - base) - 1;
       load8<BF16>(raw, p.x, (base + min(c, last)) * ld + (brings ? 8 * oct : 0), p.vec);
       dzc = p.dz[base + min(c, last)];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int row = 8 * (i >> 2) + 4 * h + (i & 3);
-        const int64_t at = base + min(row, last);
-        v[i] = element<BF16>(p.x, at * ld + col);
-        dz[i] = row <= there ? p.dz[at] : 0.0f;
-      }
-      if (c > there) dzc = 0.0f;
+      for (int i = 0; i < 8; ++i)
+        v[i] = element<BF16>(p.x, (base + min(8 * (i >> 2) + 4 * h + (i & 3), last)) * ld + col);
+      if (mine + c >= end) dzc = 0.0f;
     }
+  };
+  // (bf16: a step's rows are on their way while the step before is worked on; fp32
+  // has no registers left for them)
+  if (BF16) fetch(begin + 16 * wave);
+#pragma unroll 1
+  for (int64_t row0 = begin; row0 < end; row0 += R) {
+    if (!BF16) fetch(row0 + 16 * wave);
     __syncthreads();   // (the step before is done with the room)
     {
       // (a row whose dz is 0 adds nothing, whatever it holds)
       const bool on = dzc != 0.0f;
-      if (oct == 0) d0 += dzc;
+      if (oct == 0) {
+        d0 += dzc;
+        dzs[wave][c] = dzc;
+      }
       if (brings) {
 #pragma unroll
         for (auto &r : raw) r = on ? r : gu32x4{0, 0, 0, 0};
@@ -300,14 +306,19 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
 #pragma unroll
         for (int i = 0; i < NP; ++i) lx[tile][oct >> 1][i][16 * half + c + 32 * (oct & 1)] = x[i];
       }
+      __builtin_amdgcn_wave_barrier();
       gu32x4 qp[3];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t p0, p1, p2;
-        const float a = dz[2 * i] != 0.0f ? dz[2 * i] * v[2 * i] : 0.0f;
-        const float b = dz[2 * i + 1] != 0.0f ? dz[2 * i + 1] * v[2 * i + 1] : 0.0f;
-        split2(a, b, p0, p1, p2);
-        qp[0][i] = p0, qp[1][i] = p1, qp[2][i] = p2;
+      for (int j = 0; j < 2; ++j) {
+        const gf32x4 dz = *(const gf32x4 *)&dzs[wave][8 * j + 4 * h];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t p0, p1, p2;
+          const float a = dz[2 * i] != 0.0f ? dz[2 * i] * v[4 * j + 2 * i] : 0.0f;
+          const float b = dz[2 * i + 1] != 0.0f ? dz[2 * i + 1] * v[4 * j + 2 * i + 1] : 0.0f;
+          split2(a, b, p0, p1, p2);
+          qp[0][2 * j + i] = p0, qp[1][2 * j + i] = p1, qp[2][2 * j + i] = p2;
+        }
       }
       if constexpr (IN == 32) {
 #pragma unroll
@@ -318,6 +329,7 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
       }
     }
     __syncthreads();
+    if (BF16) fetch(row0 + R + 16 * wave);
     if (works) {
 #pragma unroll 1
       for (int t = rg; t < kTiles; t += RG) {
@@ -545,6 +557,29 @@ template <bool BF16>
 __global__ __launch_bounds__(kThreads) void k_gated_reduce(GatedParams p, int chunks) {
   const int f = blockIdx.x / chunks, ch = blockIdx.x % chunks;
   const int IN = p.in_dim, H = p.hidden, HI = H * IN;
+  __shared__ double part[kRedParts][kRedEl];
+  const int el = threadIdx.x % kRedEl, sl = threadIdx.x / kRedEl;
+  const int e = ch * kRedEl + el;
+  const int size = gated_part_size(H, IN);
+  // where the element stands in a workgroup's sums
+  int at = -1, unit = -1;
+  if (e < 2 * HI) {
+    const int m = e >= HI, i = m ? e - HI : e;
+    unit = i / IN;
+    at = (unit / kGatedGroup) * kGatedGroup * 2 * IN + (m * kGatedGroup + unit % kGatedGroup) * IN + i % IN;
+  } else if (e == 2 * HI) {
+    at = size - 1;
+  }
+  const int first = p.bwd_wg[f], n = p.bwd_wg[f + 1] - first;
+  const int per = (n + kRedParts - 1) / kRedParts;
+  double v = 0.0;
+  if (p.g_w1 && at >= 0) {
+    const int lo = sl * per, hi = min(lo + per, n);
+    const float *src = p.part + (size_t)first * size + at;
+#pragma unroll 8
+    for (int i = lo; i < hi; ++i) v += (double)src[(size_t)i * size];
+  }
+  // (the loss's sums after the loads above are on their way)
   double scale = 1.0;
   if (p.eta) {
     __shared__ double ls[kThreads][2];
@@ -568,28 +603,6 @@ __global__ __launch_bounds__(kThreads) void k_gated_reduce(GatedParams p, int ch
     if (ch == 0 && threadIdx.x == 0) p.loss[f] = total > 0.0 ? (float)(ls[0][0] * scale) : 0.0f;
   }
   if (!p.g_w1) return;
-  __shared__ double part[kRedParts][kRedEl];
-  const int el = threadIdx.x % kRedEl, sl = threadIdx.x / kRedEl;
-  const int e = ch * kRedEl + el;
-  const int size = gated_part_size(H, IN);
-  // where the element stands in a workgroup's sums
-  int at = -1, unit = -1;
-  if (e < 2 * HI) {
-    const int m = e >= HI, i = m ? e - HI : e;
-    unit = i / IN;
-    at = (unit / kGatedGroup) * kGatedGroup * 2 * IN + (m * kGatedGroup + unit % kGatedGroup) * IN + i % IN;
-  } else if (e == 2 * HI) {
-    at = size - 1;
-  }
-  const int first = p.bwd_wg[f], n = p.bwd_wg[f + 1] - first;
-  const int per = (n + kRedParts - 1) / kRedParts;
-  double v = 0.0;
-  if (at >= 0) {
-    const int lo = sl * per, hi = min(lo + per, n);
-    const float *src = p.part + (size_t)first * size + at;
-#pragma unroll 8
-    for (int i = lo; i < hi; ++i) v += (double)src[(size_t)i * size];
-  }
   part[sl][el] = v;
   __syncthreads();
   if (sl > 0) return;   // (the first half of the first wave is left)
