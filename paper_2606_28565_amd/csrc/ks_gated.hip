@@ -46,8 +46,9 @@ __device__ __forceinline__ float element(const void *p, int64_t i) {
 }
 
 __device__ __forceinline__ int family_of(const int32_t (&off)[KS_NFAM + 1], int wg) {
-  int f = 0;
-  while (wg >= off[f + 1]) ++f;
+  int f = 0;   // (all offsets read at once: no chain of scalar loads)
+#pragma unroll
+  for (int i = 1; i < KS_NFAM; ++i) f += wg >= off[i];
   return f;
 }
 
@@ -438,99 +439,167 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
 
 // ------------------------------------------------------------ rows' gradients
 // dx = W1^T dg + W2^T du: units are summed over, so here the units are the row
-// operand of the projections (a lane holds four units of one row) and what it
-// makes of them is the column operand of the next product.  fp32 throughout,
-// from fp32 copies of the weights in LDS; rows of IN + 4 floats keep both the
-// 16-byte reads along a row and the reads across rows off each other's banks.
+// operand of the projections, as in k_gated_forward (a lane holds 16 units of one row),
+// and what it makes of them is the column operand of the next product, features x rows,
+// whose row operand is the weights transposed: eight units of a feature per lane, in
+// the order in which a lane has them.  Both forms of 128 units' weights are in LDS;
+// wider heads take them in two parts for 512 rows at a time.  With 16 inputs the
+// instruction's 32 rows are the features twice, against the first and the second piece
+// of an fp32 weight (then the third and nothing).
+//
+// (100,003 rows of fp32 32-67 on the fp32 instruction: 32 us; so KROWS us.)
 template <bool BF16, int IN>
-__global__ __launch_bounds__(kThreads, 2) void k_gated_rows(GatedParams p) {
-  constexpr int KC = IN / 16, LD = IN + 4, RT = 2, H = gated::kMaxHidden;
-  __shared__ __align__(16) float lw[2][H][LD];
-  __shared__ __align__(16) float l3[H];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4, c = lane & 15;
+__global__ __launch_bounds__(512, 2) void k_gated_rows(GatedParams p) {
+  constexpr int HID = 128, E = BF16 ? 2 : 4, W = 8, T = 2;
+  using G = Block<BF16, IN, HID>;
+  constexpr int KC = G::KC, NP = G::NP, NT = IN == 32 ? NP : BF16 ? 1 : 2;   // operands of the weights transposed
+  __shared__ __align__(16) uint32_t lds[G::kLds];
+  __shared__ __align__(16) gu32x4 lt[HID / 32][2][2][NT][64];   // [32 units][W1, W2][16 units]
+  const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wg = blockIdx.x, f = family_of(p.fwd_wg, wg);
-  const int nb = (p.hidden + 15) / 16;
-  for (int i = threadIdx.x; i < nb * 16 * IN; i += kThreads) {
-    const int h = i / IN, d = i % IN;
-    const int64_t at = ((int64_t)f * p.hidden + h) * IN + d;
-    lw[0][h][d] = h < p.hidden ? element<BF16>(p.w1, at) : 0.0f;
-    lw[1][h][d] = h < p.hidden ? element<BF16>(p.w2, at) : 0.0f;
-  }
-  for (int h = threadIdx.x; h < nb * 16; h += kThreads)
-    l3[h] = h < p.hidden ? element<BF16>(p.w3, (int64_t)f * p.hidden + h) : 0.0f;
-  __syncthreads();
   const int64_t begin = p.fam_off[f] + (int64_t)(wg - p.fwd_wg[f]) * p.fwd_tiles * 64;
   const int64_t fam_end = p.fam_off[f + 1];
   const int64_t end = begin + (int64_t)p.fwd_tiles * 64 < fam_end ? begin + (int64_t)p.fwd_tiles * 64 : fam_end;
-  for (int64_t row0 = begin + 16 * RT * wave; row0 < end; row0 += 16 * RT * (kThreads / 64)) {
-    float x[RT][KC][4], dz[RT];
-    gf32x4 acc[RT][KC] = {};
+  const int parts = (p.hidden + HID - 1) / HID;
+  for (int64_t row0 = begin; row0 < end; row0 += 32 * T * W) {
+    gf32x16 acc[T] = {};
+    for (int part = 0; part < parts; ++part) {
+      const int hid = min(p.hidden - part * HID, HID), nb = (hid + 31) / 32;
+      if (parts > 1 || row0 == begin) {
+        if (part > 0 || row0 > begin) __syncthreads();
+        const int64_t unit0 = (int64_t)f * p.hidden + part * HID;
+        const char *w1 = (const char *)p.w1 + unit0 * IN * E, *w2 = (const char *)p.w2 + unit0 * IN * E;
+        G::stage(lds, w1, w2, (const char *)p.w3 + unit0 * E, (const char *)p.b3 + f * E, hid, (int)threadIdx.x, 64 * W);
+        for (int i = threadIdx.x; i < nb * 4 * 64; i += 64 * W) {
+          const int l = i & 63, j = (i >> 6) & 1, m = (i >> 7) & 1, blk = i >> 8;
+          const int feature = l & (IN - 1);
+          float v[8];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const int64_t r = row0 + 16 * t + c, at = r < end ? r : end - 1;
-      dz[t] = r < end ? p.dz[at] : 0.0f;
-#pragma unroll
-      for (int k = 0; k < KC; ++k)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float v = element<BF16>(p.x, at * p.ldx + 16 * k + 4 * q + j);
-          x[t][k][j] = dz[t] != 0.0f ? v : 0.0f;
-        }
-    }
-#pragma unroll 1
-    for (int b = 0; b < nb; ++b) {
-      gf32x4 g[RT] = {}, u[RT] = {};
-#pragma unroll
-      for (int k = 0; k < KC; ++k) {
-        const gf32x4 wa = *(const gf32x4 *)&lw[0][16 * b + c][16 * k + 4 * q];
-        const gf32x4 wb = *(const gf32x4 *)&lw[1][16 * b + c][16 * k + 4 * q];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            g[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(wa[j], x[t][k][j], g[t], 0, 0, 0);
-            u[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(wb[j], x[t][k][j], u[t], 0, 0, 0);
+          for (int u = 0; u < 8; ++u) {
+            const int unit = 32 * blk + 16 * j + 8 * (u >> 2) + 4 * (l >> 5) + (u & 3);
+            v[u] = element<BF16>(m ? w2 : w1, (int64_t)(unit < hid ? unit : 0) * IN + feature);
+            if (unit >= hid) v[u] = 0.0f;
           }
-      }
-      const gf32x4 w3 = *(const gf32x4 *)&l3[16 * b + 4 * q];
+          gu32x4 q[3];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float wa[KC], wb[KC];
+          for (int u = 0; u < 4; ++u) {
+            uint32_t p0, p1, p2;
+            split2(v[2 * u], v[2 * u + 1], p0, p1, p2);
+            q[0][u] = p0, q[1][u] = p1, q[2][u] = p2;
+          }
+          const gu32x4 none = {0, 0, 0, 0};
+          const bool second = IN == 16 && (l & 16);
+          if constexpr (IN == 32) {
+#pragma unroll
+            for (int u = 0; u < NT; ++u) lt[blk][m][j][u][l] = q[u];
+          } else {
+            lt[blk][m][j][0][l] = !second ? q[0] : BF16 ? none : q[1];
+            if constexpr (NT == 2) lt[blk][m][j][1][l] = !second ? q[2] : none;
+          }
+        }
+        __syncthreads();
+      }
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        const int64_t r0 = row0 + 32 * (W * t + wave);
+        if (r0 >= end) break;
+        const int64_t row = r0 + n, at = row < end ? row : end - 1;
+        const float dz = row < end ? p.dz[at] : 0.0f;
+        gu32x4 x[KC][NP];
 #pragma unroll
         for (int k = 0; k < KC; ++k) {
-          wa[k] = lw[0][16 * b + 4 * q + r][16 * k + c];
-          wb[k] = lw[1][16 * b + 4 * q + r][16 * k + c];
-        }
+          gu32x4 raw[BF16 ? 1 : 2];
+          load8<BF16>(raw, p.x, at * p.ldx + 16 * k + 8 * h, p.vec);
+          // (a row whose dz is 0 gets zeros, whatever it holds)
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-          const float dy = dz[t] * w3[r];
-          const float s = sigmoid(g[t][r]), a = g[t][r] * s;
-          const float du = dy * a, dg = dy * u[t][r] * (fmaf(-a, s, a) + s);
+          for (auto &r : raw) r = dz != 0.0f ? r : gu32x4{0, 0, 0, 0};
+          Back<BF16, IN>::pieces(raw, x[k]);
+        }
+#pragma unroll 1
+        for (int blk = 0; blk < nb; ++blk) {
+          const uint32_t *w = lds + blk * G::kBlk;
+          gf32x16 g = {}, u = {};
 #pragma unroll
           for (int k = 0; k < KC; ++k) {
-            acc[t][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(wa[k], dg, acc[t][k], 0, 0, 0);
-            acc[t][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(wb[k], du, acc[t][k], 0, 0, 0);
+            auto both = [&](int i, int j) {
+              g = Back<BF16, IN>::mfma(*(const gu32x4 *)(w + k * G::kFrag + 256 * i + 4 * lane), x[k][j], g);
+              u = Back<BF16, IN>::mfma(*(const gu32x4 *)(w + (KC + k) * G::kFrag + 256 * i + 4 * lane), x[k][j], u);
+            };
+            if constexpr (!BF16) {
+              both(2, 0);
+              both(1, 1);
+              both(0, 2);
+              both(1, 0);
+              both(0, 1);
+            }
+            both(0, 0);
+          }
+          const float *w3 = (const float *)w + 2 * KC * G::kFrag + 16 * h;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            gu32x4 d[2][3];   // dg and du of 16 units in pieces (bf16: two, as in k_gated_sums)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float a[2], e[2];
+#pragma unroll
+              for (int o = 0; o < 2; ++o) {
+                const int r = 8 * j + 2 * i + o;
+                const float dy = dz * w3[r], gr = g[r], s = sigmoid(gr), si = gr * s;
+                a[o] = dy * si;
+                e[o] = dy * u[r] * fmaf(s, gr - si, s);
+              }
+              uint32_t p0, p1, p2 = 0;
+              if constexpr (BF16) split2(e[0], e[1], p0, p1);
+              else split2(e[0], e[1], p0, p1, p2);
+              d[0][0][i] = p0, d[0][1][i] = p1, d[0][2][i] = p2;
+              if constexpr (BF16) split2(a[0], a[1], p0, p1);
+              else split2(a[0], a[1], p0, p1, p2);
+              d[1][0][i] = p0, d[1][1][i] = p1, d[1][2][i] = p2;
+            }
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+              auto add = [&](int i, int k) { acc[t] = Back<BF16, IN>::mfma(lt[blk][m][j][i][lane], d[m][k], acc[t]); };
+              if constexpr (BF16) {
+                add(0, 1);
+              } else if constexpr (IN == 32) {
+                add(2, 0);
+                add(1, 1);
+                add(0, 2);
+                add(1, 0);
+                add(0, 1);
+              } else {
+                add(1, 0);
+                add(0, 2);
+                add(0, 1);
+              }
+              add(0, 0);
+            }
           }
         }
       }
     }
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const int64_t r = row0 + 16 * t + c;
-      if (r >= end) continue;
+    for (int t = 0; t < T; ++t) {
+      const int64_t row = row0 + 32 * (W * t + wave) + n;
+      if (row >= end) continue;
+      const bool on = p.dz[row] != 0.0f;   // (zeros even where a weight is not finite)
 #pragma unroll
-      for (int k = 0; k < KC; ++k) {
-        // (a row without weight gets zeros even where a weight is not finite)
-        gf32x4 v = acc[t][k];
-        if (dz[t] == 0.0f) v = gf32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        const int64_t at = r * p.g_ldx + 16 * k + 4 * q;
+      for (int i = 0; i < IN / 8; ++i) {
+        gf32x4 v;
+#pragma unroll
+        for (int o = 0; o < 4; ++o) {
+          const float s = IN == 16 && !BF16 ? acc[t][4 * i + o] + acc[t][8 + 4 * i + o] : acc[t][4 * i + o];
+          v[o] = on ? s : 0.0f;
+        }
+        const int64_t at = row * p.g_ldx + 8 * i + 4 * h;
         if constexpr (BF16) {
           uint16_t *o = (uint16_t *)p.g_x + at;
           if (p.g_vec) {
             *(u32x2 *)o = u32x2{bf16_of(v[0]) | (uint32_t)bf16_of(v[1]) << 16, bf16_of(v[2]) | (uint32_t)bf16_of(v[3]) << 16};
           } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = bf16_of(v[i]);
+            for (int k = 0; k < 4; ++k) o[k] = bf16_of(v[k]);
           }
         } else {
           float *o = (float *)p.g_x + at;
@@ -538,7 +607,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_gated_rows(GatedParams p) {
             *(gf32x4 *)o = v;
           } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = v[i];
+            for (int k = 0; k < 4; ++k) o[k] = v[k];
           }
         }
       }
@@ -659,7 +728,7 @@ hipError_t launch_gated_sums(const GatedParams &p, hipStream_t s) {
 }
 
 hipError_t launch_gated_rows(const GatedParams &p, hipStream_t s) {
-  const dim3 grid(p.fwd_wg[KS_NFAM]), block(kThreads);
+  const dim3 grid(p.fwd_wg[KS_NFAM]), block(512);
   if (grid.x == 0) return hipSuccess;
   if (p.bf16) {
     if (p.in_dim == 16) hipLaunchKernelGGL((k_gated_rows<true, 16>), grid, block, 0, s, p);
