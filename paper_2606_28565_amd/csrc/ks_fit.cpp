@@ -43,15 +43,16 @@ ks_status check_rows(const ks_heads *h, const ks_rows *r) {
 // workgroups (two per CU and one to follow each), so that the weights' way into
 // LDS is paid for by several tiles where there are many, and one pass of the four
 // waves each where there are few.  Backward: about 512 workgroups (two per CU are
-// resident), each at least the rows it takes at a time.  The split depends on
+// resident; one with fp32 heads of 32 inputs, 256 then), each at least the rows it
+// takes at a time.  The split depends on
 // sizes alone, so results do not depend on the device.
-constexpr int64_t kFwdWgs = 1024, kBwdWgs = 512;
+constexpr int64_t kFwdWgs = 1024;
 
 void plan(ks::GatedParams &p, const ks_heads *h, const ks_rows *r) {
   const int64_t tiles = (r->n_rows + 63) / 64;
   p.fwd_tiles = (int32_t)(4 * std::max<int64_t>(1, (tiles + 4 * kFwdWgs - 1) / (4 * kFwdWgs)));
-  const int64_t unit = ks::kGatedStep;
-  p.bwd_rows = (int32_t)(unit * std::max<int64_t>(1, (r->n_rows + unit * kBwdWgs - 1) / (unit * kBwdWgs)));
+  const int64_t unit = ks::kGatedStep, wgs = h->precision == KS_F32 && h->in_dim == 32 ? 256 : 512;
+  p.bwd_rows = (int32_t)(unit * std::max<int64_t>(1, (r->n_rows + unit * wgs - 1) / (unit * wgs)));
   p.fwd_wg[0] = p.bwd_wg[0] = 0;
   for (int f = 0; f < KS_NFAM; ++f) {
     const int64_t n = r->fam_off[f + 1] - r->fam_off[f];
