@@ -104,7 +104,7 @@ constexpr double kUniqF32Rate = 1.9e14, kUniqMost = 2.0 * 128 * (32 + 128) / kUn
 // the head's seconds per pair
 double head_secs(const ks_heads *h) {
   if (h->mode == KS_ETA_GATED)
-    return h->hidden * (h->precision == KS_BF16 ? 0.45e-12 : h->in_dim == 16 ? 0.5e-12 : 0.85e-12);
+    return h->hidden * (h->precision == KS_BF16 ? 0.34e-12 : h->in_dim == 16 ? 0.45e-12 : 0.65e-12);
   const double rate = h->precision == KS_F32 ? kUniqF32Rate : h->hidden == 64 ? 0.65e15 : 1.2e15;
   return 2.0 * h->hidden * (h->in_dim + h->hidden) / rate;
 }

@@ -218,3 +218,35 @@ def test_no_tensors():
     abi.ks_adamw(abi.adamw_config(1e-3, step_dev=count), (abi.ks_tensor * 0)(), abi.current_stream())
     torch.cuda.synchronize()
     assert int(count) == 1
+
+
+def test_more_than_2_to_the_32_elements():
+    """States in 8 bits of one tensor of 2^32 + 1000 elements: its two ends and the
+    elements around 2^31 and 2^32."""
+    import torch
+    n = (1 << 32) + 1000
+    free, _ = torch.cuda.mem_get_info()
+    if free < 60 << 30:
+        pytest.skip("needs 60 GiB of device memory")
+    p = torch.ones(n, device="cuda")
+    g = torch.full((n,), 0.25, dtype=torch.bfloat16, device="cuda")
+    m = torch.zeros(n, dtype=torch.uint8, device="cuda")
+    v = torch.zeros(n, dtype=torch.uint8, device="cuda")
+    blocks = -(-n // 64)
+    d = {"param": p, "grad": g, "m": m.view(torch.float8_e4m3fn), "v": v.view(torch.float8_e5m2), "weight_decay": 0.0,
+         "m_exp": torch.ones(blocks, dtype=torch.uint8, device="cuda"),
+         "v_exp": torch.ones(blocks, dtype=torch.uint8, device="cuda"), "copy": None}
+    spans = [slice(a, a + 256) for a in (0, (1 << 31) - 128, (1 << 32) - 128, n - 256)]
+    rng = np.random.default_rng(4)
+    given = []
+    for s in spans:
+        t = torch.from_numpy(rng.normal(size=256).astype(np.float32)).bfloat16().cuda()
+        g[s] = t
+        given.append(t.float().cpu().numpy())
+    run([d], 8, step=1)
+    for s, gr in zip(spans, given):
+        mm, vv = o.moments32(np.zeros(256, np.float32), np.zeros(256, np.float32), gr, CFG["grad_scale"], CFG["beta1"], CFG["beta2"])
+        want = o.step(np.ones(256), mm, vv, CFG["lr"], 0.0, CFG["beta1"], CFG["beta2"], CFG["eps"], 1)
+        up = np.abs(want - 1)
+        assert (np.abs(values(p[s]) - want) <= 12 * o.EPS * up + 3 * o.EPS * (1 + np.abs(want))).all()
+    assert (p[1000:1100] == p[1000]).all() and p[1000] < 1

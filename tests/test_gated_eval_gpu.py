@@ -302,3 +302,20 @@ def test_simulation_with_gated_heads():
     assert (res["state"] == 2).all() and res["n_steps"] == again["n_steps"]
     np.testing.assert_array_equal(res["step_latency"], again["step_latency"])
     assert (res["step_latency"] > 0).all()
+
+
+def test_allocation_free_evaluation(small):
+    """ks_eval_steps_static takes gated heads: the results of ks_eval_steps."""
+    import torch
+    d, _ = weights("bf16", 32, 200)
+    ns = len(small.specs["peak_flops"])
+    want, _ = evaluate(small, d, ns, per_pair=False)
+    di = abi.DeviceInputs(small)
+    so_t, so = abi.step_outputs(small.desc.n_steps, ns)
+    flags = torch.full((1,), 7, dtype=torch.int32, device="cuda")
+    abi.ks_eval_steps_static(di.desc, di.steps, di.specs_ptr, ns, abi.gated_heads(d["w1"], d["w2"], d["w3"], d["b3"]),
+                             di.host, so, None, flags.data_ptr(), abi.current_stream())
+    torch.cuda.synchronize()
+    assert int(flags) == 0
+    for k in ("t_body", "t_step"):
+        np.testing.assert_array_equal(so_t[k].cpu().numpy(), want[k])

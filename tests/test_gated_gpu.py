@@ -434,3 +434,117 @@ def test_captured_loss_replays():
     h["w1"] = d["w1"].double().cpu().numpy()
     check_loss(h, off, eta, weight, 0.5, (loss.double().cpu().numpy(), z.double().cpu().numpy(),
                                           {k: v.double().cpu().numpy() for k, v in out.items()}))
+
+
+# ------------------------------------------------------------------ the far ends
+def test_offsets_past_32_bits():
+    """Rows 2^16 elements apart: 10.5 GB from the first to the last."""
+    import torch
+    n, ld, inp, hid = 40_000, 1 << 16, 16, 48
+    d, h, off = make(n, "f32", inp, hid)
+    far = torch.empty(n * ld, dtype=torch.float32, device="cuda").view(n, ld)[:, :inp]
+    far.copy_(d["x"])
+    near = forward(d, off)
+    dz = torch.randn(n, generator=torch.Generator().manual_seed(5)).cuda()
+    grads = backward(d, off, dz)
+    d["x"] = far
+    assert (forward(d, off) == near).all()
+    got = backward(d, off, dz)
+    for k in grads:
+        assert (got[k] == grads[k]).all(), k
+
+
+@pytest.mark.parametrize("prec,inp,hid", [("bf16", 16, 130), ("f32", 32, 129), ("f32", 16, 40)])
+def test_rows_gradient_many_rows(prec, inp, hid):
+    """More rows than a workgroup takes in one pass, heads in one part and in two:
+    a sample of rows of each family (each row's gradient depends on that row alone)."""
+    import torch
+    n = 600_001
+    d, h, off = make(n, prec, inp, hid)
+    dz = torch.randn(n, generator=torch.Generator().manual_seed(5))
+    got = backward(d, off, dz.cuda())["x"]
+    rng = np.random.default_rng(1)
+    for f in range(NFAM):
+        if off[f] == off[f + 1]:
+            continue
+        r = np.unique(np.concatenate([rng.integers(off[f], off[f + 1], 300), [off[f], off[f + 1] - 1]]))
+        _, k = o.block(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], h["b3"][f])
+        want, err = o.gradients(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], dz.numpy()[r], k, 1, bits(prec))
+        # (bf16 rounds dg and du to 2^-18 before the sum over the units, and the result to 2^-8)
+        extra = 2.0 ** -18 * (np.abs(dz.numpy()[r])[:, None] * (
+            np.abs(h["w3"][f] * k["u"] * (k["s"] + k["a"] * (1 - k["s"]))) @ np.abs(h["w1"][f])
+            + np.abs(h["w3"][f] * k["a"]) @ np.abs(h["w2"][f]))) if prec == "bf16" else 0.0
+        half = 2.0 ** -8 if prec == "bf16" else 0.0
+        bound = err["x"] + extra + half * (np.abs(want["x"]) + err["x"] + extra)
+        assert (np.abs(got[r] - want["x"]) <= bound).all(), (f, np.max(np.abs(got[r] - want["x"]) / bound))
+
+
+@pytest.mark.parametrize("scale", [1e-12, 1e12])
+def test_features_of_any_size(scale):
+    """fp32 features far from 1, with weights that bring the gates back: the pieces
+    keep their precision."""
+    import torch
+    d, h, off = make(300, "f32", 32, 70)
+    d["x"].mul_(scale)
+    d["w1"].div_(scale)
+    d["w2"].div_(scale)
+    h["x"], h["w1"], h["w2"] = (d[k].double().cpu().numpy() for k in ("x", "w1", "w2"))
+    check_forward(d, h, off, forward(d, off))
+    dz = torch.randn(300, generator=torch.Generator().manual_seed(5))
+    check_grads(h, off, dz.numpy(), backward(d, off, dz.cuda()), "f32")
+
+
+@pytest.mark.parametrize("prec", ["f32", "bf16"])
+def test_what_is_not_finite_stays_in_its_row_and_family(prec):
+    """A NaN or infinity in a row that counts: that row's z, its family's gradients and
+    loss, and nothing else."""
+    import torch
+    d, h, off = make(500, prec, 16, 64)
+    clean = forward(d, off)
+    dz = torch.randn(500, generator=torch.Generator().manual_seed(5)).cuda()
+    grads = backward(d, off, dz)
+    d["x"][off[5] + 3, 2] = float("nan")
+    d["x"][off[5] + 4, 3] = float("inf")
+    z = forward(d, off)
+    bad = np.zeros(500, bool)
+    bad[[off[5] + 3, off[5] + 4]] = True
+    assert not np.isfinite(z[bad]).any() and (z[~bad] == clean[~bad]).all()
+    got = backward(d, off, dz)
+    for k in ("w1", "w2", "w3"):
+        others = [f for f in range(NFAM) if f != 5]
+        assert (got[k][others] == grads[k][others]).all() and not np.isfinite(got[k][5]).all(), k
+    assert not np.isfinite(got["x"][bad]).any() and (got["x"][~bad] == grads["x"][~bad]).all()
+    eta, weight = targets(500)
+    loss, _, _ = run_loss(d, off, eta.cuda(), weight.cuda(), 0.5)
+    assert not np.isfinite(loss[5]) and np.isfinite(loss[others]).all()
+
+
+def test_two_streams_at_once():
+    """Two losses in flight, each with its own workspace: the bits of each alone."""
+    import torch
+    sets = []
+    for seed in (1, 2):
+        d, _, off = make(30_000, "bf16", 32, 256, seed=seed)
+        eta, weight = targets(30_000, seed)
+        eta, weight = eta.cuda(), weight.cuda()
+        hd, rows = heads_of(d), abi.feature_rows(d["x"], off)
+        out = {k: torch.empty(d[k].shape, device="cuda") for k in ("w1", "w2", "w3", "b3")}
+        loss = torch.empty(NFAM, device="cuda")
+        ws = torch.empty(abi.ks_gated_workspace_bytes(hd, rows), dtype=torch.uint8, device="cuda")
+        sets.append((d, hd, rows, abi.eta_target(eta, weight, 0.5), out, abi.gated_grad(**out), loss, ws, eta, weight))
+
+    def call(s, stream):
+        abi.ks_gated_loss(s[1], s[2], s[3], s[6].data_ptr(), None, s[5], s[7].data_ptr(), s[7].numel(), stream)
+
+    alone = []
+    for s in sets:
+        call(s, abi.current_stream())
+        torch.cuda.synchronize()
+        alone.append((s[6].clone(), {k: v.clone() for k, v in s[4].items()}))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for s, st in zip(sets, streams):
+            call(s, st.cuda_stream)
+    torch.cuda.synchronize()
+    for s, a in zip(sets, alone):
+        assert (s[6] == a[0]).all() and all((s[4][k] == a[1][k]).all() for k in a[1])
