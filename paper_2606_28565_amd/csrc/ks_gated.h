@@ -12,11 +12,14 @@
 // fp32 operands are split into three bf16 pieces that sum to them exactly (from
 // 2^-102 up; below, what is lost is under 2^-126) and the six products of the
 // largest pieces are taken: the three left out are below 2^-25 of the product.
-// The bf16 instruction runs beside other waves' vector work; the fp32 one does not
-// (measured on pairs of waves: bf16 32x32x16 with FMAs takes the longer of the two,
-// fp32 32x32x2 the sum of both), and the vector work is what bounds this block: an
-// exponential and a reciprocal per gate.  (1M rows of 32-256: 305 us on the fp32
-// instruction.)
+// The bf16 instruction runs beside other waves' vector work, most of the way; the fp32
+// one does not (two waves of each per SIMD: 32x32x16 bf16 and multiplications take 888
+// cycles, alone 659 and 369; 16x16x4 fp32 940, alone 578 and 367), and the vector work
+// is what bounds this block: an exponential, a reciprocal and five more per gate.
+//
+// 2M rows of bf16 32-256: 175 us, the vector units 81% busy.  1M rows of fp32 32-256:
+// 169 us (six products at the rate of a large bf16 product: 159; on the fp32
+// instruction it took 305).
 #pragma once
 
 #include <stdint.h>

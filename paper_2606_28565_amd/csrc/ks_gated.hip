@@ -187,7 +187,7 @@ __global__ __launch_bounds__(64 * N, 2) void k_gated_forward(GatedParams p) {
 // and leaves both in LDS.  What a unit makes of a row is three pieces too for fp32
 // heads (gradients are then sums of unrounded terms); for bf16 heads, whose features
 // and weights are rounded to 2^-9, two, within 2^-18 of each term (5 instructions
-// fewer of 19 per gate; 2M rows of 32-256: 437 us, with three 530).
+// fewer of 19 per gate; 2M rows of 32-256: 437 us where three took 530).
 //
 // Which rows a lane's eight inner indices of dW stand for is free, as long as both
 // operands agree: those it has, 8 (i / 4) + 4 (its half) + i mod 4 of each 16.  With 16
@@ -195,14 +195,16 @@ __global__ __launch_bounds__(64 * N, 2) void k_gated_forward(GatedParams p) {
 // the second piece of dz x (then the third and nothing): a unit's gradient is the sum
 // of the two halves.
 //
-// Vector work bounds it: 8 instructions, an exponential and a reciprocal for each gate
-// and 7 to split what it makes.  A wave alone issues a vector instruction every 7.5
-// cycles, four per SIMD one every 2.7 (FMA) to 4.4, hence 128 registers and 32 units per
-// wave; and the 32x32x16 instruction runs beside them where 16x16x32 does not (two
-// waves of each kind per SIMD: 678 cycles where one kind alone takes 647 and 367;
-// 16x16x32 625, of 322 and 367).  (2M rows of 32-256 in bf16, loss and gradients: 64
-// units per wave, z exchanged between them and dz formed on the way took 776 us, this
-// and k_gated_forward take 437 and 175.)
+// Vector work bounds it: 6 instructions, an exponential and a reciprocal for each gate
+// and 6 (two pieces) or 11 to split what it makes, for each 28 or so cycles of the
+// matrix unit.  A wave alone issues a vector instruction every 7.5 cycles, four per
+// SIMD one every 2.7 (FMA) to 5 (conversions): hence 128 registers and 32 units per
+// wave; and the 32x32x16 instruction runs beside them where 16x16x32 does not (two waves
+// of each kind per SIMD, multiplications: 888 cycles, alone 659 and 369; 16x16x32 671,
+// alone 326 and 369).  2M rows of bf16 32-256: 425 us, the vector units 71% and the
+// matrix units 44% busy.  (64 units per wave, z exchanged between the unit groups and
+// dz formed on the way, one pass in all: 776 us, where this and k_gated_forward take
+// 600.)
 template <bool BF16, int IN>
 struct Back {
   static constexpr int KC = IN / 16, W = 8;
