@@ -449,7 +449,12 @@ ks_status ks_eval_steps_static(const ks_desc* desc, const ks_steps* steps,
  * (ks_gated_loss) and moves the parameters (ks_adamw); the fitted weights price
  * records through the evaluation calls (mode KS_ETA_GATED).  ks_gated_forward and
  * ks_gated_backward are the block by itself, for losses of the caller's own.
- * None of these calls synchronizes; all can be captured into a graph.
+ * None of these calls synchronizes; all can be captured into a graph.  What a call
+ * writes may not overlap what else it reads or writes, and calls that may run at
+ * the same time (two streams, two captured graphs) need a workspace each.
+ * Numbers are taken as they come: products of fp32 heads are those of fp32 for
+ * magnitudes from 2^-102, and a row, dz or weight that is not finite makes what
+ * depends on it not finite.
  */
 
 /* Feature rows, family-major: rows [fam_off[f], fam_off[f+1]) are family f's and
@@ -467,8 +472,8 @@ typedef struct ks_rows {
 /* Gradients (device, overwritten; families without rows get zeros).
  * w1, w2: [KS_NFAM][hidden][in_dim], w3: [KS_NFAM][hidden], b3: [KS_NFAM], all
  * fp32 whatever the heads' precision, all four or none of them NULL.
- * x: [n_rows][ldx] of heads.precision's type, or NULL; it may not overlap the
- * rows themselves. */
+ * x: [n_rows][ldx] of heads.precision's type, or NULL; ldx from in_dim to 2^20, and
+ * it may not overlap the rows themselves. */
 typedef struct ks_gated_grad {
   float *w1, *w2, *w3, *b3;
   void *x;
@@ -477,7 +482,8 @@ typedef struct ks_gated_grad {
 
 /* Measured efficiency factors.  A row counts when its eta is finite and above 0
  * and its weight (1 without weights) is finite and above 0; the others, whatever
- * their features, add nothing to the loss or to any gradient. */
+ * their features, add nothing to the loss or to any gradient.  Weights go into
+ * fp32 products as they are: 2^-60 .. 2^60 is safe. */
 typedef struct ks_eta_target {
   const float *eta;       /* device [n_rows]                                 */
   const float *weight;    /* device [n_rows] or NULL                         */
@@ -555,8 +561,8 @@ typedef struct ks_adamw_config {
   uint32_t *step_dev;
 } ks_adamw_config;
 
-/* tensors: HOST array of n_tensors (read during the call); no two may share a
- * param.  Launches: one for every 200 tensors, one more with step_dev. */
+/* tensors: HOST array of n_tensors (read during the call); no two may share
+ * elements of a param.  Launches: one for every 200 tensors, one more with step_dev. */
 ks_status ks_adamw(const ks_adamw_config *config, const ks_tensor *tensors, int32_t n_tensors, hipStream_t stream);
 
 /* Synchronous device-side check of the inputs: step order within families,

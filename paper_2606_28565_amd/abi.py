@@ -548,15 +548,21 @@ def gated_heads(w1, w2, w3, b3) -> ks_heads:
     return hd
 
 
+def _row_stride(x) -> int:
+    if x.dim() != 2 or (x.numel() and x.stride(1) != 1):
+        raise ValueError("x is not [rows][in_dim] with adjacent elements")
+    if x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+        raise ValueError(f"x has rows of {x.shape[1]} elements every {x.stride(0)}")
+    return max(x.stride(0), x.shape[1])
+
+
 def feature_rows(x, fam_off) -> ks_rows:
     """Feature rows x [n][in_dim] (any row stride), grouped by family."""
     r = ks_rows()
-    if x.dim() != 2 or (x.numel() and x.stride(1) != 1):
-        raise ValueError("x is not [rows][in_dim] with adjacent elements")
-    r.n_rows = x.shape[0]
+    r.n_rows, r.ldx = x.shape[0], _row_stride(x)
     for f in range(NFAM + 1):
         r.fam_off[f] = int(fam_off[f])
-    r.x, r.ldx = _ptr(x) if x.numel() else None, max(x.stride(0), x.shape[1])
+    r.x = _ptr(x) if x.numel() else None
     return r
 
 
@@ -569,9 +575,8 @@ def gated_grad(w1=None, w2=None, w3=None, b3=None, x=None) -> ks_gated_grad:
             raise ValueError(f"the gradient of {name} is not fp32")
         setattr(g, name, _whole(t))
     if x is not None:
-        if x.dim() != 2 or (x.numel() and x.stride(1) != 1):
-            raise ValueError("x is not [rows][in_dim] with adjacent elements")
-        g.x, g.ldx = _ptr(x) if x.numel() else None, max(x.stride(0), x.shape[1])
+        g.ldx = _row_stride(x)
+        g.x = _ptr(x) if x.numel() else None
     return g
 
 

@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <utility>
 #include <vector>
 
 #include "ks.h"
@@ -170,8 +171,8 @@ ks_status ks_gated_backward(const ks_heads *heads, const ks_rows *rows, const fl
   if (st != KS_OK) return st;
   if (grad->x) {
     const int64_t e = p.bf16 ? 2 : 4;
-    if (grad->ldx < heads->in_dim || grad->ldx > (int64_t(1) << 31))
-      return set_error(KS_EINVAL, "grad.ldx %lld outside in_dim %d .. 2^31", (long long)grad->ldx, heads->in_dim);
+    if (grad->ldx < heads->in_dim || grad->ldx > (int64_t(1) << 20))
+      return set_error(KS_EINVAL, "grad.ldx %lld outside in_dim %d .. 2^20", (long long)grad->ldx, heads->in_dim);
     if (!aligned(grad->x, e)) return set_error(KS_EINVAL, "grad.x is not aligned to its type");
     if (rows->n_rows > 0 && overlap(grad->x, ((rows->n_rows - 1) * grad->ldx + heads->in_dim) * e, rows->x,
                                     ((rows->n_rows - 1) * rows->ldx + heads->in_dim) * e))
@@ -252,7 +253,7 @@ ks_status ks_adamw(const ks_adamw_config *c, const ks_tensor *tensors, int32_t n
   if (n_tensors < 0) return set_error(KS_EINVAL, "n_tensors %d below 0", n_tensors);
   if (n_tensors > 0 && !tensors) return set_error(KS_EINVAL, "tensors is NULL");
   if (c->state_bits != 8 && c->state_bits != 32) return set_error(KS_EINVAL, "state_bits %d not 8 or 32", c->state_bits);
-  if (!std::isfinite(c->lr) || c->lr < 0.0) return set_error(KS_EINVAL, "lr %g not finite and 0 or more", c->lr);
+  if (!std::isfinite((float)c->lr) || c->lr < 0.0) return set_error(KS_EINVAL, "lr %g not finite and 0 or more", c->lr);
   if (!(c->beta1 >= 0.0 && c->beta1 < 1.0) || !(c->beta2 >= 0.0 && c->beta2 < 1.0))
     return set_error(KS_EINVAL, "beta1 %g or beta2 %g outside [0, 1)", c->beta1, c->beta2);
   if (!((float)c->eps > 0.0f) || !std::isfinite((float)c->eps)) return set_error(KS_EINVAL, "eps %g not above 0", c->eps);
@@ -264,7 +265,8 @@ ks_status ks_adamw(const ks_adamw_config *c, const ks_tensor *tensors, int32_t n
     const ks_tensor &t = tensors[i];
     if (t.n < 0 || t.n > (int64_t(1) << 33)) return set_error(KS_ERANGE, "tensor %d: n %lld outside 0..2^33", i, (long long)t.n);
     if (t.grad_type != KS_F32 && t.grad_type != KS_BF16) return set_error(KS_EINVAL, "tensor %d: grad_type %d unknown", i, t.grad_type);
-    if (!std::isfinite(t.weight_decay)) return set_error(KS_EINVAL, "tensor %d: weight_decay not finite", i);
+    if (!std::isfinite((float)(1.0 - c->lr * (double)t.weight_decay)))
+      return set_error(KS_EINVAL, "tensor %d: weight_decay %g not finite, or too large for lr", i, t.weight_decay);
     if (t.n == 0) continue;
     if (!t.param || !t.grad || !t.m || !t.v) return set_error(KS_EINVAL, "tensor %d: a pointer is NULL", i);
     if (eight ? !t.m_exp || !t.v_exp : t.m_exp || t.v_exp)
@@ -274,12 +276,16 @@ ks_status ks_adamw(const ks_adamw_config *c, const ks_tensor *tensors, int32_t n
       return set_error(KS_EINVAL, "tensor %d: a pointer is not aligned to its type", i);
   }
   try {
-    std::vector<const float *> at;
+    std::vector<std::pair<uintptr_t, uintptr_t>> at;   // [begin, end)
     at.reserve(n_tensors);
     for (int i = 0; i < n_tensors; ++i)
-      if (tensors[i].n > 0) at.push_back(tensors[i].param);
+      if (tensors[i].n > 0) {
+        const uintptr_t p = reinterpret_cast<uintptr_t>(tensors[i].param);
+        at.emplace_back(p, p + (uintptr_t)tensors[i].n * sizeof(float));
+      }
     std::sort(at.begin(), at.end());
-    if (std::adjacent_find(at.begin(), at.end()) != at.end()) return set_error(KS_EINVAL, "two tensors share a param");
+    for (size_t i = 1; i < at.size(); ++i)
+      if (at[i].first < at[i - 1].second) return set_error(KS_EINVAL, "two tensors share elements of a param");
   } catch (...) {
     return set_error(KS_EINVAL, "no host memory for %d tensors", n_tensors);
   }

@@ -27,9 +27,10 @@ def feature_rows_of(inputs: abi.DeviceInputs, in_dim: int = 16, precision: str =
     dev = inputs.ws.device
     x = torch.empty((n * s, in_dim), dtype=torch.bfloat16 if precision == "bf16" else torch.float32, device=dev)
     roof = torch.empty(n * s, device=dev)
-    abi.ks_features(inputs.desc, inputs.specs_ptr, s, in_dim, abi.KS_BF16 if precision == "bf16" else abi.KS_F32,
-                    x.data_ptr() if n else None, in_dim, roof.data_ptr() if n else None, inputs.ws_ptr, inputs.ws_bytes,
-                    abi.current_stream())
+    with torch.cuda.device(dev):
+        abi.ks_features(inputs.desc, inputs.specs_ptr, s, in_dim, abi.KS_BF16 if precision == "bf16" else abi.KS_F32,
+                        x.data_ptr() if n else None, in_dim, roof.data_ptr() if n else None, inputs.ws_ptr,
+                        inputs.ws_bytes, abi.current_stream())
     return SimpleNamespace(x=x, t_roof=roof, fam_off=[s * int(v) for v in inputs.desc.fam_off])
 
 
@@ -40,6 +41,8 @@ class Measurements:
     def __init__(self, x, fam_off, eta, weight=None, huber: float = float("inf")):
         if eta.shape != x.shape[:1]:
             raise ValueError(f"eta is {tuple(eta.shape)}, not one per row of {tuple(x.shape)}")
+        if any(t is not None and t.device != x.device for t in (eta, weight)):
+            raise ValueError("x, eta and weight are not on one device")
         self.x, self.eta, self.weight = x, eta, weight
         self.rows = abi.feature_rows(x, fam_off)
         self.target = abi.eta_target(eta, weight, huber)
@@ -84,27 +87,38 @@ class GatedFit:
                             "weight_decay": weight_decay if k in ("w1", "w2") else 0.0})
         self.tensors = abi.adamw_tensors(tensors)
         self.config = abi.adamw_config(lr, state_bits=state_bits, step_dev=self.count)
-        self.ws = None
+        self.ws, self.rooms = None, []
 
     def workspace(self, data: Measurements) -> int:
-        """Room for a step on these rows; called by ``step``, and before a capture."""
+        """Room for a step on these rows; called by ``step``, and before a capture.
+        Smaller rooms are kept: captured steps go on using them."""
         import torch
+        like = self.weights["w1"]
+        if data.x.device != like.device or data.x.dtype != like.dtype or data.x.shape[1] != self.heads.in_dim:
+            raise ValueError(f"rows are {data.x.dtype} [{data.x.shape[1]}] on {data.x.device}, "
+                             f"not {like.dtype} [{self.heads.in_dim}] on {like.device}")
         need = abi.ks_gated_workspace_bytes(self.heads, data.rows)
         if need == 0:
             raise abi.KsError(abi.KS_EINVAL, abi.ks_last_error())
         if self.ws is None or self.ws.numel() < need:
             self.ws = torch.empty(need, dtype=torch.uint8, device=self.loss.device)
+            self.rooms.append(self.ws)
         return need
 
     def gradients(self, data: Measurements):
-        """The loss per family [NFAM] and, in ``self.grad``, its gradients."""
+        """The loss per family [NFAM] and, in ``self.grad``, its gradients; the next
+        call writes the same tensors."""
+        import torch
         need = self.workspace(data)
-        abi.ks_gated_loss(self.heads, data.rows, data.target, self.loss.data_ptr(), None, self.grad_struct,
-                          self.ws.data_ptr(), need, abi.current_stream())
+        with torch.cuda.device(self.loss.device):
+            abi.ks_gated_loss(self.heads, data.rows, data.target, self.loss.data_ptr(), None, self.grad_struct,
+                              self.ws.data_ptr(), need, abi.current_stream())
         return self.loss
 
     def step(self, data: Measurements):
-        """One step; returns the loss per family before it (device, [NFAM])."""
+        """One step; returns the loss per family before it (``gradients``)."""
+        import torch
         loss = self.gradients(data)
-        abi.ks_adamw(self.config, self.tensors, abi.current_stream())
+        with torch.cuda.device(loss.device):
+            abi.ks_adamw(self.config, self.tensors, abi.current_stream())
         return loss

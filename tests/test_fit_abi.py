@@ -135,6 +135,7 @@ def test_bad_gradients():
     far = A + (1 << 16)
     assert back(A, A, A, A, far, 15) == abi.KS_EINVAL            # a row does not fit its stride
     assert back(A, A, A, A, far + 2, 16) == abi.KS_EINVAL        # not aligned to its type
+    assert back(A, A, A, A, far, (1 << 20) + 1) == abi.KS_EINVAL
     assert back(A, A, A, A, A, 16) == abi.KS_EINVAL              # over the rows themselves
     assert back(A, A, A, A, A + 16 * 4 * 19, 16) == abi.KS_EINVAL   # over the last of them
     assert abi.ks_gated_backward(h, r, None, abi.ks_gated_grad(A, A, A, A, None, 0), A, big, None, check=False) == abi.KS_EINVAL
@@ -201,12 +202,13 @@ def test_bad_adamw():
 
     good = dict(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, grad_scale=1.0, state_bits=32, step=1)
     nan, inf = float("nan"), float("inf")
-    for kw in (dict(lr=-1.0), dict(lr=nan), dict(lr=inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=nan),
+    for kw in (dict(lr=-1.0), dict(lr=nan), dict(lr=inf), dict(lr=1e39), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=nan),
                dict(eps=0.0), dict(eps=-1.0), dict(eps=1e-60), dict(eps=inf), dict(grad_scale=nan), dict(grad_scale=1e300),
                dict(state_bits=16), dict(state_bits=0), dict(step=0)):
         assert call(abi.adamw_config(**{**good, **kw}), tensor()) == abi.KS_EINVAL, kw
     cfg, cfg8 = abi.adamw_config(**good), abi.adamw_config(**{**good, "state_bits": 8})
     for kw in (dict(param=None), dict(grad=None), dict(m=None), dict(v=None), dict(grad_type=2), dict(weight_decay=nan),
+               dict(weight_decay=inf),
                dict(param=A + 2), dict(grad=A + 2), dict(m=A + 1), dict(v=A + 2), dict(copy=A + 1), dict(m_exp=A)):
         assert call(cfg, tensor(param=A + 4096), tensor(**kw)) == abi.KS_EINVAL, kw
     for n in (-1, (1 << 35) + 1):
@@ -214,6 +216,8 @@ def test_bad_adamw():
     assert call(cfg8, tensor()) == abi.KS_EINVAL
     assert call(cfg8, tensor(m_exp=A)) == abi.KS_EINVAL
     assert call(cfg, tensor(), tensor()) == abi.KS_EINVAL         # the same parameter twice
+    assert "share" in abi.ks_last_error()
+    assert call(cfg, tensor(param=A + 36), tensor()) == abi.KS_EINVAL   # ... its last element
     assert "share" in abi.ks_last_error()
     assert abi.load().ks_adamw(C.byref(cfg), None, 2, None) == abi.KS_EINVAL
     assert abi.load().ks_adamw(C.byref(cfg), None, -1, None) == abi.KS_EINVAL
@@ -232,6 +236,12 @@ def test_binding_refuses_what_it_cannot_describe():
         abi.gated_heads(z(NFAM, 16, 64).transpose(1, 2), w[1], w[2], w[3])
     with pytest.raises(ValueError):
         abi.feature_rows(z(16, 30).t(), [0] * 11)
+    for x in (z(16).expand(30, 16), z(64).as_strided((10, 16), (4, 1))):   # rows over one another
+        with pytest.raises(ValueError):
+            abi.feature_rows(x, [0] * 11)
+        with pytest.raises(ValueError):
+            abi.gated_grad(x=x)
+    assert abi.feature_rows(z(16).expand(1, 16), [0] * 11).ldx == 16
     with pytest.raises(ValueError):
         abi.gated_grad(w1=w[0].bfloat16())
     with pytest.raises(ValueError):

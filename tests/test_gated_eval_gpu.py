@@ -286,6 +286,50 @@ def test_captured_fit():
     assert int(graphed.count) == 6
 
 
+def test_captured_fit_beside_larger_rows():
+    """A captured step keeps its workspace when the same fit then takes more rows:
+    replays in turn with eager steps on the larger set train as eager steps do."""
+    import torch
+    few, many = (abi.DeviceInputs(gen.config1(0, n)) for n in (2, 12))
+    sets = []
+    for i, di in enumerate((few, many)):
+        r = fit.feature_rows_of(di, 16)
+        eta = 1 + torch.rand(len(r.x), generator=torch.Generator().manual_seed(i)).cuda()
+        sets.append(fit.Measurements(r.x, r.fam_off, eta))
+    eager, graphed = fit.GatedFit(16, 64, seed=2), fit.GatedFit(16, 64, seed=2)
+    eager.step(sets[0])
+    graphed.step(sets[0])
+    torch.cuda.synchronize()
+    gr = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr):
+        graphed.step(sets[0])
+    first = graphed.ws.data_ptr()
+    for i in range(4):
+        eager.step(sets[1])
+        graphed.step(sets[1])
+        assert graphed.ws.data_ptr() != first
+        other = torch.full((len(sets[0].x), 64), float("nan"), device="cuda")   # takes memory that is free
+        eager.step(sets[0])
+        gr.replay()
+        torch.cuda.synchronize()
+        assert other.isnan().all()
+        for k in eager.param:
+            assert (eager.param[k] == graphed.param[k]).all(), (i, k)
+
+
+def test_fit_refuses_rows_of_another_kind():
+    import torch
+    ft = fit.GatedFit(16, 32, "bf16")
+    off = [0] + [6] * NFAM
+    eta = torch.ones(6, device="cuda")
+    for x in (torch.zeros(6, 16, device="cuda"), torch.zeros(6, 40, device="cuda").bfloat16()[:, :32]):
+        with pytest.raises(ValueError):
+            ft.step(fit.Measurements(x, off, eta))
+    with pytest.raises(ValueError):
+        fit.Measurements(torch.zeros(6, 16, device="cuda"), off, eta.cpu())
+    assert int(ft.count) == 0
+
+
 def test_simulation_with_gated_heads():
     """The serving simulation takes gated heads like any others: its first step's
     latency is the evaluation's."""
