@@ -42,13 +42,12 @@ def block(x, w1, w2, w3, b3):
     return z, {"g": g, "u": u, "s": s, "a": a, "y": y, "err": {"g": eg, "u": eu, "s": es, "a": ea, "y": ey, "z": ez}}
 
 
-def gradients(x, w1, w2, w3, dz, k, terms, term_bits=25):
+def gradients(x, w1, w2, w3, dz, k, terms):
     """Gradients of sum dz z from ``block``'s dict k: w1, w2, w3, b3, x, and bounds on
     their fp32 errors.  terms: additions in fp32 that one sum over rows goes through
-    in a row.  term_bits: what a unit makes of a row is within 2^-term_bits of itself
-    when it is summed (18 for bf16 heads: two bfloat16 pieces, the second rounds a rest
-    of at most 2^-9 of the value to 2^-9 of that).  Rows whose dz is 0 add nothing,
-    whatever they hold."""
+    in a row.  What a unit makes of a row is summed in three exact pieces; the products
+    of pieces left out are below 2^-25 of it.  Rows whose dz is 0 add nothing, whatever
+    they hold."""
     dz = np.asarray(dz, np.float64)
     on = dz != 0
     x = np.where(on[:, None], np.asarray(x, np.float64), 0.0)
@@ -64,7 +63,7 @@ def gradients(x, w1, w2, w3, dz, k, terms, term_bits=25):
     edg = np.abs(dy) * (e0["u"] * np.abs(t) + np.abs(u) * et + e0["u"] * et) + 6 * EPS * np.abs(dg)
     val = {"w1": dg.T @ x, "w2": du.T @ x, "w3": (dz[:, None] * y).sum(0), "b3": dz.sum(), "x": dg @ w1 + du @ w2}
     ax, H = np.abs(x), w1.shape[0]
-    long = (terms + 8) * EPS + 2.0 ** -term_bits
+    long = (terms + 8) * EPS + 2.0 ** -25
     # (dw3 may come as W2 . sum dz a x: its terms are dW2's, weighted)
     err = {"w1": edg.T @ ax + long * (np.abs(dg).T @ ax), "w2": edu.T @ ax + long * (np.abs(du).T @ ax),
            "w3": (((np.abs(dz)[:, None] * (e0["a"] + (4 * EPS + long) * np.abs(a))).T @ ax) * np.abs(w2)).sum(1),

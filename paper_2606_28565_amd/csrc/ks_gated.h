@@ -48,20 +48,31 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 // a pair of values as three packed pairs of pieces.  (A piece could be taken off in one
 // instruction, the dot product with (-1, 0) or (0, -1), but that one waits for the
 // matrix instructions of every wave, as the shift or mask and the subtraction do not.)
+//
+// The first piece is rounded, so what is left is at most 2^-9; the second is cut
+// off, so that what it leaves, at most 2^-16, fits the third exactly.
+__device__ __forceinline__ uint32_t upper(float v) { return __builtin_bit_cast(uint32_t, v) & 0xFFFF0000u; }
+__device__ __forceinline__ uint32_t pack_upper(float lo, float hi) {
+  return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302);
+}
 __device__ __forceinline__ void split2(float a, float b, uint32_t &p0, uint32_t &p1, uint32_t &p2) {
   p0 = pack2(a, b);
   a -= __builtin_bit_cast(float, p0 << 16);
   b -= __builtin_bit_cast(float, p0 & 0xFFFF0000u);
-  p1 = pack2(a, b);
-  a -= __builtin_bit_cast(float, p1 << 16);
-  b -= __builtin_bit_cast(float, p1 & 0xFFFF0000u);
-  p2 = pack2(a, b);
+  p1 = pack_upper(a, b);
+  a -= __builtin_bit_cast(float, upper(a));
+  b -= __builtin_bit_cast(float, upper(b));
+  p2 = pack_upper(a, b);
 }
-
-// ... as two, to within 2^-18 of each (half a step of a half step, 2^-9 2^-9)
-__device__ __forceinline__ void split2(float a, float b, uint32_t &p0, uint32_t &p1) {
-  p0 = pack2(a, b);
-  p1 = pack2(a - __builtin_bit_cast(float, p0 << 16), b - __builtin_bit_cast(float, p0 & 0xFFFF0000u));
+// ... all cut off: for a factor of one piece, where no product is left out
+__device__ __forceinline__ void cut2(float a, float b, uint32_t &p0, uint32_t &p1, uint32_t &p2) {
+  p0 = pack_upper(a, b);
+  a -= __builtin_bit_cast(float, upper(a));
+  b -= __builtin_bit_cast(float, upper(b));
+  p1 = pack_upper(a, b);
+  a -= __builtin_bit_cast(float, upper(a));
+  b -= __builtin_bit_cast(float, upper(b));
+  p2 = pack_upper(a, b);
 }
 
 // HID: the widest block that fits the LDS room (any narrower one too)

@@ -10,7 +10,8 @@
 //   du = dz w3 a,  dg = dz w3 u silu'(g),  silu'(g) = s + s (g - a),  dw3 += dz a u.
 // w3 is one factor of a unit over all rows, so k_gated_sums leaves it out and
 // k_gated_reduce multiplies the finished sums by it.  dz is one factor of a row
-// over all units, so it goes to the rows' side of the product, dW = (..)^T (dz x).
+// over all units: fp32 heads have it on the rows' side of the product, dW =
+// (..)^T (dz x); bf16 heads, whose rows are one exact piece, on the units' side.
 // And u = W2 x, so sum dz a u = W2 . (sum dz a x): dw3 follows from the finished
 // sum of dW2.
 #include <hip/hip_runtime.h>
@@ -21,6 +22,7 @@
 namespace ks {
 
 using gated::Block;
+using gated::cut2;
 using gated::gbf16x8;
 using gated::gf32x16;
 using gated::gf32x4;
@@ -29,6 +31,7 @@ using gated::sigmoid;
 using gated::split2;
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t any16 __attribute__((may_alias));
 
 namespace {
 
@@ -183,34 +186,35 @@ __global__ __launch_bounds__(64 * N, 2) void k_gated_forward(GatedParams p) {
 // of them is the row operand of the next product, units x features, without any
 // exchange between lanes.  The eight waves are the unit groups (HG) times row groups
 // (RG).  What depends on the rows alone is made once for all of them: each wave
-// brings 16 rows a step, as the projections' operand and as dz x in three bf16 pieces,
-// and leaves both in LDS.  What a unit makes of a row is three pieces too for fp32
-// heads (gradients are then sums of unrounded terms); for bf16 heads, whose features
-// and weights are rounded to 2^-9, two, within 2^-18 of each term (5 instructions
-// fewer of 19 per gate; 2M rows of 32-256: 437 us where three took 530).
+// brings 16 rows a step, as the projections' operand and as the column operand of dW,
+// and leaves both in LDS.  What a unit makes of a row is three bf16 pieces, exactly.
+// The column operand is dz x in three pieces and six products for fp32 heads; for
+// bf16 heads it is the rows as they are and three products, dz a multiplication of
+// each of a unit's two terms.  (With dz x there too, six products, and two pieces of
+// the terms, within 2^-18 of each, 2M rows of 32-256 took 421 us and weight
+// gradients came out with 3e-6 where fp32 sums have 2e-6; with three pieces 530 us.
+// So 411 us.)
 //
 // Which rows a lane's eight inner indices of dW stand for is free, as long as both
 // operands agree: those it has, 8 (i / 4) + 4 (its half) + i mod 4 of each 16.  With 16
-// inputs the instruction's 32 columns are the features twice, against the first and
-// the second piece of dz x (then the third and nothing): a unit's gradient is the sum
-// of the two halves.
+// inputs the instruction's 32 columns are the features twice: for fp32 heads against
+// the first and the second piece of dz x (then the third and nothing), a unit's gradient
+// the sum of the two halves; bf16 heads have no use for the second.
 //
 // Vector work bounds it: 6 instructions, an exponential and a reciprocal for each gate
-// and 6 (two pieces) or 11 to split what it makes, for each 28 or so cycles of the
-// matrix unit.  A wave alone issues a vector instruction every 7.5 cycles, four per
-// SIMD one every 2.7 (FMA) to 5 (conversions): hence 128 registers and 32 units per
-// wave; and the 32x32x16 instruction runs beside them where 16x16x32 does not (two waves
-// of each kind per SIMD, multiplications: 888 cycles, alone 659 and 369; 16x16x32 671,
-// alone 326 and 369).  2M rows of bf16 32-256: 425 us, the vector units 71% and the
-// matrix units 44% busy.  (64 units per wave, z exchanged between the unit groups and
-// dz formed on the way, one pass in all: 776 us, where this and k_gated_forward take
-// 600.)
+// (bf16: 8) and 11 to split what it makes, for each 48 (bf16: 16) cycles of the matrix
+// unit.  A wave alone issues a vector instruction every 7.5 cycles, four per
+// SIMD one every 2.7 (FMA) to 5 (conversions: the pieces are cut off, not rounded,
+// where that is as good): hence 128 registers and 32 units per wave; and the 32x32x16
+// instruction runs beside them where 16x16x32 does not (two waves of each kind per
+// SIMD, multiplications: 888 cycles, alone 659 and 369; 16x16x32 671, alone 326 and
+// 369).  (64 units per wave, z exchanged between the unit groups and dz formed on the
+// way, one pass in all: 776 us, where this and k_gated_forward take 585.)
 template <bool BF16, int IN>
 struct Back {
   static constexpr int KC = IN / 16, W = 8;
   static constexpr int NP = BF16 ? 1 : 3;      // pieces of the projections' operands
-  static constexpr int NQ = IN == 16 ? 2 : 3;  // column operands of dW
-  static constexpr int NA = BF16 ? 2 : 3;      // pieces of its row operands
+  static constexpr int NQ = BF16 ? 1 : IN == 16 ? 2 : 3;   // column operands of dW
   // eight consecutive values as pieces
   __device__ static __forceinline__ void pieces(const gu32x4 (&raw)[BF16 ? 1 : 2], gu32x4 (&x)[NP]) {
     if constexpr (BF16) x[0] = raw[0];
@@ -224,7 +228,7 @@ struct Back {
 template <bool BF16, int IN>
 __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(GatedParams p) {
   using K = Back<BF16, IN>;
-  constexpr int KC = K::KC, W = K::W, NP = K::NP, NQ = K::NQ, NA = K::NA, R = 16 * W;   // rows of a step
+  constexpr int KC = K::KC, W = K::W, NP = K::NP, NQ = K::NQ, R = 16 * W;   // rows of a step
   constexpr int kTiles = R / 32;
   constexpr int kX = kTiles * KC * NP * 64 * 4, kQ = kTiles * 2 * NQ * 64 * 4, kJoin = (W - 1) * 16 * 64;
   __shared__ __align__(16) uint32_t lds[kX + kQ > kJoin ? kX + kQ : kJoin];
@@ -274,16 +278,20 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
       const char *x = (const char *)p.x + mine * ld * E;
       load8<BF16>(raw, x + off_row, 0, p.vec);
       dzc = p.dz[mine + c];
+      if constexpr (!BF16) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = element<BF16>(x + (size_t)(8 * (i >> 2) + (i & 3)) * ld * E + off_col, 0);
+        for (int i = 0; i < 8; ++i) v[i] = element<BF16>(x + (size_t)(8 * (i >> 2) + (i & 3)) * ld * E + off_col, 0);
+      }
     } else {   // past the last row a lane reads the last
       const int64_t base = mine < end ? mine : end - 1;
       const int last = (int)(end - base) - 1;
       load8<BF16>(raw, p.x, (base + min(c, last)) * ld + (brings ? 8 * oct : 0), p.vec);
       dzc = p.dz[base + min(c, last)];
+      if constexpr (!BF16) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        v[i] = element<BF16>(p.x, (base + min(8 * (i >> 2) + 4 * h + (i & 3), last)) * ld + col);
+        for (int i = 0; i < 8; ++i)
+          v[i] = element<BF16>(p.x, (base + min(8 * (i >> 2) + 4 * h + (i & 3), last)) * ld + col);
+      }
       if (mine + c >= end) dzc = 0.0f;
     }
   };
@@ -311,25 +319,37 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
         for (int i = 0; i < NP; ++i) lx[tile][oct >> 1][i][16 * half + c + 32 * (oct & 1)] = x[i];
       }
       __builtin_amdgcn_wave_barrier();
-      gu32x4 qp[3];
+      if constexpr (BF16) {
+        // (the rows as they lie in LDS now: those without dz are zeros)
+        const any16 *own = (const any16 *)&lx[tile][col >> 4][0][16 * half + 4 * h + 32 * ((col >> 3) & 1)] + (col & 7);
+        gu32x4 q;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const gf32x4 dz = *(const gf32x4 *)&dzs[wave][8 * j + 4 * h];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          uint32_t p0, p1, p2;
-          const float a = dz[2 * i] != 0.0f ? dz[2 * i] * v[4 * j + 2 * i] : 0.0f;
-          const float b = dz[2 * i + 1] != 0.0f ? dz[2 * i + 1] * v[4 * j + 2 * i + 1] : 0.0f;
-          split2(a, b, p0, p1, p2);
-          qp[0][2 * j + i] = p0, qp[1][2 * j + i] = p1, qp[2][2 * j + i] = p2;
+        for (int i = 0; i < 4; ++i) {
+          const any16 *at = own + 8 * (8 * (i >> 1) + 2 * (i & 1));
+          q[i] = at[0] | (uint32_t)at[8] << 16;
         }
-      }
-      if constexpr (IN == 32) {
-#pragma unroll
-        for (int i = 0; i < 3; ++i) lq[tile][half][i][lane] = qp[i];
+        lq[tile][half][0][lane] = q;
       } else {
-        lq[tile][half][0][lane] = n < 16 ? qp[0] : qp[1];
-        lq[tile][half][1][lane] = n < 16 ? qp[2] : gu32x4{0, 0, 0, 0};
+        gu32x4 qp[3];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const gf32x4 dz = *(const gf32x4 *)&dzs[wave][8 * j + 4 * h];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            uint32_t p0, p1, p2;
+            const float a = dz[2 * i] != 0.0f ? dz[2 * i] * v[4 * j + 2 * i] : 0.0f;
+            const float b = dz[2 * i + 1] != 0.0f ? dz[2 * i + 1] * v[4 * j + 2 * i + 1] : 0.0f;
+            split2(a, b, p0, p1, p2);
+            qp[0][2 * j + i] = p0, qp[1][2 * j + i] = p1, qp[2][2 * j + i] = p2;
+          }
+        }
+        if constexpr (IN == 32) {
+#pragma unroll
+          for (int i = 0; i < 3; ++i) lq[tile][half][i][lane] = qp[i];
+        } else {
+          lq[tile][half][0][lane] = n < 16 ? qp[0] : qp[1];
+          lq[tile][half][1][lane] = n < 16 ? qp[2] : gu32x4{0, 0, 0, 0};
+        }
       }
     }
     __syncthreads();
@@ -359,25 +379,29 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          gu32x4 w[2][NA];   // pieces of what the unit makes of 8 rows: for dW1, dW2
+          gu32x4 w[2][3];   // pieces of what the unit makes of 8 rows: for dW1, dW2
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float a[2], e[2];
 #pragma unroll
             for (int o = 0; o < 2; ++o) {
-              const float gr = g[8 * j + 2 * i + o], s = sigmoid(gr);
-              a[o] = gr * s;
-              e[o] = u[8 * j + 2 * i + o] * fmaf(s, gr - a[o], s);   // u silu'(g)
+              const int r = 2 * i + o;
+              const float gr = g[8 * j + r], s = sigmoid(gr), si = gr * s;
+              e[o] = u[8 * j + r] * fmaf(s, gr - si, s);   // u silu'(g)
+              a[o] = si;
+              if constexpr (BF16) {
+                const float dz = dzs[2 * t + j][8 * (r >> 2) + 4 * h + (r & 3)];
+                e[o] *= dz;
+                a[o] *= dz;
+              }
             }
             uint32_t p0, p1, p2;
-            if constexpr (NA == 3) split2(e[0], e[1], p0, p1, p2);
-            else split2(e[0], e[1], p0, p1);
-            w[0][0][i] = p0, w[0][1][i] = p1;
-            if constexpr (NA == 3) w[0][2][i] = p2;
-            if constexpr (NA == 3) split2(a[0], a[1], p0, p1, p2);
-            else split2(a[0], a[1], p0, p1);
-            w[1][0][i] = p0, w[1][1][i] = p1;
-            if constexpr (NA == 3) w[1][2][i] = p2;
+            if constexpr (BF16) cut2(e[0], e[1], p0, p1, p2);
+            else split2(e[0], e[1], p0, p1, p2);
+            w[0][0][i] = p0, w[0][1][i] = p1, w[0][2][i] = p2;
+            if constexpr (BF16) cut2(a[0], a[1], p0, p1, p2);
+            else split2(a[0], a[1], p0, p1, p2);
+            w[1][0][i] = p0, w[1][1][i] = p1, w[1][2][i] = p2;
           }
           gu32x4 x[NQ];
 #pragma unroll
@@ -386,15 +410,18 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
             dw[0] = K::mfma(w[0][i], x[k], dw[0]);
             dw[1] = K::mfma(w[1][i], x[k], dw[1]);
           };
-          if constexpr (IN == 32) {
-            if constexpr (NA == 3) add(2, 0);
+          if constexpr (BF16) {
+            add(2, 0);
+            add(1, 0);
+          } else if constexpr (IN == 32) {
+            add(2, 0);
             add(1, 1);
             add(0, 2);
             add(1, 0);
             add(0, 1);
           } else {
             add(0, 1);
-            if constexpr (NA == 3) add(2, 0);
+            add(2, 0);
             add(1, 0);
           }
           add(0, 0);
@@ -430,7 +457,7 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       float v = dw[m][i];
-      if constexpr (IN == 16) v += __shfl_xor(v, 16);   // the features' second half of the columns
+      if constexpr (IN == 16 && !BF16) v += __shfl_xor(v, 16);   // the features' second half of the columns
       if (n < IN) own[(m * kGatedGroup + 8 * (i >> 2) + 4 * h + (i & 3)) * IN + n] = v;
     }
   if (hg == 0 && lane == 0) {
@@ -541,7 +568,7 @@ __global__ __launch_bounds__(512, 2) void k_gated_rows(GatedParams p) {
           const float *w3 = (const float *)w + 2 * KC * G::kFrag + 16 * h;
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            gu32x4 d[2][3];   // dg and du of 16 units in pieces (bf16: two, as in k_gated_sums)
+            gu32x4 d[2][3];   // dg and du of 16 units in pieces
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               float a[2], e[2];
@@ -552,11 +579,11 @@ __global__ __launch_bounds__(512, 2) void k_gated_rows(GatedParams p) {
                 a[o] = dy * si;
                 e[o] = dy * u[r] * fmaf(s, gr - si, s);
               }
-              uint32_t p0, p1, p2 = 0;
-              if constexpr (BF16) split2(e[0], e[1], p0, p1);
+              uint32_t p0, p1, p2;
+              if constexpr (BF16) cut2(e[0], e[1], p0, p1, p2);
               else split2(e[0], e[1], p0, p1, p2);
               d[0][0][i] = p0, d[0][1][i] = p1, d[0][2][i] = p2;
-              if constexpr (BF16) split2(a[0], a[1], p0, p1);
+              if constexpr (BF16) cut2(a[0], a[1], p0, p1, p2);
               else split2(a[0], a[1], p0, p1, p2);
               d[1][0][i] = p0, d[1][1][i] = p1, d[1][2][i] = p2;
             }
@@ -564,6 +591,7 @@ __global__ __launch_bounds__(512, 2) void k_gated_rows(GatedParams p) {
             for (int m = 0; m < 2; ++m) {
               auto add = [&](int i, int k) { acc[t] = Back<BF16, IN>::mfma(lt[blk][m][j][i][lane], d[m][k], acc[t]); };
               if constexpr (BF16) {
+                add(0, 2);
                 add(0, 1);
               } else if constexpr (IN == 32) {
                 add(2, 0);

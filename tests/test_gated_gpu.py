@@ -150,12 +150,6 @@ def backward(d, off, dz, dx=True, ldg=None, repeat=1):
     return r
 
 
-def bits(prec):
-    """bf16 heads sum what a unit makes of a row to 2^-18 of it, fp32 heads unrounded
-    (three exact pieces; the products left out are below 2^-25)."""
-    return 18 if prec == "bf16" else 25
-
-
 def check_grads(h, off, dz, got, prec, dx=True):
     with np.errstate(invalid="ignore"):
         for f in range(NFAM):
@@ -165,7 +159,7 @@ def check_grads(h, off, dz, got, prec, dx=True):
                     assert (got[k][f] == 0).all(), (k, f)
                 continue
             _, k = o.block(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], h["b3"][f])
-            want, err = o.gradients(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], dz[r], k, 16 + len(dz) // 128, bits(prec))
+            want, err = o.gradients(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], dz[r], k, 16 + len(dz) // 128)
             for key in ("w1", "w2", "w3", "b3"):
                 off_by = np.abs(got[key][f] - want[key])
                 assert (off_by <= err[key]).all(), (key, f, np.max(off_by / np.maximum(err[key], 1e-300)))
@@ -305,7 +299,7 @@ def check_loss(h, off, eta, weight, huber, got, grad=True, prec="f32"):
             continue
         sg = o.sigmoid(-zo)
         edz = share * (er * (sg + ez / 4) + slope * (ez / 4 + 8 * o.EPS * sg)) + 8 * o.EPS * np.abs(dz)
-        val, err = o.gradients(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], dz, k, 16 + len(eta) // 128, bits(prec))
+        val, err = o.gradients(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], dz, k, 16 + len(eta) // 128)
         # what an error of dz makes of the sums: their derivative by dz
         x = np.where(on[:, None], h["x"][r], 0.0)
         t = np.abs(k["s"] + k["a"] * (1 - k["s"])) * np.abs(k["u"]) * np.abs(h["w3"][f])
@@ -469,7 +463,7 @@ def test_rows_gradient_many_rows(prec, inp, hid):
             continue
         r = np.unique(np.concatenate([rng.integers(off[f], off[f + 1], 300), [off[f], off[f + 1] - 1]]))
         _, k = o.block(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], h["b3"][f])
-        want, err = o.gradients(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], dz.numpy()[r], k, 1, bits(prec))
+        want, err = o.gradients(h["x"][r], h["w1"][f], h["w2"][f], h["w3"][f], dz.numpy()[r], k, 1)
         # (bf16 rounds dg and du to 2^-18 before the sum over the units, and the result to 2^-8)
         extra = 2.0 ** -18 * (np.abs(dz.numpy()[r])[:, None] * (
             np.abs(h["w3"][f] * k["u"] * (k["s"] + k["a"] * (1 - k["s"]))) @ np.abs(h["w1"][f])
