@@ -22,7 +22,6 @@
 namespace ks {
 
 using gated::Block;
-using gated::cut2;
 using gated::gbf16x8;
 using gated::gf32x16;
 using gated::gf32x4;
@@ -193,7 +192,7 @@ __global__ __launch_bounds__(64 * N, 2) void k_gated_forward(GatedParams p) {
 // each of a unit's two terms.  (With dz x there too, six products, and two pieces of
 // the terms, within 2^-18 of each, 2M rows of 32-256 took 421 us and weight
 // gradients came out with 3e-6 where fp32 sums have 2e-6; with three pieces 530 us.
-// So 411 us.)
+// So 425 us, and 3e-7.)
 //
 // Which rows a lane's eight inner indices of dW stand for is free, as long as both
 // operands agree: those it has, 8 (i / 4) + 4 (its half) + i mod 4 of each 16.  With 16
@@ -204,8 +203,8 @@ __global__ __launch_bounds__(64 * N, 2) void k_gated_forward(GatedParams p) {
 // Vector work bounds it: 6 instructions, an exponential and a reciprocal for each gate
 // (bf16: 8) and 11 to split what it makes, for each 48 (bf16: 16) cycles of the matrix
 // unit.  A wave alone issues a vector instruction every 7.5 cycles, four per
-// SIMD one every 2.7 (FMA) to 5 (conversions: the pieces are cut off, not rounded,
-// where that is as good): hence 128 registers and 32 units per wave; and the 32x32x16
+// SIMD one every 2.7 (FMA) to 5 (conversions: pieces after the first are cut off, not rounded,
+// which is as good): hence 128 registers and 32 units per wave; and the 32x32x16
 // instruction runs beside them where 16x16x32 does not (two waves of each kind per
 // SIMD, multiplications: 888 cycles, alone 659 and 369; 16x16x32 671, alone 326 and
 // 369).  (64 units per wave, z exchanged between the unit groups and dz formed on the
@@ -396,11 +395,9 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
               }
             }
             uint32_t p0, p1, p2;
-            if constexpr (BF16) cut2(e[0], e[1], p0, p1, p2);
-            else split2(e[0], e[1], p0, p1, p2);
+            split2(e[0], e[1], p0, p1, p2);
             w[0][0][i] = p0, w[0][1][i] = p1, w[0][2][i] = p2;
-            if constexpr (BF16) cut2(a[0], a[1], p0, p1, p2);
-            else split2(a[0], a[1], p0, p1, p2);
+            split2(a[0], a[1], p0, p1, p2);
             w[1][0][i] = p0, w[1][1][i] = p1, w[1][2][i] = p2;
           }
           gu32x4 x[NQ];
@@ -580,11 +577,9 @@ __global__ __launch_bounds__(512, 2) void k_gated_rows(GatedParams p) {
                 e[o] = dy * u[r] * fmaf(s, gr - si, s);
               }
               uint32_t p0, p1, p2;
-              if constexpr (BF16) cut2(e[0], e[1], p0, p1, p2);
-              else split2(e[0], e[1], p0, p1, p2);
+              split2(e[0], e[1], p0, p1, p2);
               d[0][0][i] = p0, d[0][1][i] = p1, d[0][2][i] = p2;
-              if constexpr (BF16) cut2(a[0], a[1], p0, p1, p2);
-              else split2(a[0], a[1], p0, p1, p2);
+              split2(a[0], a[1], p0, p1, p2);
               d[1][0][i] = p0, d[1][1][i] = p1, d[1][2][i] = p2;
             }
 #pragma unroll
