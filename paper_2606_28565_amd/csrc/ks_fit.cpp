@@ -48,6 +48,14 @@ ks_status check_rows(const ks_heads *h, const ks_rows *r) {
 // takes at a time.  The split depends on
 // sizes alone, so results do not depend on the device.
 constexpr int64_t kFwdWgs = 1024;
+// The loss takes both passes in one launch up to about a workgroup per CU (and each
+// family's last one): a launch, the weights' way to the registers and dz's way through
+// memory are saved, but that kernel has two waves per SIMD, where the gradients alone
+// have four except with fp32 heads of 32 inputs.  fp32 16-64, 4099 rows: 16 us in one
+// launch, 19 in two; bf16 32-256, 32,000 rows 36 and 45, 100,000 rows 68 and 64,
+// 500,000 rows 184 and 161; fp32 32-256, 500,000 rows 260 and 298, 2,000,003 rows
+// 1148 and 1123.
+constexpr int32_t kOneLaunch = 256 + KS_NFAM;
 
 void plan(ks::GatedParams &p, const ks_heads *h, const ks_rows *r) {
   const int64_t tiles = (r->n_rows + 63) / 64;
@@ -62,15 +70,15 @@ void plan(ks::GatedParams &p, const ks_heads *h, const ks_rows *r) {
   }
 }
 
-// Workspace: the backward workgroups' sums, then (the loss) the forward
-// workgroups' sums and each row's dz.
+// Workspace: the backward workgroups' sums, then (the loss) the sums of those that
+// take the forward pass, and each row's dz.
 struct Room {
   size_t loss, dz, total;
 };
 Room room_of(const ks::GatedParams &p) {
   Room o;
   o.loss = align256((size_t)p.bwd_wg[KS_NFAM] * ks::gated_part_size(p.hidden, p.in_dim) * sizeof(float));
-  o.dz = o.loss + align256((size_t)p.fwd_wg[KS_NFAM] * 2 * sizeof(double));
+  o.dz = o.loss + align256((size_t)std::max(p.fwd_wg[KS_NFAM], p.bwd_wg[KS_NFAM]) * 2 * sizeof(double));
   o.total = o.dz + align256((size_t)p.fam_off[KS_NFAM] * sizeof(float));
   return o;
 }
@@ -184,7 +192,7 @@ ks_status ks_gated_backward(const ks_heads *heads, const ks_rows *rows, const fl
   p.dz = dz;
   p.part = static_cast<float *>(ws);
   if (p.g_w1) {
-    hipError_t e = ks::launch_gated_sums(p, stream);
+    hipError_t e = ks::launch_gated_sums(p, false, stream);
     if (e == hipSuccess) e = ks::launch_gated_reduce(p, stream);
     if (e != hipSuccess) return hip_error(e, "gated backward launch");
   }
@@ -222,10 +230,12 @@ ks_status ks_gated_loss(const ks_heads *heads, const ks_rows *rows, const ks_eta
   p.loss = loss;
   p.loss_part = reinterpret_cast<double *>(w + room.loss);
   p.part = reinterpret_cast<float *>(w);
-  if (p.g_w1) p.dz_out = reinterpret_cast<float *>(w + room.dz);
+  const bool one = p.g_w1 && p.bwd_wg[KS_NFAM] <= kOneLaunch;
+  std::memcpy(p.loss_wg, one ? p.bwd_wg : p.fwd_wg, sizeof p.loss_wg);
+  if (p.g_w1 && !one) p.dz_out = reinterpret_cast<float *>(w + room.dz);
   p.dz = p.dz_out;
-  hipError_t e = ks::launch_gated_forward(p, stream);
-  if (e == hipSuccess && p.g_w1) e = ks::launch_gated_sums(p, stream);
+  hipError_t e = one ? hipSuccess : ks::launch_gated_forward(p, stream);
+  if (e == hipSuccess && p.g_w1) e = ks::launch_gated_sums(p, one, stream);
   if (e == hipSuccess) e = ks::launch_gated_reduce(p, stream);
   return hip_error(e, "gated loss launch");
 }

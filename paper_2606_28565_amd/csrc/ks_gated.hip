@@ -3,6 +3,7 @@
 //
 //   k_gated_forward   z, and for a fit the loss sums and dz of each row
 //   k_gated_sums      weight gradients of a workgroup's rows, held in registers
+//                     (for few rows with the loss's forward pass)
 //   k_gated_rows      gradients of the rows
 //   k_gated_reduce    sums of the workgroups' gradients in a fixed order
 //
@@ -224,14 +225,21 @@ struct Back {
   }
 };
 
-template <bool BF16, int IN>
-__global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(GatedParams p) {
+//
+// LOSS: the loss's forward pass in the same launch, for few rows (one step each) and
+// for fp32 heads of 32 inputs.  A wave's weights are the row operand there: a lane
+// then holds 16 of its units for one row, adds up their part of z, and the unit groups'
+// parts meet in LDS.
+template <bool BF16, int IN, bool LOSS>
+__global__ __launch_bounds__(512, (!LOSS && (BF16 || IN == 16) ? 4 : 2)) void k_gated_sums(GatedParams p) {
   using K = Back<BF16, IN>;
   constexpr int KC = K::KC, W = K::W, NP = K::NP, NQ = K::NQ, R = 16 * W;   // rows of a step
   constexpr int kTiles = R / 32;
   constexpr int kX = kTiles * KC * NP * 64 * 4, kQ = kTiles * 2 * NQ * 64 * 4, kJoin = (W - 1) * 16 * 64;
   __shared__ __align__(16) uint32_t lds[kX + kQ > kJoin ? kX + kQ : kJoin];
   __shared__ __align__(16) float dzs[W][16];
+  __shared__ float w3s[LOSS ? 256 : 1], zs[LOSS ? W : 1][LOSS ? R : 1];   // [unit group]: its part of z
+  double sum = 0.0, total = 0.0;
   gu32x4(*lx)[KC][NP][64] = reinterpret_cast<gu32x4(*)[KC][NP][64]>(lds);          // [tile]: rows
   gu32x4(*lq)[2][NQ][64] = reinterpret_cast<gu32x4(*)[2][NQ][64]>(lds + kX);       // [tile][16 rows]: dz x
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, c = lane & 15;
@@ -276,7 +284,7 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
     if (mine + 16 <= end) {
       const char *x = (const char *)p.x + mine * ld * E;
       load8<BF16>(raw, x + off_row, 0, p.vec);
-      dzc = p.dz[mine + c];
+      dzc = LOSS ? 0.0f : p.dz[mine + c];
       if constexpr (!BF16) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = element<BF16>(x + (size_t)(8 * (i >> 2) + (i & 3)) * ld * E + off_col, 0);
@@ -285,7 +293,7 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
       const int64_t base = mine < end ? mine : end - 1;
       const int last = (int)(end - base) - 1;
       load8<BF16>(raw, p.x, (base + min(c, last)) * ld + (brings ? 8 * oct : 0), p.vec);
-      dzc = p.dz[base + min(c, last)];
+      dzc = LOSS ? 0.0f : p.dz[base + min(c, last)];
       if constexpr (!BF16) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -295,13 +303,69 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
     }
   };
   // (a step's rows are on their way while the step before is worked on; fp32 with 16
-  // inputs has no registers left for them)
-  constexpr bool kAhead = BF16 || IN == 32;
+  // inputs has no registers left for them, and a LOSS has one step otherwise)
+  constexpr bool kAhead = BF16 ? !LOSS : IN == 32;
   if (kAhead) fetch(begin + 16 * wave);
+  if (LOSS && threadIdx.x < 256)
+    w3s[threadIdx.x] = (int)threadIdx.x < p.hidden ? element<BF16>(p.w3, (int64_t)f * p.hidden + threadIdx.x) : 0.0f;
 #pragma unroll 1
   for (int64_t row0 = begin; row0 < end; row0 += R) {
     if (!kAhead) fetch(row0 + 16 * wave);
     __syncthreads();   // (the step before is done with the room)
+    auto put = [&]() {
+      gu32x4 x[NP];
+      K::pieces(raw, x);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) lx[tile][oct >> 1][i][16 * half + c + 32 * (oct & 1)] = x[i];
+    };
+    if constexpr (LOSS) {
+      const int64_t row = row0 + 16 * wave + c;
+      const bool in = row < end;
+      const float eta = p.eta[in ? row : end - 1], wt = p.weight ? p.weight[in ? row : end - 1] : 1.0f;
+      if (brings) put();
+      __syncthreads();
+      if (works) {
+#pragma unroll 1
+        for (int t = rg; t < kTiles; t += RG) {
+          if (row0 + 32 * t >= end) break;
+          gf32x16 g = {}, u = {};
+#pragma unroll
+          for (int k = 0; k < KC; ++k) {
+            auto both = [&](int i, int j) {
+              g = K::mfma(wgt[0][k][j], lx[t][k][i][lane], g);
+              u = K::mfma(wgt[1][k][j], lx[t][k][i][lane], u);
+            };
+            if constexpr (!BF16) {
+              both(2, 0);
+              both(1, 1);
+              both(0, 2);
+              both(1, 0);
+              both(0, 1);
+            }
+            both(0, 0);
+          }
+          float z = 0.0f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            z = fmaf(g[r] * sigmoid(g[r]) * u[r], w3s[hg * kGatedGroup + 8 * (r >> 2) + 4 * h + (r & 3)], z);
+          z += __shfl_xor(z, 32);
+          if (h == 0) zs[hg][32 * t + n] = z;
+        }
+      }
+      __syncthreads();
+      float z = element<BF16>(p.b3, f);
+      for (int i = 0; i < HG; ++i) z += zs[i][16 * wave + c];
+      const bool counts = in && eta > 0.0f && eta < __builtin_inff() && wt > 0.0f && wt < __builtin_inff();
+      const EtaTerm e = eta_term(z, eta, wt, p.huber);
+      dzc = counts ? e.dz : 0.0f;
+      if (oct == 0) {
+        if (in && p.z) p.z[row] = z;
+        if (counts) {
+          sum += (double)e.loss;
+          total += (double)wt;
+        }
+      }
+    }
     {
       // (a row whose dz is 0 adds nothing, whatever it holds)
       const bool on = dzc != 0.0f;
@@ -309,13 +373,10 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
         d0 += dzc;
         dzs[wave][c] = dzc;
       }
-      if (brings) {
+      if (brings && !(LOSS && on)) {
 #pragma unroll
         for (auto &r : raw) r = on ? r : gu32x4{0, 0, 0, 0};
-        gu32x4 x[NP];
-        K::pieces(raw, x);
-#pragma unroll
-        for (int i = 0; i < NP; ++i) lx[tile][oct >> 1][i][16 * half + c + 32 * (oct & 1)] = x[i];
+        put();
       }
       __builtin_amdgcn_wave_barrier();
       if constexpr (BF16) {
@@ -426,8 +487,20 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
       }
     }
   }
-  // db3, and the row groups' sums onto the first's in order (in the same room)
+  // db3, the loss, and the row groups' sums onto the first's in order (in the same room)
   __shared__ float d0s[W];
+  __shared__ double loss[LOSS ? W : 1][2];
+  if constexpr (LOSS) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      sum += __shfl_xor(sum, d);
+      total += __shfl_xor(total, d);
+    }
+    if (lane == 0) {
+      loss[wave][0] = sum;
+      loss[wave][1] = total;
+    }
+  }
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) d0 += __shfl_xor(d0, d);
   if (lane == 0) d0s[wave] = d0;
@@ -461,6 +534,14 @@ __global__ __launch_bounds__(512, (BF16 || IN == 16 ? 4 : 2)) void k_gated_sums(
     float v = 0.0f;
     for (int i = 0; i < W; ++i) v += d0s[i];
     out[gated_part_size(p.hidden, IN) - 1] = v;
+    if constexpr (LOSS) {
+      for (int i = 1; i < W; ++i) {
+        sum += loss[i][0];
+        total += loss[i][1];
+      }
+      p.loss_part[2 * wg] = sum;
+      p.loss_part[2 * wg + 1] = total;
+    }
   }
 }
 
@@ -679,7 +760,7 @@ __global__ __launch_bounds__(kThreads) void k_gated_reduce(GatedParams p, int ch
   if (p.eta) {
     __shared__ double ls[kThreads][2];
     double a = 0.0, b = 0.0;
-    for (int w = p.fwd_wg[f] + (int)threadIdx.x; w < p.fwd_wg[f + 1]; w += kThreads) {
+    for (int w = p.loss_wg[f] + (int)threadIdx.x; w < p.loss_wg[f + 1]; w += kThreads) {
       a += p.loss_part[2 * w];
       b += p.loss_part[2 * w + 1];
     }
@@ -740,16 +821,22 @@ hipError_t launch_gated_forward(const GatedParams &p, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_gated_sums(const GatedParams &p, hipStream_t s) {
+template <bool LOSS>
+static void sums_of(const GatedParams &p, hipStream_t s) {
   const dim3 grid(p.bwd_wg[KS_NFAM]), block(512);
-  if (grid.x == 0) return hipSuccess;
   if (p.bf16) {
-    if (p.in_dim == 16) hipLaunchKernelGGL((k_gated_sums<true, 16>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((k_gated_sums<true, 32>), grid, block, 0, s, p);
+    if (p.in_dim == 16) hipLaunchKernelGGL((k_gated_sums<true, 16, LOSS>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((k_gated_sums<true, 32, LOSS>), grid, block, 0, s, p);
   } else {
-    if (p.in_dim == 16) hipLaunchKernelGGL((k_gated_sums<false, 16>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((k_gated_sums<false, 32>), grid, block, 0, s, p);
+    if (p.in_dim == 16) hipLaunchKernelGGL((k_gated_sums<false, 16, LOSS>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((k_gated_sums<false, 32, LOSS>), grid, block, 0, s, p);
   }
+}
+
+hipError_t launch_gated_sums(const GatedParams &p, bool loss, hipStream_t s) {
+  if (p.bwd_wg[KS_NFAM] == 0) return hipSuccess;
+  if (loss) sums_of<true>(p, s);
+  else sums_of<false>(p, s);
   return hipGetLastError();
 }
 

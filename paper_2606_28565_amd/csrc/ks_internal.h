@@ -306,7 +306,8 @@ struct GatedParams {
   const float *eta, *weight;
   float huber;
   float *dz_out;                     // w drho/dz, not yet over sum w; null: the loss alone
-  double *loss_part;                 // [forward workgroups][2]: sum w rho, sum w
+  int32_t loss_wg[KS_NFAM + 1];      // the workgroups that take the forward pass
+  double *loss_part;                 // of each of them: sum w rho, sum w
   float *loss;                       // [KS_NFAM]
   // gradients
   const float *dz;
@@ -323,7 +324,7 @@ constexpr int gated_part_size(int hidden, int in_dim) {
   return (hidden + kGatedGroup - 1) / kGatedGroup * kGatedGroup * 2 * in_dim + 1;
 }
 hipError_t launch_gated_forward(const GatedParams &p, hipStream_t s);
-hipError_t launch_gated_sums(const GatedParams &p, hipStream_t s);
+hipError_t launch_gated_sums(const GatedParams &p, bool loss, hipStream_t s);
 hipError_t launch_gated_rows(const GatedParams &p, hipStream_t s);     // g_x
 hipError_t launch_gated_reduce(const GatedParams &p, hipStream_t s);   // gradients and the loss
 

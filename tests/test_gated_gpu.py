@@ -358,6 +358,22 @@ def test_rows_that_do_not_count(prec, hid):
     check_loss(h, off, eta, weight, 0.5, got, prec=prec)
 
 
+@pytest.mark.parametrize("n", [33_000, 36_000])
+@pytest.mark.parametrize("prec,inp,hid", [("f32", 16, 64), ("f32", 32, 140), ("bf16", 16, 33), ("bf16", 32, 256)])
+def test_loss_beside_the_switch_to_two_launches(n, prec, inp, hid):
+    """Row counts on both sides of the switch, every ninth row never measured and
+    without features."""
+    import torch
+    d, h, off = make(n, prec, inp, hid)
+    eta, weight = targets(n)
+    eta[4::9] = float("nan")
+    d["x"][torch.arange(4, n, 9).cuda()] = float("nan")
+    h["x"][4::9] = float("nan")
+    got = run_loss(d, off, eta.cuda(), weight.cuda(), 0.4)
+    assert np.isnan(got[1][4::9]).all() and np.isfinite(np.delete(got[1], np.arange(4, n, 9))).all()
+    check_loss(h, off, eta, weight, 0.4, got, prec=prec)
+
+
 def test_loss_alone_is_the_same_loss():
     """The loss without gradients comes from another kernel, which adds a row's units
     in another order (32 of a lane's registers at a time instead of 16 lanes): each sum
