@@ -193,7 +193,7 @@ __global__ __launch_bounds__(64 * N, 2) void k_gated_forward(GatedParams p) {
 // each of a unit's two terms.  (With dz x there too, six products, and two pieces of
 // the terms, within 2^-18 of each, 2M rows of 32-256 took 421 us and weight
 // gradients came out with 3e-6 where fp32 sums have 2e-6; with three pieces 530 us.
-// So 425 us, and 3e-7.)
+// So 417 to 433 us, and 3e-7.)
 //
 // Which rows a lane's eight inner indices of dW stand for is free, as long as both
 // operands agree: those it has, 8 (i / 4) + 4 (its half) + i mod 4 of each 16.  With 16
@@ -202,14 +202,15 @@ __global__ __launch_bounds__(64 * N, 2) void k_gated_forward(GatedParams p) {
 // the sum of the two halves; bf16 heads have no use for the second.
 //
 // Vector work bounds it: 6 instructions, an exponential and a reciprocal for each gate
-// (bf16: 8) and 11 to split what it makes, for each 48 (bf16: 16) cycles of the matrix
-// unit.  A wave alone issues a vector instruction every 7.5 cycles, four per
-// SIMD one every 2.7 (FMA) to 5 (conversions: pieces after the first are cut off, not rounded,
-// which is as good): hence 128 registers and 32 units per wave; and the 32x32x16
-// instruction runs beside them where 16x16x32 does not (two waves of each kind per
-// SIMD, multiplications: 888 cycles, alone 659 and 369; 16x16x32 671, alone 326 and
-// 369).  (64 units per wave, z exchanged between the unit groups and dz formed on the
-// way, one pass in all: 776 us, where this and k_gated_forward take 585.)
+// (bf16: 8) and 11 to make what it makes into pieces, for each 48 (bf16: 16) cycles of
+// the matrix unit: 2M rows of bf16 32-256, the vector units 93% and the matrix units 30%
+// busy.  A wave alone issues a vector instruction every 7.5 cycles, four per SIMD one
+// every 2.7 (FMA) to 5 (conversions; so only the first piece is one): hence 128
+// registers and 32 units per wave; and the 32x32x16 instruction runs beside them where
+// 16x16x32 does not (two waves of each kind per SIMD, multiplications: 888 cycles, alone
+// 659 and 369; 16x16x32 671, alone 326 and 369).  (64 units per wave, z exchanged between
+// the unit groups and dz formed on the way, one pass in all: 776 us, where this and
+// k_gated_forward take 600.)
 template <bool BF16, int IN>
 struct Back {
   static constexpr int KC = IN / 16, W = 8;
@@ -225,7 +226,6 @@ struct Back {
   }
 };
 
-//
 // LOSS: the loss's forward pass in the same launch, for few rows (one step each) and
 // for fp32 heads of 32 inputs.  A wave's weights are the row operand there: a lane
 // then holds 16 of its units for one row, adds up their part of z, and the unit groups'
