@@ -40,34 +40,41 @@ ks_status check_rows(const ks_heads *h, const ks_rows *r) {
   return KS_OK;
 }
 
-// Rows over workgroups.  Forward: four waves of 64 rows at a time; about 1024
-// workgroups (two per CU and one to follow each), so that the weights' way into
-// LDS is paid for by several tiles where there are many, and one pass of the four
-// waves each where there are few.  Backward: about 512 workgroups (two per CU are
-// resident; one with fp32 heads of 32 inputs, 256 then), each at least the rows it
-// takes at a time.  The split depends on
-// sizes alone, so results do not depend on the device.
-constexpr int64_t kFwdWgs = 1024;
+// Rows over workgroups; the split depends on sizes alone, so results do not depend on
+// the device.  Gradients: all workgroups resident at once, families' last ones
+// included, so that each brings its weights once and none waits for another to end; two
+// per CU, or one for the rows' and with fp32 heads of 32 inputs (with multiples of 128
+// rows and remainders on top, 1,000,003 rows of fp32 32-256 took 427 us, so 363; 65,536
+// rows 64, so 46).  Forward the same where the weights leave room for one workgroup per
+// CU (fp32, 32 inputs, over 128 units: 163 us, so 154; 100,003 rows 31, so 23), else
+// about 1024 (three or four per CU; three of fp32 16-256: 109 us, 113 with 768).
 // The loss takes both passes in one launch up to about a workgroup per CU (and each
 // family's last one): a launch, the weights' way to the registers and dz's way through
 // memory are saved, but that kernel has two waves per SIMD, where the gradients alone
 // have four except with fp32 heads of 32 inputs.  fp32 16-64, 4099 rows: 16 us in one
 // launch, 19 in two; bf16 32-256, 32,000 rows 36 and 45, 100,000 rows 68 and 64,
-// 500,000 rows 184 and 161; fp32 32-256, 500,000 rows 260 and 298, 2,000,003 rows
-// 1148 and 1123.
+// 500,000 rows 184 and 161; fp32 32-256, 500,000 rows 261 and 297, 2,000,003 rows
+// 976 and 1000.
 constexpr int32_t kOneLaunch = 256 + KS_NFAM;
 
-void plan(ks::GatedParams &p, const ks_heads *h, const ks_rows *r) {
-  const int64_t tiles = (r->n_rows + 63) / 64;
-  p.fwd_tiles = (int32_t)(4 * std::max<int64_t>(1, (tiles + 4 * kFwdWgs - 1) / (4 * kFwdWgs)));
-  const int64_t unit = ks::kGatedStep, wgs = h->precision == KS_F32 && h->in_dim == 32 ? 256 : 512;
-  p.bwd_rows = (int32_t)(unit * std::max<int64_t>(1, (r->n_rows + unit * wgs - 1) / (unit * wgs)));
-  p.fwd_wg[0] = p.bwd_wg[0] = 0;
-  for (int f = 0; f < KS_NFAM; ++f) {
-    const int64_t n = r->fam_off[f + 1] - r->fam_off[f];
-    p.fwd_wg[f + 1] = p.fwd_wg[f] + (int32_t)((n + 64 * p.fwd_tiles - 1) / (64 * p.fwd_tiles));
-    p.bwd_wg[f + 1] = p.bwd_wg[f] + (int32_t)((n + p.bwd_rows - 1) / p.bwd_rows);
+// The least rows a workgroup takes, a multiple of unit and at least least, with which
+// wgs workgroups (or one per family) are enough; off: their numbers.
+int32_t split(const ks_rows *r, int64_t least, int64_t unit, int64_t wgs, int32_t (&off)[KS_NFAM + 1]) {
+  int64_t rows = std::max(least, ((r->n_rows + wgs - 1) / wgs + unit - 1) / unit * unit);
+  for (;; rows += unit) {
+    off[0] = 0;
+    for (int f = 0; f < KS_NFAM; ++f) off[f + 1] = off[f] + (int32_t)((r->fam_off[f + 1] - r->fam_off[f] + rows - 1) / rows);
+    if (off[KS_NFAM] <= wgs) return (int32_t)rows;
   }
+}
+
+void plan(ks::GatedParams &p, const ks_heads *h, const ks_rows *r) {
+  const bool wide = h->precision == KS_F32 && h->in_dim == 32;
+  p.fwd_tiles = split(r, 256, 256, wide && h->hidden > 128 ? 256 : 1024, p.fwd_wg) / 64;   // 64 rows for each of four waves
+  // 32 rows for each of its row groups, a step at least
+  const int groups = (h->hidden + ks::kGatedGroup - 1) / ks::kGatedGroup, row_groups = groups > 4 ? 1 : groups > 2 ? 2 : 4;
+  p.bwd_rows = split(r, ks::kGatedStep, 32 * row_groups, wide ? 256 : 512, p.bwd_wg);
+  p.row_rows = split(r, 256, 256, 256, p.row_wg);   // 32 rows for each of its eight waves
 }
 
 // Workspace: the backward workgroups' sums, then (the loss) the sums of those that

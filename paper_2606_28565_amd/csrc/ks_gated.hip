@@ -565,10 +565,10 @@ __global__ __launch_bounds__(512, 2) void k_gated_rows(GatedParams p) {
   __shared__ __align__(16) gu32x4 lt[HID / 32][2][2][NT][64];   // [32 units][W1, W2][16 units]
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wg = blockIdx.x, f = family_of(p.fwd_wg, wg);
-  const int64_t begin = p.fam_off[f] + (int64_t)(wg - p.fwd_wg[f]) * p.fwd_tiles * 64;
+  const int wg = blockIdx.x, f = family_of(p.row_wg, wg);
+  const int64_t begin = p.fam_off[f] + (int64_t)(wg - p.row_wg[f]) * p.row_rows;
   const int64_t fam_end = p.fam_off[f + 1];
-  const int64_t end = begin + (int64_t)p.fwd_tiles * 64 < fam_end ? begin + (int64_t)p.fwd_tiles * 64 : fam_end;
+  const int64_t end = begin + p.row_rows < fam_end ? begin + p.row_rows : fam_end;
   const int parts = (p.hidden + HID - 1) / HID;
   for (int64_t row0 = begin; row0 < end; row0 += 32 * T * W) {
     gf32x16 acc[T] = {};
@@ -841,7 +841,7 @@ hipError_t launch_gated_sums(const GatedParams &p, bool loss, hipStream_t s) {
 }
 
 hipError_t launch_gated_rows(const GatedParams &p, hipStream_t s) {
-  const dim3 grid(p.fwd_wg[KS_NFAM]), block(512);
+  const dim3 grid(p.row_wg[KS_NFAM]), block(512);
   if (grid.x == 0) return hipSuccess;
   if (p.bf16) {
     if (p.in_dim == 16) hipLaunchKernelGGL((k_gated_rows<true, 16>), grid, block, 0, s, p);

@@ -290,7 +290,7 @@ hipError_t launch_validate(const ValidateParams &p, hipStream_t s);
 
 // ---- gated heads over rows (ks_gated.hip)
 // A forward workgroup takes fwd_tiles 64-row tiles of one family, a backward
-// workgroup bwd_rows rows of one (a multiple of kGatedStep).
+// workgroup bwd_rows rows of one, one for the rows' gradients row_rows.
 struct GatedParams {
   const void *x;
   int64_t ldx;
@@ -299,8 +299,8 @@ struct GatedParams {
   int32_t in_dim, hidden;
   bool bf16;
   const void *w1, *w2, *w3, *b3;
-  int32_t fwd_tiles, bwd_rows;
-  int32_t fwd_wg[KS_NFAM + 1], bwd_wg[KS_NFAM + 1];
+  int32_t fwd_tiles, bwd_rows, row_rows;
+  int32_t fwd_wg[KS_NFAM + 1], bwd_wg[KS_NFAM + 1], row_wg[KS_NFAM + 1];
   float *z;                          // nullable
   // the loss (eta null: none)
   const float *eta, *weight;
