@@ -68,6 +68,13 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t &p0, uint32_t 
   p2 = pack_upper(a, b);
 }
 
+// 1 + e^-z: the exponent's rounding, 2^-24 of |z| log2 e, is put back to first order
+__device__ __forceinline__ float eta_of(float z) {
+  constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+  const float t = z * -kLog2e, lo = fmaf(z, -kLog2e, -t) - z * 1.92596299e-8f, e = __builtin_amdgcn_exp2f(t);
+  return 1.0f + (fabsf(z) < 80.0f ? fmaf(e * kLn2, lo, e) : e);
+}
+
 // HID: the widest block that fits the LDS room (any narrower one too)
 template <bool BF16, int IN, int HID>
 struct Block {
@@ -186,12 +193,15 @@ struct Block {
         products(blk + (KC + kc) * kFrag, lane, x, kc, u);
       }
       const float *w3 = (const float *)blk + 2 * KC * kFrag + (lane >> 5) * 16;
+      float y[2] = {0.0f, 0.0f};   // (of a block by itself: 16 + 8 additions in a row for 256 units, not 128)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float w = w3[r];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) z[i] = fmaf(w, g[i][r] * sigmoid(g[i][r]) * u[i][r], z[i]);
+        for (int i = 0; i < 2; ++i) y[i] = fmaf(w, g[i][r] * sigmoid(g[i][r]) * u[i][r], y[i]);
       }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) z[i] += y[i];
     }
     // lanes 32.. of the first block's sums for lanes ..31 of the second's
     const auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, z[0]), __builtin_bit_cast(uint32_t, z[1]),

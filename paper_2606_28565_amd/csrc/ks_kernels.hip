@@ -1436,6 +1436,9 @@ struct HeadGated {
   }
 };
 
+template <class H> struct IsGated { static constexpr bool value = false; };
+template <bool BF16, int IN, int HID> struct IsGated<HeadGated<BF16, IN, HID>> { static constexpr bool value = true; };
+
 struct HeadOne {
   static constexpr int LDS_DW = 1;
   static constexpr bool kMlp = false;
@@ -2115,7 +2118,8 @@ __global__ __launch_bounds__(kWgThreads, MinWg<KIND>::value) void k_eval(EvalPar
             float x[IN];
             features<IN, H::kRaw>(rc, sc, o, x);
             const float z = H::mlp(x, lds);
-            eta = 1.0f + __expf(-z);
+            if constexpr (IsGated<H>::value) eta = gated::eta_of(z);
+            else eta = 1.0f + __expf(-z);
           }
         }
       }

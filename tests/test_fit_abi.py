@@ -124,6 +124,25 @@ def test_workspace():
         assert abi.ks_gated_loss(h, r, t, A, None, g, ws, size, None, check=False) == abi.KS_EWORKSPACE
 
 
+@pytest.mark.parametrize("prec", [abi.KS_F32, abi.KS_BF16])
+@pytest.mark.parametrize("hid,inp", [(1, 16), (96, 32), (129, 32), (256, 16)])
+def test_workspace_of_any_split(prec, hid, inp):
+    """Rows over the families in any way, up to the most there may be: the room is
+    that of at most 512 workgroups' sums (1024 of the forward pass), and each row's dz."""
+    h = heads(hidden=hid, in_dim=inp, precision=prec)
+    part = 4 * ((hid + 31) // 32 * 32 * 2 * inp + 1)
+    rng = np.random.default_rng(5)
+    for n in (0, 1, 9, 127, 128, 129, 5120, 65536, 65537, 131072, 10**6, (1 << 31) - 1):
+        for k in range(4):
+            r = rows(n, ldx=inp)
+            cut = np.sort(rng.integers(0, n + 1, NFAM - 1)) if k < 2 else np.full(NFAM - 1, n if k == 2 else 0)
+            for f in range(1, NFAM):
+                r.fam_off[f] = int(cut[f - 1])
+            r.fam_off[NFAM] = n
+            need = abi.ks_gated_workspace_bytes(h, r)
+            assert 4 * n <= need - (256 if n == 0 else 0) <= 512 * part + 1024 * 16 + 4 * n + 3 * 256, (n, k)
+
+
 def test_bad_gradients():
     h, r, big = heads(), rows(), 1 << 40
 
