@@ -17,8 +17,8 @@
 // cycles, alone 659 and 369; 16x16x4 fp32 940, alone 578 and 367), and the vector work
 // is what bounds this block: an exponential, a reciprocal and five more per gate.
 //
-// 2M rows of bf16 32-256: 175 us, the vector units 81% busy.  1M rows of fp32 32-256:
-// 169 us (six products at the rate of a large bf16 product: 159; on the fp32
+// 2M rows of bf16 32-256: 165 us, the vector units 91% busy.  1M rows of fp32 32-256:
+// 158 us (six products at the rate of a large bf16 product: 159; on the fp32
 // instruction it took 305).
 #pragma once
 

@@ -193,7 +193,7 @@ __global__ __launch_bounds__(64 * N, 2) void k_gated_forward(GatedParams p) {
 // each of a unit's two terms.  (With dz x there too, six products, and two pieces of
 // the terms, within 2^-18 of each, 2M rows of 32-256 took 421 us and weight
 // gradients came out with 3e-6 where fp32 sums have 2e-6; with three pieces 530 us.
-// So 417 to 433 us, and 3e-7.)
+// So 402 to 424 us, and 3e-7.)
 //
 // Which rows a lane's eight inner indices of dW stand for is free, as long as both
 // operands agree: those it has, 8 (i / 4) + 4 (its half) + i mod 4 of each 16.  With 16
@@ -210,7 +210,7 @@ __global__ __launch_bounds__(64 * N, 2) void k_gated_forward(GatedParams p) {
 // 16x16x32 does not (two waves of each kind per SIMD, multiplications: 888 cycles, alone
 // 659 and 369; 16x16x32 671, alone 326 and 369).  (64 units per wave, z exchanged between
 // the unit groups and dz formed on the way, one pass in all: 776 us, where this and
-// k_gated_forward take 600.)
+// k_gated_forward take 570.)
 template <bool BF16, int IN>
 struct Back {
   static constexpr int KC = IN / 16, W = 8;
@@ -555,7 +555,7 @@ __global__ __launch_bounds__(512, (!LOSS && (BF16 || IN == 16) ? 4 : 2)) void k_
 // instruction's 32 rows are the features twice, against the first and the second piece
 // of an fp32 weight (then the third and nothing).
 //
-// (100,003 rows of fp32 32-67 on the fp32 instruction: 32 us; so 26 us.)
+// (100,003 rows of fp32 32-67 on the fp32 instruction: 32 us; so 24 us.)
 template <bool BF16, int IN>
 __global__ __launch_bounds__(512, 2) void k_gated_rows(GatedParams p) {
   constexpr int HID = 128, E = BF16 ? 2 : 4, W = 8, T = 2;
