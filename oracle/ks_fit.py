@@ -22,8 +22,8 @@ def block(x, w1, w2, w3, b3):
     """One family's rows: z and a dict of what the gradients need.  "err": bounds
     on the fp32 error of g, u, s, a and z.
 
-    A projection of D products: (D + 1) roundings of partial sums below the sum of
-    magnitudes.  s = 1 / (1 + 2^(-g log2 e)): the exponent is rounded twice (the
+    A projection of D products: D roundings of partial sums below the sum of
+    magnitudes, and 2^-24 of each product (pieces left out).  s = 1 / (1 + 2^(-g log2 e)): the exponent is rounded twice (the
     constant and the product: relative 2 EPS of |g| log2 e, a relative
     2 |g| EPS of e^-g), the exponential and the reciprocal are within 2 EPS (one unit
     of the last place), the sum within EPS; the exponential's error counts (1 - s)."""
@@ -46,7 +46,8 @@ def gradients(x, w1, w2, w3, dz, k, terms):
     """Gradients of sum dz z from ``block``'s dict k: w1, w2, w3, b3, x, and bounds on
     their fp32 errors.  terms: additions in fp32 that one sum over rows goes through
     in a row.  What a unit makes of a row is summed in three exact pieces; the products
-    of pieces left out are below 2^-25 of it.  Rows whose dz is 0 add nothing, whatever
+    of pieces left out are at most 2 2^-9 2^-16 = 2^-24 of it (a second piece is at most
+    2^-9 of the number, the third 2^-7 of the second).  Rows whose dz is 0 add nothing, whatever
     they hold."""
     dz = np.asarray(dz, np.float64)
     on = dz != 0
@@ -63,7 +64,7 @@ def gradients(x, w1, w2, w3, dz, k, terms):
     edg = np.abs(dy) * (e0["u"] * np.abs(t) + np.abs(u) * et + e0["u"] * et) + 6 * EPS * np.abs(dg)
     val = {"w1": dg.T @ x, "w2": du.T @ x, "w3": (dz[:, None] * y).sum(0), "b3": dz.sum(), "x": dg @ w1 + du @ w2}
     ax, H = np.abs(x), w1.shape[0]
-    long = (terms + 8) * EPS + 2.0 ** -25
+    long = (terms + 8) * EPS + 2.0 ** -24
     # (dw3 may come as W2 . sum dz a x: its terms are dW2's, weighted)
     err = {"w1": edg.T @ ax + long * (np.abs(dg).T @ ax), "w2": edu.T @ ax + long * (np.abs(du).T @ ax),
            "w3": (((np.abs(dz)[:, None] * (e0["a"] + (4 * EPS + long) * np.abs(a))).T @ ax) * np.abs(w2)).sum(1),

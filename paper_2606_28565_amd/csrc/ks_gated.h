@@ -11,7 +11,9 @@
 //
 // fp32 operands are split into three bf16 pieces that sum to them exactly (from
 // 2^-102 up; below, what is lost is under 2^-126) and the six products of the
-// largest pieces are taken: the three left out are below 2^-25 of the product.
+// largest pieces are taken: the three left out are at most 2^-24 of the product (the
+// second piece is at most 2^-9 of the number and the third 2^-16), its own rounding in
+// fp32.
 // The bf16 instruction runs beside other waves' vector work, most of the way; the fp32
 // one does not (two waves of each per SIMD: 32x32x16 bf16 and multiplications take 888
 // cycles, alone 659 and 369; 16x16x4 fp32 940, alone 578 and 367), and the vector work
