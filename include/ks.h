@@ -502,7 +502,9 @@ size_t ks_gated_workspace_bytes(const ks_heads *heads, const ks_rows *rows);
  *   dw3 = dz a u, db3 = dz, du = dz w3 a, dg = dz w3 u (s + a (1 - s)),
  *   dW1 = dg x^T, dW2 = du x^T, dx = W1^T dg + W2^T du.
  * A row whose dz is 0 adds nothing, whatever its features, and its dx is 0.
- * Sums are formed in a fixed order: the same call gives the same bits. */
+ * Sums are formed in a fixed order: the same call gives the same bits.  A sum stays in
+ * the matrix unit's registers for 8192 rows at most (6e-8 low where all terms have one
+ * sign), then joins its workgroup's in fp32 and at last all workgroups' in 64 bits. */
 ks_status ks_gated_backward(const ks_heads *heads, const ks_rows *rows, const float *dz, const ks_gated_grad *grad,
                             void *ws, size_t ws_bytes, hipStream_t stream);
 

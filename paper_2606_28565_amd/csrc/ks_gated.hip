@@ -248,9 +248,10 @@ __global__ __launch_bounds__(512, (!LOSS && (BF16 || IN == 16) ? 4 : 2)) void k_
   const int hg = wave % HG, rg = wave / HG;
   const bool works = rg < RG;
   const int wg = blockIdx.x, f = family_of(p.bwd_wg, wg);
-  const int64_t begin = p.fam_off[f] + (int64_t)(wg - p.bwd_wg[f]) * p.bwd_rows;
-  const int64_t fam_end = p.fam_off[f + 1];
-  const int64_t end = begin + p.bwd_rows < fam_end ? begin + p.bwd_rows : fam_end;
+  // (a launch takes kGatedRun rows of each workgroup; the next goes on from there)
+  const int64_t first = p.fam_off[f] + (int64_t)(wg - p.bwd_wg[f]) * p.bwd_rows, begin = first + p.run;
+  const int64_t last = min(first + p.bwd_rows, p.fam_off[f + 1]), end = min(begin + kGatedRun, last);
+  if (begin >= end) return;   // (of a family's last workgroup)
   gf32x16 dw[2] = {gf32x16{}, gf32x16{}};
   float d0 = 0.0f;
   gu32x4 wgt[2][KC][NP];
@@ -528,19 +529,21 @@ __global__ __launch_bounds__(512, (!LOSS && (BF16 || IN == 16) ? 4 : 2)) void k_
     for (int i = 0; i < 16; ++i) {
       float v = dw[m][i];
       if constexpr (IN == 16 && !BF16) v += __shfl_xor(v, 16);   // the features' second half of the columns
-      if (n < IN) own[(m * kGatedGroup + 8 * (i >> 2) + 4 * h + (i & 3)) * IN + n] = v;
+      float *at = own + (m * kGatedGroup + 8 * (i >> 2) + 4 * h + (i & 3)) * IN + n;
+      if (n < IN) *at = p.run ? *at + v : v;
     }
   if (hg == 0 && lane == 0) {
     float v = 0.0f;
     for (int i = 0; i < W; ++i) v += d0s[i];
-    out[gated_part_size(p.hidden, IN) - 1] = v;
+    float *at = out + gated_part_size(p.hidden, IN) - 1;
+    *at = p.run ? *at + v : v;
     if constexpr (LOSS) {
       for (int i = 1; i < W; ++i) {
         sum += loss[i][0];
         total += loss[i][1];
       }
-      p.loss_part[2 * wg] = sum;
-      p.loss_part[2 * wg + 1] = total;
+      p.loss_part[2 * wg] = p.run ? p.loss_part[2 * wg] + sum : sum;
+      p.loss_part[2 * wg + 1] = p.run ? p.loss_part[2 * wg + 1] + total : total;
     }
   }
 }
@@ -835,9 +838,14 @@ static void sums_of(const GatedParams &p, hipStream_t s) {
 
 hipError_t launch_gated_sums(const GatedParams &p, bool loss, hipStream_t s) {
   if (p.bwd_wg[KS_NFAM] == 0) return hipSuccess;
-  if (loss) sums_of<true>(p, s);
-  else sums_of<false>(p, s);
-  return hipGetLastError();
+  GatedParams q = p;
+  for (q.run = 0; q.run < p.bwd_rows; q.run += kGatedRun) {
+    if (loss) sums_of<true>(q, s);
+    else sums_of<false>(q, s);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_gated_rows(const GatedParams &p, hipStream_t s) {

@@ -300,6 +300,7 @@ struct GatedParams {
   bool bf16;
   const void *w1, *w2, *w3, *b3;
   int32_t fwd_tiles, bwd_rows, row_rows;
+  int64_t run;                       // k_gated_sums: its workgroups' rows from here on
   int32_t fwd_wg[KS_NFAM + 1], bwd_wg[KS_NFAM + 1], row_wg[KS_NFAM + 1];
   float *z;                          // nullable
   // the loss (eta null: none)
@@ -320,6 +321,10 @@ struct GatedParams {
 // k_gated_sums: rows a workgroup takes at a time, units per wave; floats of its sums:
 // by groups of 32 units dW1 and dW2 (the last group whole), then db3
 constexpr int kGatedStep = 128, kGatedGroup = 32;
+// ... and at most in a launch: the matrix instruction's sums come out low by some 7e-12
+// of themselves for every row (it drops what lies far below the running sum), so a
+// sum in registers ends there and is added, rounded to nearest, to those before it
+constexpr int kGatedRun = 64 * kGatedStep;
 constexpr int gated_part_size(int hidden, int in_dim) {
   return (hidden + kGatedGroup - 1) / kGatedGroup * kGatedGroup * 2 * in_dim + 1;
 }

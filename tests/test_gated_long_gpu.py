@@ -1,0 +1,78 @@
+"""Gated heads over many rows: sums of one sign over tens of millions of rows, and
+calls whose workgroups go through their row loops more than once.
+
+Sums of one sign.  The rows recur every 100,003, so that the oracle's 64-bit sums are
+those of one period.  What is checked is the mean over the elements of the signed
+relative error, which roundings to nearest leave alone (they average out over the
+workgroups and the elements): left are what the hardware's exponential, sum and
+reciprocal of a gate lean to one side, 4 x 2^-24 at most, what a sum in registers loses,
+7.2e-12 a row over 8192 rows (6e-8), and the result's own rounding, 6e-8 at most: 3.6e-7,
+held to 2^-21 = 4.8e-7.  One sum in registers over all rows of a workgroup came out
+1.0e-6 (130M rows) and 1.1e-6 (40M) low."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+from oracle import ks_fit as o
+from paper_2606_28565_amd import abi
+from tests.test_gated_gpu import NFAM, check_loss, make, run_loss, targets
+
+pytestmark = pytest.mark.gpu
+PERIOD, LEAN, FAM = 100_003, 2.0 ** -21, 4
+
+
+def periodic(prec, inp, hid, times, zero_w3=False):
+    """Rows of one family, of one sign like its weights: device tensors of all rows,
+    float64 of one period."""
+    import torch
+    dt = torch.bfloat16 if prec == "bf16" else torch.float32
+    g = torch.Generator().manual_seed(3)
+    x = torch.rand(PERIOD, inp, generator=g).to(dt)
+    w = {"w1": torch.rand(NFAM, hid, inp, generator=g) * 0.3, "w2": torch.rand(NFAM, hid, inp, generator=g) * 0.3,
+         "w3": torch.rand(NFAM, hid, generator=g) + 0.3, "b3": torch.zeros(NFAM)}
+    if zero_w3:
+        w["w3"].zero_()
+    w = {k: v.to(dt) for k, v in w.items()}
+    d = {"x": x.cuda().repeat(times, 1), **{k: v.cuda() for k, v in w.items()}}
+    h = {"x": x.double().numpy(), **{k: v[FAM].double().numpy() for k, v in w.items()}}
+    return d, h, [0] * (FAM + 1) + [times * PERIOD] * (NFAM - FAM)
+
+
+def lean(got, want):
+    return float(np.mean((got - want) / want))
+
+
+@pytest.mark.parametrize("prec,inp,times", [("bf16", 16, 1300), ("f32", 16, 1300), ("bf16", 32, 1300), ("f32", 32, 400)])
+def test_sums_of_one_sign(prec, inp, times):
+    import torch
+    d, h, off = periodic(prec, inp, 8, times)
+    dz = torch.rand(PERIOD, generator=torch.Generator().manual_seed(4)) + 0.5
+    dz_all = dz.cuda().repeat(times)
+    hd, rows = abi.gated_heads(d["w1"], d["w2"], d["w3"], d["b3"]), abi.feature_rows(d["x"], off)
+    out = {k: torch.empty(d[k].shape, device="cuda") for k in ("w1", "w2", "w3", "b3")}
+    ws = torch.empty(abi.ks_gated_workspace_bytes(hd, rows), dtype=torch.uint8, device="cuda")
+    abi.ks_gated_backward(hd, rows, dz_all.data_ptr(), abi.gated_grad(**out), ws.data_ptr(), ws.numel(), abi.current_stream())
+    torch.cuda.synchronize()
+    _, k = o.block(h["x"], h["w1"], h["w2"], h["w3"], h["b3"])
+    want, _ = o.gradients(h["x"], h["w1"], h["w2"], h["w3"], dz.double().numpy(), k, 1)
+    for key in want.keys() - {"x"}:
+        got = out[key].double().cpu().numpy()
+        assert abs(lean(got[FAM], times * want[key])) <= LEAN, (key, lean(got[FAM], times * want[key]))
+        assert (np.delete(got, FAM, 0) == 0).all(), key
+
+
+@pytest.mark.parametrize("prec,inp,times", [("bf16", 16, 1300), ("f32", 32, 400)])
+def test_loss_sums_of_one_sign(prec, inp, times):
+    """In two launches and in one.  w3 and b3 are zero and the targets far, so every
+    row's dz is 1/2 to the bit and the gradients of w3 are means of a u / 2."""
+    import torch
+    d, h, off = periodic(prec, inp, 8, times, zero_w3=True)
+    eta = torch.full((times * PERIOD,), 1e4, device="cuda")
+    loss, z, grads = run_loss(d, off, eta, None, 1.0)
+    assert (z == 0).all()
+    want = np.log(1e4) - np.log(2) - 0.5
+    assert abs(loss[FAM] - want) <= 1e-6 * want and (np.delete(loss, FAM) == 0).all()
+    assert grads["b3"][FAM] == 0.5 and (grads["w1"] == 0).all() and (grads["w2"] == 0).all()
+    _, k = o.block(h["x"], h["w1"], h["w2"], h["w3"], h["b3"])
+    assert abs(lean(grads["w3"][FAM], k["y"].mean(0) / 2)) <= LEAN
