@@ -230,7 +230,10 @@ struct Back {
 // for fp32 heads of 32 inputs.  A wave's weights are the row operand there: a lane
 // then holds 16 of its units for one row, adds up their part of z, and the unit groups'
 // parts meet in LDS.
-template <bool BF16, int IN, bool LOSS>
+//
+// A launch takes kGatedRun rows of each workgroup.  MORE: a later launch, which goes on
+// from there and adds to what the workgroup stored (one whose rows have ended, zeros).
+template <bool BF16, int IN, bool LOSS, bool MORE>
 __global__ __launch_bounds__(512, (!LOSS && (BF16 || IN == 16) ? 4 : 2)) void k_gated_sums(GatedParams p) {
   using K = Back<BF16, IN>;
   constexpr int KC = K::KC, W = K::W, NP = K::NP, NQ = K::NQ, R = 16 * W;   // rows of a step
@@ -248,10 +251,8 @@ __global__ __launch_bounds__(512, (!LOSS && (BF16 || IN == 16) ? 4 : 2)) void k_
   const int hg = wave % HG, rg = wave / HG;
   const bool works = rg < RG;
   const int wg = blockIdx.x, f = family_of(p.bwd_wg, wg);
-  // (a launch takes kGatedRun rows of each workgroup; the next goes on from there)
-  const int64_t first = p.fam_off[f] + (int64_t)(wg - p.bwd_wg[f]) * p.bwd_rows, begin = first + p.run;
-  const int64_t last = min(first + p.bwd_rows, p.fam_off[f + 1]), end = min(begin + kGatedRun, last);
-  if (begin >= end) return;   // (of a family's last workgroup)
+  const int64_t first = p.fam_off[f] + (int64_t)(wg - p.bwd_wg[f]) * p.bwd_rows, begin = MORE ? first + p.run : first;
+  const int64_t end = min(min(first + p.bwd_rows, p.fam_off[f + 1]), begin + kGatedRun);
   gf32x16 dw[2] = {gf32x16{}, gf32x16{}};
   float d0 = 0.0f;
   gu32x4 wgt[2][KC][NP];
@@ -523,27 +524,36 @@ __global__ __launch_bounds__(512, (!LOSS && (BF16 || IN == 16) ? 4 : 2)) void k_
   if (!works || rg > 0) return;
   float *out = p.part + (size_t)wg * gated_part_size(p.hidden, IN);
   float *own = out + hg * kGatedGroup * 2 * IN;
+  auto at = [&](int m, int i) { return own + (m * kGatedGroup + 8 * (i >> 2) + 4 * h + (i & 3)) * IN + n; };
 #pragma unroll
   for (int m = 0; m < 2; ++m)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float v = dw[m][i];
-      if constexpr (IN == 16 && !BF16) v += __shfl_xor(v, 16);   // the features' second half of the columns
-      float *at = own + (m * kGatedGroup + 8 * (i >> 2) + 4 * h + (i & 3)) * IN + n;
-      if (n < IN) *at = p.run ? *at + v : v;
+    for (int i = 0; i < 16; ++i)
+      if constexpr (IN == 16 && !BF16) dw[m][i] += __shfl_xor(dw[m][i], 16);   // the features' second half of the columns
+  if (n < IN) {
+    if constexpr (MORE) {
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dw[m][i] += *at(m, i);
     }
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) *at(m, i) = dw[m][i];
+  }
   if (hg == 0 && lane == 0) {
     float v = 0.0f;
     for (int i = 0; i < W; ++i) v += d0s[i];
-    float *at = out + gated_part_size(p.hidden, IN) - 1;
-    *at = p.run ? *at + v : v;
+    float *last = out + gated_part_size(p.hidden, IN) - 1;
+    *last = MORE ? *last + v : v;
     if constexpr (LOSS) {
       for (int i = 1; i < W; ++i) {
         sum += loss[i][0];
         total += loss[i][1];
       }
-      p.loss_part[2 * wg] = p.run ? p.loss_part[2 * wg] + sum : sum;
-      p.loss_part[2 * wg + 1] = p.run ? p.loss_part[2 * wg + 1] + total : total;
+      p.loss_part[2 * wg] = MORE ? p.loss_part[2 * wg] + sum : sum;
+      p.loss_part[2 * wg + 1] = MORE ? p.loss_part[2 * wg + 1] + total : total;
     }
   }
 }
@@ -824,28 +834,29 @@ hipError_t launch_gated_forward(const GatedParams &p, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <bool LOSS>
-static void sums_of(const GatedParams &p, hipStream_t s) {
+template <bool LOSS, bool MORE>
+static hipError_t sums_of(const GatedParams &p, hipStream_t s) {
   const dim3 grid(p.bwd_wg[KS_NFAM]), block(512);
-  if (p.bf16) {
-    if (p.in_dim == 16) hipLaunchKernelGGL((k_gated_sums<true, 16, LOSS>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((k_gated_sums<true, 32, LOSS>), grid, block, 0, s, p);
+  if constexpr (LOSS && MORE) {   // (the others take a loss of so many rows in two launches)
+    if (p.bf16 || p.in_dim == 16) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((k_gated_sums<false, 32, true, true>), grid, block, 0, s, p);
+  } else if (p.bf16) {
+    if (p.in_dim == 16) hipLaunchKernelGGL((k_gated_sums<true, 16, LOSS, MORE>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((k_gated_sums<true, 32, LOSS, MORE>), grid, block, 0, s, p);
   } else {
-    if (p.in_dim == 16) hipLaunchKernelGGL((k_gated_sums<false, 16, LOSS>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((k_gated_sums<false, 32, LOSS>), grid, block, 0, s, p);
+    if (p.in_dim == 16) hipLaunchKernelGGL((k_gated_sums<false, 16, LOSS, MORE>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((k_gated_sums<false, 32, LOSS, MORE>), grid, block, 0, s, p);
   }
+  return hipGetLastError();
 }
 
 hipError_t launch_gated_sums(const GatedParams &p, bool loss, hipStream_t s) {
   if (p.bwd_wg[KS_NFAM] == 0) return hipSuccess;
+  hipError_t e = loss ? sums_of<true, false>(p, s) : sums_of<false, false>(p, s);
   GatedParams q = p;
-  for (q.run = 0; q.run < p.bwd_rows; q.run += kGatedRun) {
-    if (loss) sums_of<true>(q, s);
-    else sums_of<false>(q, s);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  for (q.run = kGatedRun; e == hipSuccess && q.run < p.bwd_rows; q.run += kGatedRun)
+    e = loss ? sums_of<true, true>(q, s) : sums_of<false, true>(q, s);
+  return e;
 }
 
 hipError_t launch_gated_rows(const GatedParams &p, hipStream_t s) {
