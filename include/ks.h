@@ -453,8 +453,10 @@ ks_status ks_eval_steps_static(const ks_desc* desc, const ks_steps* steps,
  * writes may not overlap what else it reads or writes, and calls that may run at
  * the same time (two streams, two captured graphs) need a workspace each.
  * Numbers are taken as they come: products of fp32 heads are those of fp32 for
- * magnitudes from 2^-102, and a row, dz or weight that is not finite makes what
- * depends on it not finite.
+ * magnitudes from 2^-102 up, and a row, dz or weight that is not finite makes what
+ * depends on it not finite.  The weights' gradients are sums of products with dz x
+ * (fp32 heads) or of x with dz a and dz u silu'(g) (bf16 heads): those too are held from
+ * 2^-102 up.
  */
 
 /* Feature rows, family-major: rows [fam_off[f], fam_off[f+1]) are family f's and

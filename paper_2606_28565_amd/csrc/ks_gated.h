@@ -60,8 +60,12 @@ __device__ __forceinline__ uint32_t upper(float v) { return __builtin_bit_cast(u
 __device__ __forceinline__ uint32_t pack_upper(float lo, float hi) {
   return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302);
 }
+// ANY: numbers up to fp32's largest, whose nearest bfloat16 is infinity from 3.396e38 up:
+// they leave the largest finite one as the first piece.
+template <bool ANY = false>
 __device__ __forceinline__ void split2(float a, float b, uint32_t &p0, uint32_t &p1, uint32_t &p2) {
-  p0 = pack2(a, b);
+  constexpr float kTop = 0x1.fep127f;
+  p0 = ANY ? pack2(__builtin_amdgcn_fmed3f(a, -kTop, kTop), __builtin_amdgcn_fmed3f(b, -kTop, kTop)) : pack2(a, b);
   a -= __builtin_bit_cast(float, p0 << 16);
   b -= __builtin_bit_cast(float, p0 & 0xFFFF0000u);
   p1 = pack_upper(a, b);
@@ -96,7 +100,7 @@ struct Block {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         uint32_t p0, p1, p2;
-        split2(j < 2 ? a[2 * j] : b[2 * j - 4], j < 2 ? a[2 * j + 1] : b[2 * j - 3], p0, p1, p2);
+        split2<true>(j < 2 ? a[2 * j] : b[2 * j - 4], j < 2 ? a[2 * j + 1] : b[2 * j - 3], p0, p1, p2);
         p[0][j] = p0;
         p[1][j] = p1;
         p[2][j] = p2;

@@ -606,7 +606,7 @@ __global__ __launch_bounds__(512, 2) void k_gated_rows(GatedParams p) {
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             uint32_t p0, p1, p2;
-            split2(v[2 * u], v[2 * u + 1], p0, p1, p2);
+            split2<true>(v[2 * u], v[2 * u + 1], p0, p1, p2);
             q[0][u] = p0, q[1][u] = p1, q[2][u] = p2;
           }
           const gu32x4 none = {0, 0, 0, 0};
