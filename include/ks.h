@@ -474,8 +474,9 @@ typedef struct ks_rows {
 /* Gradients (device, overwritten; families without rows get zeros).
  * w1, w2: [KS_NFAM][hidden][in_dim], w3: [KS_NFAM][hidden], b3: [KS_NFAM], all
  * fp32 whatever the heads' precision, all four or none of them NULL.
- * x: [n_rows][ldx] of heads.precision's type, or NULL; ldx from in_dim to 2^20, and
- * it may not overlap the rows themselves. */
+ * x: [n_rows][ldx] of heads.precision's type, or NULL; ldx from in_dim to 2^20.  It may
+ * not overlap the rows themselves; the two may be columns of one buffer, with the same
+ * row stride. */
 typedef struct ks_gated_grad {
   float *w1, *w2, *w3, *b3;
   void *x;

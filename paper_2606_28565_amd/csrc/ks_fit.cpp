@@ -138,10 +138,13 @@ ks_status take_grad(ks::GatedParams &p, const ks_gated_grad *g) {
   return KS_OK;
 }
 
-// a device range's bytes, for overlap checks of strided rows
-bool overlap(const void *a, int64_t na, const void *b, int64_t nb) {
-  const char *x = static_cast<const char *>(a), *y = static_cast<const char *>(b);
-  return x < y + nb && y < x + na;
+// whether n rows of width bytes each lda bytes apart share any with n rows ldb apart
+bool overlap(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t n, int64_t width) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  if (x >= y + (n - 1) * ldb + width || y >= x + (n - 1) * lda + width) return false;
+  // columns of one buffer: apart in every period of the stride
+  const uint64_t at = lda == ldb ? (x > y ? x - y : lda - (y - x) % lda) % lda : 0;
+  return lda != ldb || at < (uint64_t)width || at + width > (uint64_t)lda;
 }
 
 }  // namespace
@@ -189,8 +192,7 @@ ks_status ks_gated_backward(const ks_heads *heads, const ks_rows *rows, const fl
     if (grad->ldx < heads->in_dim || grad->ldx > (int64_t(1) << 20))
       return set_error(KS_EINVAL, "grad.ldx %lld outside in_dim %d .. 2^20", (long long)grad->ldx, heads->in_dim);
     if (!aligned(grad->x, e)) return set_error(KS_EINVAL, "grad.x is not aligned to its type");
-    if (rows->n_rows > 0 && overlap(grad->x, ((rows->n_rows - 1) * grad->ldx + heads->in_dim) * e, rows->x,
-                                    ((rows->n_rows - 1) * rows->ldx + heads->in_dim) * e))
+    if (rows->n_rows > 0 && overlap(grad->x, grad->ldx * e, rows->x, rows->ldx * e, rows->n_rows, heads->in_dim * e))
       return set_error(KS_EINVAL, "grad.x overlaps rows.x");
     p.g_x = grad->x;
     p.g_ldx = grad->ldx;

@@ -13,7 +13,7 @@ import numpy as np
 import pytest
 
 from paper_2606_28565_amd.abi import NFAM
-from tests.test_host_asan import CSRC, HOST, ROCM_INCLUDE, ROOT, SAN_ENV
+from tests.test_host_asan import CSRC, HOST, KS_EINVAL, KS_OK, ROCM_INCLUDE, ROOT, SAN_ENV
 
 
 @pytest.fixture(scope="module")
@@ -78,3 +78,22 @@ def test_features(driver):
     lines = [f"features {n} {s} {inp} {bf16} {pad}" for n, s in ((0, 3), (1, 1), (37, 5), (2000, 3))
              for inp in (16, 32) for bf16 in (0, 1) for pad in (0, 3)]
     assert run(driver, lines) == ["ok"] * len(lines)
+
+
+EXPECTED = {
+    "columns_apart": KS_OK, "columns_apart_before": KS_OK, "columns_far_apart": KS_OK, "columns_of_other_rows": KS_OK,
+    "columns_meet": KS_EINVAL, "columns_meet_before": KS_EINVAL, "columns_run_into_the_next_row": KS_EINVAL,
+    "columns_of_other_strides": KS_EINVAL, "same_rows": KS_EINVAL, "one_row_apart": KS_OK, "one_row_meets": KS_EINVAL,
+    "behind_the_last": KS_OK,
+}
+
+
+def statuses(driver):
+    return dict(line.split() for line in run(driver, ["args"]))
+
+
+def test_rows_and_gradients_in_one_buffer(driver):
+    """Rows and their gradients may be columns of one buffer of the same row stride; where
+    an element belongs to both, or the strides differ, the call is refused."""
+    got = statuses(driver)
+    assert {k: int(got[k]) for k in EXPECTED} == EXPECTED
