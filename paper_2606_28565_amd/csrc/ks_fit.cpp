@@ -165,6 +165,8 @@ ks_status ks_gated_forward(const ks_heads *heads, const ks_rows *rows, float *z,
 size_t ks_gated_workspace_bytes(const ks_heads *heads, const ks_rows *rows) {
   // (weights and rows need not be there yet)
   if (!heads || heads->mode != KS_ETA_GATED) return set_error(KS_EINVAL, "heads is NULL or not gated"), 0;
+  if (heads->precision != KS_F32 && heads->precision != KS_BF16)
+    return set_error(KS_EINVAL, "heads.precision %d unknown", heads->precision), 0;
   if (heads->hidden < 1 || heads->hidden > 256 || (heads->in_dim != 16 && heads->in_dim != 32))
     return set_error(KS_EINVAL, "heads.hidden %d or in_dim %d not supported", heads->hidden, heads->in_dim), 0;
   if (check_rows(heads, rows) != KS_OK) return 0;

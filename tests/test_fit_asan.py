@@ -97,3 +97,8 @@ def test_rows_and_gradients_in_one_buffer(driver):
     an element belongs to both, or the strides differ, the call is refused."""
     got = statuses(driver)
     assert {k: int(got[k]) for k in EXPECTED} == EXPECTED
+
+
+def test_workspace_of_an_unknown_precision(driver):
+    got = statuses(driver)
+    assert (got["workspace"], got["workspace_of_unknown_precision"]) == ("1", "0")
