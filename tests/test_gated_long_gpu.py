@@ -76,3 +76,30 @@ def test_loss_sums_of_one_sign(prec, inp, times):
     assert grads["b3"][FAM] == 0.5 and (grads["w1"] == 0).all() and (grads["w2"] == 0).all()
     _, k = o.block(h["x"], h["w1"], h["w2"], h["w3"], h["b3"])
     assert abs(lean(grads["w3"][FAM], k["y"].mean(0) / 2)) <= LEAN
+
+
+@pytest.mark.parametrize("prec,inp,hid", [("f32", 16, 20), ("bf16", 16, 33), ("bf16", 32, 40), ("f32", 32, 24)])
+def test_loss_loops(prec, inp, hid):
+    """A loss whose forward workgroups take more than their 256 rows of one pass (fp32 with
+    32 inputs: more than two steps of the one launch), the last in part; every seventh row
+    was never measured and holds anything."""
+    import torch
+    n = 300_011
+    d, h, off = make(n, prec, inp, hid)
+    eta, weight = targets(n)
+    eta[3::7] = float("nan")
+    d["x"][torch.arange(3, n, 7).cuda()] = float("nan")
+    h["x"][3::7] = float("nan")
+    got = run_loss(d, off, eta.cuda(), weight.cuda(), 0.4)
+    assert np.isnan(got[1][3::7]).all() and np.isfinite(np.delete(got[1], np.arange(3, n, 7))).all()
+    check_loss(h, off, eta, weight, 0.4, got, prec=prec)
+
+
+@pytest.mark.parametrize("n,hid", [(1, 256), (9, 129), (300, 256), (140_001, 129), (140_001, 256)])
+def test_loss_alone_of_wide_fp32_heads(n, hid):
+    """The forward kernel of eight waves with the loss: few rows, and more than its 512
+    rows of one pass."""
+    d, h, off = make(n, "f32", 32, hid)
+    eta, weight = targets(n)
+    loss, z, _ = run_loss(d, off, eta.cuda(), weight.cuda(), 0.4, grad=False)
+    check_loss(h, off, eta, weight, 0.4, (loss, z, {}), grad=False)
