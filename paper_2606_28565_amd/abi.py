@@ -40,6 +40,7 @@ class ks_spec(C.Structure):
 
 
 class ks_heads(C.Structure):
+    place = fits = None
     _fields_ = [("in_dim", C.c_int32), ("hidden", C.c_int32), ("precision", C.c_int32),
                 ("mode", C.c_int32), ("w1", P), ("w2", P), ("b2", P), ("w3", P), ("b3", P),
                 ("bounded_mask", C.c_uint32), ("grid_mask", C.c_uint32), ("bounded", P),
@@ -105,14 +106,17 @@ class ks_sim_out(C.Structure):
 
 
 class ks_rows(C.Structure):
+    place = made = fits = None
     _fields_ = [("n_rows", C.c_int64), ("fam_off", C.c_int64 * (NFAM + 1)), ("x", P), ("ldx", C.c_int64)]
 
 
 class ks_gated_grad(C.Structure):
+    place = made = made_x = None
     _fields_ = [("w1", P), ("w2", P), ("w3", P), ("b3", P), ("x", P), ("ldx", C.c_int64)]
 
 
 class ks_eta_target(C.Structure):
+    place = made = None
     _fields_ = [("eta", P), ("weight", P), ("huber", C.c_double)]
 
 
@@ -122,6 +126,7 @@ class ks_tensor(C.Structure):
 
 
 class ks_adamw_config(C.Structure):
+    place = None
     _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
                 ("grad_scale", C.c_double), ("state_bits", C.c_int32), ("reserved", C.c_int32),
                 ("step", C.c_int64), ("step_dev", P)]
@@ -288,8 +293,30 @@ def ks_different_families(desc, n_specs, heads, kout, ws_bytes) -> int:
                                         None if kout is None else C.byref(kout), ws_bytes)
 
 
+def _agree(heads, rows, grad=None, target=None):
+    """Refuses structs that the marshalling helpers made for shapes, types or devices
+    that do not go together: the library sees addresses only, and would read or write
+    past their ends.  Structs filled by hand are taken as they are."""
+    places = {s.place for s in (heads, rows, grad, target) if s is not None} - {None}
+    if len(places) > 1 or -1 in places:
+        raise ValueError("tensors on the CPU, or on different GPUs")
+    want = heads.in_dim, heads.precision
+    if rows.made is not None and (rows.made[0] < want[0] or rows.made[1] != want[1]):
+        raise ValueError(f"rows of {rows.made[0]} elements ({_KIND[rows.made[1]]}) for heads of {want[0]} inputs "
+                         f"({_KIND.get(want[1])})")
+    if grad is not None and grad.made is not None and grad.made != (heads.hidden, heads.in_dim):
+        raise ValueError(f"gradients of [{grad.made[0]}][{grad.made[1]}] for heads of [{heads.hidden}][{heads.in_dim}]")
+    x = grad.made_x if grad is not None else None
+    if x is not None and (x[0] < rows.n_rows or x[1] < want[0] or x[2] != want[1]):
+        raise ValueError(f"rows' gradients of [{x[0]}][{x[1]}] ({_KIND[x[2]]}) for [{rows.n_rows}][{want[0]}] ({_KIND.get(want[1])})")
+    if target is not None and target.made is not None and target.made < rows.n_rows:
+        raise ValueError(f"{target.made} measured eta for {rows.n_rows} rows")
+
+
 def ks_gated_forward(heads, rows, z_ptr, stream, check=True):
-    st = load().ks_gated_forward(C.byref(heads), C.byref(rows), z_ptr, stream)
+    if heads.fits is None or heads.fits != rows.fits:   # (a short call: all at once where all are the same)
+        _agree(heads, rows)
+    st = (_lib or load()).ks_gated_forward(C.byref(heads), C.byref(rows), z_ptr, stream)
     return _check(st) if check else st
 
 
@@ -298,12 +325,14 @@ def ks_gated_workspace_bytes(heads, rows) -> int:
 
 
 def ks_gated_backward(heads, rows, dz_ptr, grad, ws_ptr, ws_bytes, stream, check=True):
+    _agree(heads, rows, grad)
     st = load().ks_gated_backward(C.byref(heads), C.byref(rows), dz_ptr, C.byref(grad), ws_ptr, ws_bytes, stream)
     return _check(st) if check else st
 
 
 def ks_gated_loss(heads, rows, target, loss_ptr, z_ptr, grad, ws_ptr, ws_bytes, stream, check=True):
     """grad: a ks_gated_grad, or None for the loss alone; z_ptr may be None."""
+    _agree(heads, rows, grad, target)
     st = load().ks_gated_loss(C.byref(heads), C.byref(rows), C.byref(target), loss_ptr, z_ptr,
                               None if grad is None else C.byref(grad), ws_ptr, ws_bytes, stream)
     return _check(st) if check else st
@@ -318,7 +347,10 @@ def ks_features(desc, specs_ptr, n_specs, in_dim, precision, x_ptr, ldx, t_roof_
 
 def ks_adamw(config, tensors, stream, check=True):
     """tensors: a ctypes array of ks_tensor (see adamw_tensors)."""
-    st = load().ks_adamw(C.byref(config), tensors, len(tensors), stream)
+    at, count = getattr(tensors, "place", None), config.place
+    if at == -1 or count == -1 or (count is not None and at is not None and at != count):
+        raise ValueError("tensors or step_dev on the CPU, or on different GPUs")
+    st = (_lib or load()).ks_adamw(C.byref(config), tensors, len(tensors), stream)
     return _check(st) if check else st
 
 
@@ -520,7 +552,25 @@ def current_stream() -> int:
 # --------------------------------------------------------------------------
 # gated heads and their fitting: torch device tensors -> ctypes structs.  The
 # structs hold addresses only: keep the tensors while the structs are used.
+# Beside the fields, each keeps as attributes what the calls above hold it to
+# (None in a struct filled by hand): its GPU's index (place; -1: the CPU) and what it
+# was made for (made: elements and precision of rows, hidden and inputs of gradients,
+# the number of targets; made_x: the rows' gradients; fits: GPU, inputs and precision).
 # --------------------------------------------------------------------------
+_KIND = {KS_F32: "fp32", KS_BF16: "bf16"}
+
+
+def _place(tensors) -> int | None:
+    """The GPU that holds all of them; None without any."""
+    on = {t.device for t in tensors if t is not None}
+    if len(on) > 1:
+        raise ValueError(f"tensors on {', '.join(sorted(map(str, on)))}, not on one device")
+    if not on:
+        return None
+    d = on.pop()
+    return -1 if d.type != "cuda" else d.index or 0
+
+
 def _precision(t) -> int:
     import torch
     if t.dtype not in (torch.float32, torch.bfloat16):
@@ -545,6 +595,8 @@ def gated_heads(w1, w2, w3, b3) -> ks_heads:
             raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}, not {w1.dtype} {want[name]}")
         setattr(hd, name, _whole(t))
     hd.precision, hd.mode = _precision(w1), KS_ETA_GATED
+    hd.place = _place((w1, w2, w3, b3))
+    hd.fits = (hd.place, hd.in_dim, hd.precision) if hd.place >= 0 else None
     return hd
 
 
@@ -563,6 +615,8 @@ def feature_rows(x, fam_off) -> ks_rows:
     for f in range(NFAM + 1):
         r.fam_off[f] = int(fam_off[f])
     r.x = _ptr(x) if x.numel() else None
+    r.place, r.made = _place((x,)), (x.shape[1], _precision(x))
+    r.fits = (r.place, *r.made) if r.place >= 0 else None
     return r
 
 
@@ -574,9 +628,18 @@ def gated_grad(w1=None, w2=None, w3=None, b3=None, x=None) -> ks_gated_grad:
         if t is not None and _precision(t) != KS_F32:
             raise ValueError(f"the gradient of {name} is not fp32")
         setattr(g, name, _whole(t))
+    if all(t is not None for t in (w1, w2, w3, b3)):
+        hidden, in_dim = w1.shape[1:] if w1.dim() == 3 else (0, 0)
+        for name, t, want in (("w1", w1, (NFAM, hidden, in_dim)), ("w2", w2, (NFAM, hidden, in_dim)),
+                              ("w3", w3, (NFAM, hidden)), ("b3", b3, (NFAM,))):
+            if tuple(t.shape) != want:
+                raise ValueError(f"the gradient of {name} is {tuple(t.shape)}, not {want}")
+        g.made = (hidden, in_dim)
     if x is not None:
         g.ldx = _row_stride(x)
         g.x = _ptr(x) if x.numel() else None
+        g.made_x = (*x.shape, _precision(x))
+    g.place = _place((w1, w2, w3, b3, x))
     return g
 
 
@@ -587,8 +650,10 @@ def eta_target(eta, weight=None, huber=float("inf")) -> ks_eta_target:
             raise ValueError("eta or weight is not fp32")
     if weight is not None and weight.shape != eta.shape:
         raise ValueError("weight is not of eta's shape")
-    return ks_eta_target(_whole(eta) if eta.numel() else None,
-                         None if weight is None or not weight.numel() else _whole(weight), huber)
+    t = ks_eta_target(_whole(eta) if eta.numel() else None,
+                      None if weight is None or not weight.numel() else _whole(weight), huber)
+    t.place, t.made = _place((eta, weight)), eta.numel()
+    return t
 
 
 def adamw_tensors(tensors):
@@ -612,13 +677,18 @@ def adamw_tensors(tensors):
         if (d["m"].dtype, d["v"].dtype) != states:
             raise ValueError(f"tensor {i}: states of {d['m'].dtype} and {d['v'].dtype}, not {states}")
         t.n, t.weight_decay, t.grad_type = n, d.get("weight_decay", 0.0), _precision(d["grad"])
+    arr.place = _place([d.get(name) for d in tensors for name in ("param", "grad", "m", "v", "copy", "m_exp", "v_exp")])
     return arr
 
 
 def adamw_config(lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, state_bits=32, step=1,
                  step_dev=None) -> ks_adamw_config:
     """step_dev: an int32 tensor of one element counting the steps made, or None."""
-    return ks_adamw_config(lr, beta1, beta2, eps, grad_scale, state_bits, 0, step, _ptr(step_dev))
+    if step_dev is not None and (step_dev.numel() != 1 or str(step_dev.dtype) not in ("torch.int32", "torch.uint32")):
+        raise ValueError(f"step_dev is {step_dev.dtype} of {step_dev.numel()} elements, not one int32")
+    c = ks_adamw_config(lr, beta1, beta2, eps, grad_scale, state_bits, 0, step, _ptr(step_dev))
+    c.place = _place((step_dev,))
+    return c
 
 
 # --------------------------------------------------------------------------
