@@ -420,6 +420,27 @@ def _ptr(t) -> int | None:
     return None if t is None else t.data_ptr()
 
 
+def _select(hd: ks_heads, bounded, grid, device) -> dict:
+    """The families of ``bounded`` and ``grid`` (see make_heads) in hd; returns the
+    device tensors that it then points at."""
+    import torch
+    t = {}
+    if bounded is not None and bounded.mask:
+        t["bounded"] = torch.from_numpy(np.ascontiguousarray(bounded.storage, np.float32).reshape(-1).copy()).to(device)
+        hd.bounded_mask = bounded.mask
+        hd.bounded = _ptr(t["bounded"])
+    if grid is not None and grid.mask:
+        t["grid"] = torch.from_numpy(np.ascontiguousarray(grid.values, np.float32).reshape(-1).copy()).to(device)
+        hd.grid_mask = grid.mask
+        hd.grid = _ptr(t["grid"])
+        for d in range(3):
+            hd.grid_axis[d] = int(grid.axes[d])
+            hd.grid_n[d] = int(grid.n[d])
+            hd.grid_lo[d] = float(grid.lo[d])
+            hd.grid_hi[d] = float(grid.hi[d])
+    return t
+
+
 class DeviceInputs:
     """The inputs of one evaluation, resident in device memory (torch
     tensors), and the ctypes structs that point at them."""
@@ -491,23 +512,7 @@ class DeviceInputs:
         hd.mode = mode
         for name in ("w1", "w2", "b2", "w3", "b3"):
             setattr(hd, name, _ptr(self.heads_t[name]))
-        if bounded is not None and bounded.mask:
-            import torch
-            self.t["bounded"] = torch.from_numpy(np.ascontiguousarray(bounded.storage, np.float32)
-                                                 .reshape(-1).copy()).to(self.t["step"].device)
-            hd.bounded_mask = bounded.mask
-            hd.bounded = _ptr(self.t["bounded"])
-        if grid is not None and grid.mask:
-            import torch
-            self.t["grid"] = torch.from_numpy(np.ascontiguousarray(grid.values, np.float32)
-                                              .reshape(-1).copy()).to(self.t["step"].device)
-            hd.grid_mask = grid.mask
-            hd.grid = _ptr(self.t["grid"])
-            for d in range(3):
-                hd.grid_axis[d] = int(grid.axes[d])
-                hd.grid_n[d] = int(grid.n[d])
-                hd.grid_lo[d] = float(grid.lo[d])
-                hd.grid_hi[d] = float(grid.hi[d])
+        self.t.update(_select(hd, bounded, grid, self.t["step"].device))
         return hd
 
     @property
@@ -584,9 +589,11 @@ def _whole(t):
     return _ptr(t)
 
 
-def gated_heads(w1, w2, w3, b3) -> ks_heads:
+def gated_heads(w1, w2, w3, b3, bounded=None, grid=None) -> ks_heads:
     """Gated heads (mode KS_ETA_GATED) over w1, w2 [NFAM][hidden][in_dim], w3
-    [NFAM][hidden], b3 [NFAM], all fp32 or all bf16."""
+    [NFAM][hidden], b3 [NFAM], all fp32 or all bf16.  bounded, grid: families that the
+    evaluation prices by the bounded head or a measured grid, as for
+    ``DeviceInputs.make_heads``; their device arrays stay with the struct (``pool``)."""
     hd = ks_heads()
     _, hd.hidden, hd.in_dim = w1.shape
     want = {"w1": (NFAM, hd.hidden, hd.in_dim), "w2": (NFAM, hd.hidden, hd.in_dim), "w3": (NFAM, hd.hidden), "b3": (NFAM,)}
@@ -597,6 +604,7 @@ def gated_heads(w1, w2, w3, b3) -> ks_heads:
     hd.precision, hd.mode = _precision(w1), KS_ETA_GATED
     hd.place = _place((w1, w2, w3, b3))
     hd.fits = (hd.place, hd.in_dim, hd.precision) if hd.place >= 0 else None
+    hd.pool = _select(hd, bounded, grid, w1.device)
     return hd
 
 

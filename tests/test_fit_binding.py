@@ -104,3 +104,26 @@ def test_adamw():
     for bad in (z(1), z(2, dtype=torch.int32), z(1, dtype=torch.int64)):
         with pytest.raises(ValueError):
             abi.adamw_config(1e-3, step_dev=bad)
+
+
+def test_gated_heads_beside_the_bounded_head_and_grids():
+    """The fields that make_heads fills for MLP heads, with arrays that live as long as the
+    struct."""
+    import ctypes as C
+
+    import numpy as np
+
+    from workload import gen
+    bounded, grid = gen.make_bounded(0b1000010010), gen.make_grid(0b0000100001)
+    h = abi.gated_heads(*tensors(), bounded=bounded, grid=grid)
+    m = abi.DeviceInputs(gen.config1(0, 1), device="cpu").make_heads("f32", 16, 64, abi.KS_ETA_GATED, bounded, grid)
+    assert (h.mode, h.hidden, h.in_dim) == (abi.KS_ETA_GATED, 8, 16)
+    for name in ("bounded_mask", "grid_mask"):
+        assert getattr(h, name) == getattr(m, name) != 0
+    for name in ("grid_axis", "grid_n", "grid_lo", "grid_hi"):
+        assert list(getattr(h, name)) == list(getattr(m, name)), name
+    for at, want in ((h.bounded, bounded.storage), (h.grid, grid.values)):
+        got = np.frombuffer((C.c_float * want.size).from_address(at), np.float32)
+        np.testing.assert_array_equal(got, np.asarray(want, np.float32).reshape(-1))
+    plain = abi.gated_heads(*tensors())
+    assert plain.bounded_mask == plain.grid_mask == 0 and plain.bounded is None and plain.grid is None

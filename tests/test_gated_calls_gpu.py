@@ -11,8 +11,9 @@ from oracle import ks_expand as ox
 from oracle import ks_oracle as o
 from oracle import ks_sim as osim
 from paper_2606_28565_amd import abi
+from tests import gpu_helpers as g
 from tests.test_gated_eval_gpu import REL, REL_BF16, gated_oracle, weights
-from tests.test_gated_gpu import check_grads, heads_of, make
+from tests.test_gated_gpu import NFAM, check_grads, heads_of, make
 from tests.test_sim_gpu import gpu_steps, host_struct, one_spec, replay, sched_struct, spec_row, u32
 from workload import gen
 
@@ -70,3 +71,22 @@ def test_simulated_steps_are_the_gated_heads(prec, inp, hid):
     for i, step in enumerate(gpu_steps(res)):
         lat = want([(q, hist) for _, q, hist in step], bool(res["step_prefill"][i]))
         assert abs(res["step_latency"][i] - lat) <= tol * lat, i
+
+
+def test_gated_heads_beside_the_bounded_head_and_grids():
+    """Built by gated_heads alone: families on the bounded head or a grid take it, the
+    others the gated block, as the oracle has them."""
+    import torch
+    wl = gen.config1(0, 8)
+    ns = len(wl.specs["peak_flops"])
+    d, w = weights("f32", 16, 96)
+    di = abi.DeviceInputs(wl)
+    for bounded, grid, share in ((gen.make_bounded(0b1000010010), None, 1.0), (None, gen.make_grid((1 << NFAM) - 1), 0.999)):
+        ref = gated_oracle(wl, w, 16, False, ns, bounded=bounded, grid=grid)
+        hd = abi.gated_heads(d["w1"], d["w2"], d["w3"], d["b3"], bounded, grid)
+        ko_t, ko = abi.kernel_outputs(wl.desc.n_rows, ns, counts=False)
+        abi.ks_eval_kernels(di.desc, di.specs_ptr, ns, hd, ko, di.ws_ptr, di.ws_bytes, abi.current_stream())
+        torch.cuda.synchronize()
+        off = g.rel_err(ko_t["eta"].cpu().numpy(), ref["eta"])
+        # (a grid's query within rounding of the box or of a cell face may go either way)
+        assert (off <= (REL if grid is None else 1e-4)).mean() >= share
