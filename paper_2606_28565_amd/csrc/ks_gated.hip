@@ -305,7 +305,8 @@ __global__ __launch_bounds__(512, (!LOSS && (BF16 || IN == 16) ? 4 : 2)) void k_
     }
   };
   // (a step's rows are on their way while the step before is worked on; fp32 with 16
-  // inputs has no registers left for them, and a LOSS has one step otherwise)
+  // inputs has no registers left for them, it spills two of its 130 as it is, and a LOSS
+  // has one step otherwise)
   constexpr bool kAhead = BF16 ? !LOSS : IN == 32;
   if (kAhead) fetch(begin + 16 * wave);
   if (LOSS && threadIdx.x < 256)

@@ -321,9 +321,10 @@ struct GatedParams {
 // k_gated_sums: rows a workgroup takes at a time, units per wave; floats of its sums:
 // by groups of 32 units dW1 and dW2 (the last group whole), then db3
 constexpr int kGatedStep = 128, kGatedGroup = 32;
-// ... and at most in a launch: the matrix instruction's sums come out low by some 7e-12
-// of themselves for every row (it drops what lies far below the running sum), so a
-// sum in registers ends there and is added, rounded to nearest, to those before it
+// ... and at most in a launch.  The matrix instruction drops what lies far below its
+// running sum: sums of one sign come out low by 4e-12 (fp32 heads of 32 inputs, of whose
+// products each is six: 7e-12) of themselves a row, 1e-6 at 130M rows.  So a sum in
+// registers ends there and is added, rounded to nearest, to those before it.
 constexpr int kGatedRun = 64 * kGatedStep;
 constexpr int gated_part_size(int hidden, int in_dim) {
   return (hidden + kGatedGroup - 1) / kGatedGroup * kGatedGroup * 2 * in_dim + 1;
