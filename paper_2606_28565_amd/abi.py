@@ -629,7 +629,7 @@ def feature_rows(x, fam_off) -> ks_rows:
 
 
 def gated_grad(w1=None, w2=None, w3=None, b3=None, x=None) -> ks_gated_grad:
-    """Where the gradients go: fp32 tensors of the weights' shapes; x [n][in_dim]
+    """Where the gradients go: fp32 tensors of the weights' shapes (or flat); x [n][in_dim]
     of the rows' type (any row stride) or None."""
     g = ks_gated_grad()
     for name, t in (("w1", w1), ("w2", w2), ("w3", w3), ("b3", b3)):
@@ -637,11 +637,12 @@ def gated_grad(w1=None, w2=None, w3=None, b3=None, x=None) -> ks_gated_grad:
             raise ValueError(f"the gradient of {name} is not fp32")
         setattr(g, name, _whole(t))
     if all(t is not None for t in (w1, w2, w3, b3)):
-        hidden, in_dim = w1.shape[1:] if w1.dim() == 3 else (0, 0)
-        for name, t, want in (("w1", w1, (NFAM, hidden, in_dim)), ("w2", w2, (NFAM, hidden, in_dim)),
-                              ("w3", w3, (NFAM, hidden)), ("b3", b3, (NFAM,))):
-            if tuple(t.shape) != want:
-                raise ValueError(f"the gradient of {name} is {tuple(t.shape)}, not {want}")
+        hidden = w3.numel() // NFAM
+        in_dim = w1.numel() // (NFAM * hidden) if hidden else 0
+        for name, t, want in (("w1", w1, NFAM * hidden * in_dim), ("w2", w2, NFAM * hidden * in_dim), ("w3", w3, NFAM * hidden),
+                              ("b3", b3, NFAM)):
+            if t.numel() != want:
+                raise ValueError(f"the gradient of {name} has {t.numel()} elements, not {want}")
         g.made = (hidden, in_dim)
     if x is not None:
         g.ldx = _row_stride(x)
@@ -692,7 +693,7 @@ def adamw_tensors(tensors):
 def adamw_config(lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, state_bits=32, step=1,
                  step_dev=None) -> ks_adamw_config:
     """step_dev: an int32 tensor of one element counting the steps made, or None."""
-    if step_dev is not None and (step_dev.numel() != 1 or str(step_dev.dtype) not in ("torch.int32", "torch.uint32")):
+    if step_dev is not None and (step_dev.numel() < 1 or step_dev.is_floating_point() or step_dev.element_size() < 4):
         raise ValueError(f"step_dev is {step_dev.dtype} of {step_dev.numel()} elements, not one int32")
     c = ks_adamw_config(lr, beta1, beta2, eps, grad_scale, state_bits, 0, step, _ptr(step_dev))
     c.place = _place((step_dev,))

@@ -78,9 +78,12 @@ def test_gradients_of_another_shape():
     assert refused(h, r, made(abi.gated_grad(x=torch.zeros(21, 40)), 0), t) == 0    # (room for more)
     w1, w2, w3, b3 = tensors()
     for bad in ((w1, w2[:, :7].contiguous(), w3, b3), (w1, w2, w3[:, :5].contiguous(), b3), (w1, w2, w3, b3[:3]),
-                (w1.reshape(-1), w2, w3, b3)):
+                (w1[:, :, :15].contiguous(), w2, w3, b3), (w1, w2, w3[:0], b3)):
         with pytest.raises(ValueError):
             abi.gated_grad(*bad)
+    flat = [v.reshape(-1) for v in (w1, w2, w3, b3)]      # (parts of one buffer, as an optimiser may keep them)
+    assert refused(h, r, made(abi.gated_grad(*flat), 0), t) == 0
+    assert refused(h, r, made(abi.gated_grad(*(v.reshape(-1) for v in tensors(16, 8))), 0), t) == 2
 
 
 def test_targets_of_another_length():
@@ -101,7 +104,7 @@ def test_adamw():
         with pytest.raises(ValueError):
             abi.ks_adamw(made(abi.adamw_config(1e-3, step_dev=count), cp), made(arr, tp), None)
     assert abi.ks_adamw(made(abi.adamw_config(-1.0, step_dev=count), 0), made(arr, 0), None, check=False) == abi.KS_EINVAL
-    for bad in (z(1), z(2, dtype=torch.int32), z(1, dtype=torch.int64)):
+    for bad in (z(1), z(0, dtype=torch.int32), z(1, dtype=torch.int16)):
         with pytest.raises(ValueError):
             abi.adamw_config(1e-3, step_dev=bad)
 
