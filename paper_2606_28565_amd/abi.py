@@ -566,14 +566,11 @@ _KIND = {KS_F32: "fp32", KS_BF16: "bf16"}
 
 
 def _place(tensors) -> int | None:
-    """The GPU that holds all of them; None without any."""
-    on = {t.device for t in tensors if t is not None}
+    """The GPU that holds all of them (-1: the CPU does); None without any."""
+    on = {t.get_device() for t in tensors if t is not None}
     if len(on) > 1:
-        raise ValueError(f"tensors on {', '.join(sorted(map(str, on)))}, not on one device")
-    if not on:
-        return None
-    d = on.pop()
-    return -1 if d.type != "cuda" else d.index or 0
+        raise ValueError(f"tensors on GPUs {sorted(on)} (-1: the CPU), not on one device")
+    return on.pop() if on else None
 
 
 def _precision(t) -> int:
