@@ -570,6 +570,100 @@ typedef struct ks_adamw_config {
  * elements of a param.  Launches: one for every 200 tensors, one more with step_dev. */
 ks_status ks_adamw(const ks_adamw_config *config, const ks_tensor *tensors, int32_t n_tensors, hipStream_t stream);
 
+/*
+ * Learned columns of a fit (Sec. 5.4-5.5: what a device adds to its datasheet is learned
+ * from its measurements).  Rows of features say nothing of what they were measured on; a
+ * category does: an id per row (a device, a library's version, an element type), whose
+ * learned columns stand beside the features.  ks_embed looks them up, ks_dropout drops
+ * elements of features (the lookup and its gradient drop learned columns themselves),
+ * ks_eta_loss turns ks_gated_forward's z into the loss and the dz that ks_gated_backward
+ * takes, and ks_embed_backward sums the rows' gradients into the table's, over the order of
+ * the ids that ks_embed_sort finds.  For one category the learned columns e are a bias of
+ * the gates and ups: with feature 15 = 1, W1[:, 15] + W1[:, 16:] e and W2's likewise make
+ * heads of 16 inputs, which the evaluation and the simulation take.
+ * The calls behave as those of the fit above: asynchronous, no allocation, capturable, a
+ * workspace (256-byte aligned) for each that may run at the same time; what a call writes may
+ * not overlap what else it reads or writes, but where said.
+ */
+
+/* Rows of a device array: element (i, j) at p + i ld + j, of type KS_F32 or KS_BF16, with
+ * any base of the type's alignment.  n_rows < 2^31, n_cols 1 .. 2^20, ld n_cols .. 2^20.
+ * Rows of 16 bytes' alignment are read and written fastest; what lies between the columns
+ * of one row and the next row is left alone. */
+typedef struct ks_matrix {
+  void *p;
+  int64_t n_rows, n_cols, ld;
+  int32_t type, reserved;
+} ks_matrix;
+
+/*
+ * Dropout from a counter: nothing is stored, and the same struct over a matrix of as many
+ * columns drops the same elements (a pass and its gradient, in any layout or type).
+ * Element (i, j) of a matrix of c columns takes draw j % 8 of block i ceil(c / 8) + j / 8: 16
+ * bits of Philox4x32-10 (Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", 2011)
+ * with the counter (block's low word, its high word, step, site) and the key (seed's low
+ * word, high word), low half of each of the four words first.  It stays where the draw is at
+ * least T = round(2^16 p) and is multiplied by 2^16 / (2^16 - T), so that its expected value
+ * is x whatever p; else it is 0, whatever x was.  T = 2^16 drops everything.
+ */
+typedef struct ks_drop {
+  double p;                        /* 0 .. 1, taken in steps of 2^-16          */
+  uint64_t seed;
+  uint32_t site;                   /* which of a step's dropouts               */
+  uint32_t step;
+  const uint32_t *step_dev;        /* NULL, or a device counter read in place of
+                                      step: ks_adamw's, so that a captured step
+                                      draws anew in each replay                */
+} ks_drop;
+
+/* y = drop(x): matrices of the same shape and type.  y may be x itself (the same address
+ * and ld); where it is other columns of x's buffer, with its ld, they may not meet. */
+ks_status ks_dropout(const ks_drop *drop, const ks_matrix *x, const ks_matrix *y, hipStream_t stream);
+
+/* y_i = drop(scale table_{ids_i}) for every row of y: ids device [y.n_rows], table one row
+ * per id, as many columns as y.  An id at or beyond table.n_rows (2^32 - 1 among them: no
+ * category, padding) gives zeros.  Computed in fp32, rounded once to y's type; scale finite
+ * in fp32.  drop: NULL for none. */
+ks_status ks_embed(const ks_matrix *table, double scale, const uint32_t *ids, const ks_drop *drop, const ks_matrix *y,
+                   hipStream_t stream);
+
+/* The rows by id (device arrays): row [n_rows] the rows' indices, by id and within one id
+ * ascending, id [n_rows] their ids (n_ids for those at or beyond n_ids, which come last), off
+ * [n_ids + 1]: id v has row[off[v]] .. row[off[v + 1] - 1].  n_rows < 2^31, n_ids 1 .. 2^31 - 1.
+ * Good for as long as the ids are the same. */
+typedef struct ks_id_order {
+  int64_t n_rows, n_ids;
+  uint32_t *row, *id, *off;
+} ks_id_order;
+
+/* Bytes of device workspace for ks_embed_sort; 0 on bad arguments.  Only sizes are read. */
+size_t ks_embed_sort_workspace_bytes(const ks_id_order *order);
+
+/* Finds the order of ids (device [n_rows]).  The same ids give the same order. */
+ks_status ks_embed_sort(const uint32_t *ids, const ks_id_order *order, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Bytes of device workspace for ks_embed_backward; 0 on bad arguments.  Only sizes are
+ * read. */
+size_t ks_embed_backward_workspace_bytes(const ks_id_order *order, const ks_matrix *dy);
+
+/* The table's gradient: grad_v = scale sum of drop(dy_i) over the rows i of id v, grad: KS_F32
+ * [n_ids][dy.n_cols], every row written (zeros for an id without rows); drop and scale as in
+ * the lookup.  Sums are formed in fp32 in a fixed order: the same call gives the same bits.
+ * An order that ks_embed_sort did not make gives sums of something else, of rows below
+ * n_rows only. */
+ks_status ks_embed_backward(const ks_id_order *order, double scale, const ks_matrix *dy, const ks_drop *drop,
+                            const ks_matrix *grad, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Bytes of device workspace for ks_eta_loss; 0 on bad arguments. */
+size_t ks_eta_loss_workspace_bytes(const int64_t fam_off[KS_NFAM + 1]);
+
+/* ks_gated_loss's loss at the z given (device [fam_off[KS_NFAM]], family-major, fam_off a
+ * host array with fam_off[0] = 0 and fewer than 2^31 rows): loss device [KS_NFAM], and dz
+ * (device, as z; may be z itself) the gradient of sum_f loss[f]; 0 for a row that does not count,
+ * whatever its z. */
+ks_status ks_eta_loss(const int64_t fam_off[KS_NFAM + 1], const float *z, const ks_eta_target *target, float *loss,
+                      float *dz, void *ws, size_t ws_bytes, hipStream_t stream);
+
 /* Synchronous device-side check of the inputs: step order within families,
  * field limits, request and expert offsets, spec sanity.  Synchronizes the
  * stream.  Returns KS_OK, KS_EINVAL or KS_ERANGE with a message. */

@@ -132,6 +132,22 @@ class ks_adamw_config(C.Structure):
                 ("step", C.c_int64), ("step_dev", P)]
 
 
+class ks_matrix(C.Structure):
+    place = None
+    _fields_ = [("p", P), ("n_rows", C.c_int64), ("n_cols", C.c_int64), ("ld", C.c_int64), ("type", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class ks_drop(C.Structure):
+    place = None
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("site", C.c_uint32), ("step", C.c_uint32), ("step_dev", P)]
+
+
+class ks_id_order(C.Structure):
+    place = None
+    _fields_ = [("n_rows", C.c_int64), ("n_ids", C.c_int64), ("row", P), ("id", P), ("off", P)]
+
+
 assert C.sizeof(ks_spec) == 64
 
 
@@ -195,6 +211,23 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     lib.ks_features.restype = C.c_int
     lib.ks_adamw.argtypes = [C.POINTER(ks_adamw_config), P, C.c_int32, P]
     lib.ks_adamw.restype = C.c_int
+    pm, pdr, po, pf = C.POINTER(ks_matrix), C.POINTER(ks_drop), C.POINTER(ks_id_order), C.POINTER(C.c_int64)
+    lib.ks_dropout.argtypes = [pdr, pm, pm, P]
+    lib.ks_dropout.restype = C.c_int
+    lib.ks_embed.argtypes = [pm, C.c_double, P, pdr, pm, P]
+    lib.ks_embed.restype = C.c_int
+    lib.ks_embed_sort_workspace_bytes.argtypes = [po]
+    lib.ks_embed_sort_workspace_bytes.restype = C.c_size_t
+    lib.ks_embed_sort.argtypes = [P, po, P, C.c_size_t, P]
+    lib.ks_embed_sort.restype = C.c_int
+    lib.ks_embed_backward_workspace_bytes.argtypes = [po, pm]
+    lib.ks_embed_backward_workspace_bytes.restype = C.c_size_t
+    lib.ks_embed_backward.argtypes = [po, C.c_double, pm, pdr, pm, P, C.c_size_t, P]
+    lib.ks_embed_backward.restype = C.c_int
+    lib.ks_eta_loss_workspace_bytes.argtypes = [pf]
+    lib.ks_eta_loss_workspace_bytes.restype = C.c_size_t
+    lib.ks_eta_loss.argtypes = [pf, P, C.POINTER(ks_eta_target), P, P, P, C.c_size_t, P]
+    lib.ks_eta_loss.restype = C.c_int
     lib.ks_set_timing_events.argtypes = [P, P]
     lib.ks_set_timing_events.restype = C.c_int
     lib.ks_different_families.argtypes = [C.POINTER(ks_desc), C.c_int32, C.POINTER(ks_heads), C.POINTER(ks_kernel_out),
@@ -351,6 +384,70 @@ def ks_adamw(config, tensors, stream, check=True):
     if at == -1 or count == -1 or (count is not None and at is not None and at != count):
         raise ValueError("tensors or step_dev on the CPU, or on different GPUs")
     st = (_lib or load()).ks_adamw(C.byref(config), tensors, len(tensors), stream)
+    return _check(st) if check else st
+
+
+def _one_place(*structs):
+    """Refuses structs that the marshalling helpers made for tensors on the CPU or on
+    different GPUs; those filled by hand are taken as they are."""
+    at = None
+    for s in structs:
+        if s is None or s.place is None:
+            continue
+        if s.place < 0 or (at is not None and s.place != at):
+            raise ValueError("tensors on the CPU, or on different GPUs")
+        at = s.place
+
+
+def _ref(s):
+    return None if s is None else C.byref(s)
+
+
+def ks_dropout(drop, x, y, stream, check=True):
+    _one_place(drop, x, y)
+    st = (_lib or load()).ks_dropout(_ref(drop), C.byref(x), C.byref(y), stream)
+    return _check(st) if check else st
+
+
+def ks_embed(table, scale, ids_ptr, drop, y, stream, check=True):
+    """drop: a ks_drop, or None."""
+    _one_place(table, drop, y)
+    st = (_lib or load()).ks_embed(C.byref(table), scale, ids_ptr, _ref(drop), C.byref(y), stream)
+    return _check(st) if check else st
+
+
+def ks_embed_sort_workspace_bytes(order) -> int:
+    return load().ks_embed_sort_workspace_bytes(C.byref(order))
+
+
+def ks_embed_sort(ids_ptr, order, ws_ptr, ws_bytes, stream, check=True):
+    _one_place(order)
+    st = (_lib or load()).ks_embed_sort(ids_ptr, C.byref(order), ws_ptr, ws_bytes, stream)
+    return _check(st) if check else st
+
+
+def ks_embed_backward_workspace_bytes(order, dy) -> int:
+    return load().ks_embed_backward_workspace_bytes(C.byref(order), C.byref(dy))
+
+
+def ks_embed_backward(order, scale, dy, drop, grad, ws_ptr, ws_bytes, stream, check=True):
+    """drop: a ks_drop, or None."""
+    _one_place(order, dy, drop, grad)
+    st = (_lib or load()).ks_embed_backward(C.byref(order), scale, C.byref(dy), _ref(drop), C.byref(grad), ws_ptr,
+                                            ws_bytes, stream)
+    return _check(st) if check else st
+
+
+def ks_eta_loss_workspace_bytes(fam_off) -> int:
+    """fam_off: see family_offsets."""
+    return load().ks_eta_loss_workspace_bytes(fam_off)
+
+
+def ks_eta_loss(fam_off, z_ptr, target, loss_ptr, dz_ptr, ws_ptr, ws_bytes, stream, check=True):
+    _one_place(target)
+    if target.made is not None and target.made < fam_off[NFAM]:
+        raise ValueError(f"{target.made} measured eta for {fam_off[NFAM]} rows")
+    st = (_lib or load()).ks_eta_loss(fam_off, z_ptr, C.byref(target), loss_ptr, dz_ptr, ws_ptr, ws_bytes, stream)
     return _check(st) if check else st
 
 
@@ -695,6 +792,45 @@ def adamw_config(lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, state_bit
     c = ks_adamw_config(lr, beta1, beta2, eps, grad_scale, state_bits, 0, step, _ptr(step_dev))
     c.place = _place((step_dev,))
     return c
+
+
+# --------------------------------------------------------------------------
+# learned columns: torch device tensors -> ctypes structs (which hold addresses only,
+# but for id_order's, which keeps its tensors)
+# --------------------------------------------------------------------------
+def matrix(t) -> ks_matrix:
+    """Rows t [n][columns] (fp32 or bf16, any row stride): a table, rows to fill or drop
+    elements of, or their gradients."""
+    ld = _row_stride(t)
+    m = ks_matrix(_ptr(t) if t.numel() else None, t.shape[0], t.shape[1], ld if t.shape[0] > 1 else t.shape[1], _precision(t))
+    m.place = _place((t,))
+    return m
+
+
+def drop(p, seed, site=0, step=0, step_dev=None) -> ks_drop:
+    """Dropout of a share p; step_dev: an int32 tensor of one element that counts the
+    steps (read in place of step), or None."""
+    if step_dev is not None and (step_dev.numel() < 1 or step_dev.is_floating_point() or step_dev.element_size() < 4):
+        raise ValueError(f"step_dev is {step_dev.dtype} of {step_dev.numel()} elements, not one int32")
+    d = ks_drop(p, seed, site, step, _ptr(step_dev))
+    d.place = _place((step_dev,))
+    return d
+
+
+def id_order(n_rows, n_ids, device="cuda") -> ks_id_order:
+    """Room for the order of n_rows ids below n_ids; its tensors stay with the struct
+    (``t``)."""
+    import torch
+    t = {name: torch.empty(n, dtype=torch.int32, device=device)
+         for name, n in (("row", n_rows), ("id", n_rows), ("off", n_ids + 1))}
+    o = ks_id_order(n_rows, n_ids, *(_ptr(v) if v.numel() else None for v in t.values()))
+    o.t, o.place = t, _place(t.values())
+    return o
+
+
+def family_offsets(fam_off):
+    """The ctypes array that ks_eta_loss takes."""
+    return (C.c_int64 * (NFAM + 1))(*(int(v) for v in fam_off))
 
 
 # --------------------------------------------------------------------------

@@ -23,6 +23,8 @@
 namespace ks {
 
 using gated::Block;
+using gated::EtaTerm;
+using gated::eta_term;
 using gated::gbf16x8;
 using gated::gf32x16;
 using gated::gf32x4;
@@ -76,31 +78,6 @@ __device__ __forceinline__ void load8(gu32x4 (&v)[BF16 ? 1 : 2], const void *x, 
       for (int j = 0; j < 8; ++j) v[j >> 2][j & 3] = p[j];
     }
   }
-}
-
-// One row's part of the loss on log eta: w rho(r), and w drho/dz.  log(1 + e^-z) is
-// max(-z, 0) + log(1 + e), e = exp(-|z|) <= 1.  On the hardware's exponential and
-// logarithm (within 2^-23 relative, the logarithm near 1 too): the exponent's
-// rounding is put back to first order, and the logarithm of the rounded 1 + e
-// corrected for that rounding, which keeps it exact relative to a small e.
-struct EtaTerm {
-  float loss, dz;
-};
-__device__ __forceinline__ EtaTerm eta_term(float z, float eta, float weight, float huber) {
-  constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-  const float t = fabsf(z) * -kLog2e, lo = fmaf(fabsf(z), -kLog2e, -t) - fabsf(z) * 1.92596299e-8f;
-  float e = __builtin_amdgcn_exp2f(t);
-  e = fmaf(e * kLn2, lo, e);
-  if (!(fabsf(z) < 126.0f)) e = z == z ? 0.0f : z;   // (below the normal range; t - t is no number at infinity)
-  const float w = 1.0f + e;
-  const float log1 = fmaf(__builtin_amdgcn_logf(w), kLn2, (e - (w - 1.0f)) * __builtin_amdgcn_rcpf(w));
-  const float at = eta < 0x1p-126f ? eta * 0x1p32f : eta;   // (the logarithm takes normal numbers)
-  const float res = fmaxf(-z, 0.0f) + log1 - (__builtin_amdgcn_logf(at) - (eta < 0x1p-126f ? 32.0f : 0.0f)) * kLn2;
-  const float size = fabsf(res);
-  const bool far = size > huber;   // (a NaN stays one)
-  const float rho = far ? huber * (size - 0.5f * huber) : 0.5f * res * res;
-  const float slope = far ? copysignf(huber, res) : res;
-  return {weight * rho, -weight * slope * sigmoid(-z)};   // d log(1 + e^-z) / dz = -sigma(-z)
 }
 
 // ------------------------------------------------------------ forward

@@ -334,6 +334,81 @@ hipError_t launch_gated_sums(const GatedParams &p, bool loss, hipStream_t s);
 hipError_t launch_gated_rows(const GatedParams &p, hipStream_t s);     // g_x
 hipError_t launch_gated_reduce(const GatedParams &p, hipStream_t s);   // gradients and the loss
 
+// ---- learned columns, dropout (ks_embed.hip) and the order of ids (ks_order.hip)
+// Eight columns of one row (a block of ks_drop's draws) are a lane's work; `blocks` of
+// them make a row, whose last one has `rem` columns (0: eight).
+struct Cols {
+  uint32_t blocks, rem;
+  uint32_t magic;                    // ceil(2^32 / blocks); 0: one block
+};
+struct Drop {
+  uint32_t key0, key1, site, step;
+  const uint32_t *step_dev;          // nullable
+  uint32_t least;                    // T: a draw at least this stays; 0: no dropout
+};
+struct EmbedParams {
+  const void *src;                   // x, or the table
+  void *dst;
+  int64_t src_ld, dst_ld, n_rows;
+  const uint32_t *ids;               // null: row i of src is i
+  uint32_t n_ids;
+  float factor;
+  Cols cols;
+  Drop drop;
+  int64_t wg0;                       // of a launch (set by it)
+};
+hipError_t launch_embed(const EmbedParams &p, bool src16, bool dst16, hipStream_t s);
+
+// Ids with at most kBackShort rows are summed by the lanes that write their rows of the
+// table, those with more by workgroups over `run` places of the order each, which leave a
+// sum for the run that began before their places (0) and for the one that goes on behind
+// them (1).
+constexpr int kBackThreads = 256;
+constexpr uint32_t kBackShort = 128, kBackRun = 8192;   // places a workgroup, at most
+constexpr uint32_t kBackMost = kBackRun / kBackShort + 2;   // ids with many rows among them, at most
+struct EmbedBackParams {
+  const void *dy;
+  int64_t ld, n_rows;
+  const uint32_t *row, *id, *off;
+  uint32_t n_ids;
+  float *grad;
+  int64_t grad_ld;
+  float factor;
+  Cols cols;
+  Drop drop;
+  int64_t short_wgs;
+  uint32_t run, runs, tiles;         // places a workgroup, parts of the order, tiles of columns
+  float *part;                       // [runs][2][8 blocks]
+  int64_t wg0;                       // of a launch (set by it)
+};
+hipError_t launch_embed_back(const EmbedBackParams &p, bool dy16, hipStream_t s);
+
+constexpr int kOrderThreads = 1024;  // of a workgroup that ranks keys
+constexpr int kOrderKeys = 4096;     // keys ranked at a time
+constexpr int kOrderBits = 10;       // of a digit, at most
+struct OrderParams {
+  const uint32_t *ids;
+  uint32_t n_rows, n_ids;
+  uint32_t *row, *id, *off;
+  uint32_t *tmp_row, *tmp_id;        // [n_rows]; null with one pass
+  uint32_t *hist, *total;            // [2^bits][chunks], [2^bits]
+  uint32_t chunk, chunks;            // keys of a workgroup, a multiple of kOrderKeys
+  int32_t bits, passes;
+};
+hipError_t launch_order(const OrderParams &p, hipStream_t s);
+
+// ---- the loss at given z (ks_eta.hip)
+struct EtaParams {
+  int64_t fam_off[KS_NFAM + 1];
+  int64_t rows;                      // of a workgroup
+  int32_t wg[KS_NFAM + 1];
+  const float *z, *eta, *weight;
+  float huber;
+  float *loss, *dz;
+  double *part;                      // [workgroups][2]
+};
+hipError_t launch_eta_loss(const EtaParams &p, hipStream_t s);
+
 // ---- AdamW (ks_adamw.hip)
 constexpr int kAdamTensors = 200;     // per launch: their table travels in the kernel arguments
 constexpr int kAdamChunk = 1024;     // elements per workgroup
