@@ -10,7 +10,20 @@ learn log eta from dimensionless features).
 
 A step is ks_gated_loss (loss and gradients) and ks_adamw (all tensors in one
 launch); it allocates nothing and can be captured into a graph.  Argument
-marshalling only, as in ``abi``: the arithmetic is in libks.so."""
+marshalling only, as in ``abi``: the arithmetic is in libks.so.
+
+Rows measured on different devices (library versions, element types) carry a category
+each, whose learned columns stand beside their 16 features:
+
+    data = Measurements(rows.x, rows.fam_off, eta, ids=device_of_row, categories=8)
+    fit = GatedFit(categories=8, dropout=0.1)
+    ...
+    abi.ks_eval_steps(..., fit.heads_for(3), ...)   # kernels of device 3
+    abi.ks_eval_steps(..., fit.heads_for(None), ...)   # of a device never measured
+
+A step is then ks_embed, ks_gated_forward, ks_eta_loss, ks_gated_backward, ks_embed_backward
+and ks_adamw.  Dropout (of learned columns; of features: ``feature_dropout``) draws anew in
+every step, in replays of a captured one too."""
 from __future__ import annotations
 
 from types import SimpleNamespace
@@ -34,27 +47,85 @@ def feature_rows_of(inputs: abi.DeviceInputs, in_dim: int = 16, precision: str =
     return SimpleNamespace(x=x, t_roof=roof, fam_off=[s * int(v) for v in inputs.desc.fam_off])
 
 
+FEATURES = 16     # before the learned columns, which are as many
+
+
 class Measurements:
     """Feature rows with their measured eta (NaN: never measured) and weights
-    (None: 1 each), kept on the device."""
+    (None: 1 each), kept on the device.  ids: an int32 category below ``categories`` for
+    each row of 16 features (others, as -1: none).  x is then a copy whose columns behind the
+    features are the learned ones, written by each step, and the ids' order is found once:
+    one fit at a time steps on such rows."""
 
-    def __init__(self, x, fam_off, eta, weight=None, huber: float = float("inf")):
+    def __init__(self, x, fam_off, eta, weight=None, huber: float = float("inf"), ids=None, categories: int = 0):
+        import torch
         if eta.shape != x.shape[:1]:
             raise ValueError(f"eta is {tuple(eta.shape)}, not one per row of {tuple(x.shape)}")
-        if any(t is not None and t.device != x.device for t in (eta, weight)):
-            raise ValueError("x, eta and weight are not on one device")
+        if any(t is not None and t.device != x.device for t in (eta, weight, ids)):
+            raise ValueError("x, eta, weight and ids are not on one device")
+        self.ids, self.categories, self.noisy = ids, 0, None
+        if ids is not None:
+            if ids.dtype != torch.int32 or ids.shape != eta.shape or not ids.is_contiguous():
+                raise ValueError(f"ids are {ids.dtype} {tuple(ids.shape)}, not int32 {tuple(eta.shape)}")
+            if x.shape[1] != FEATURES or categories < 1:
+                raise ValueError(f"rows of {x.shape[1]} features with {categories} categories: {FEATURES} and at least one")
+            self.categories = categories
+            x = torch.cat([x, torch.zeros_like(x)], 1)
         self.x, self.eta, self.weight = x, eta, weight
         self.rows = abi.feature_rows(x, fam_off)
         self.target = abi.eta_target(eta, weight, huber)
+        if ids is not None:
+            self._learned(fam_off)
+            self.sort()
+
+    def _learned(self, fam_off):
+        """What a step with learned columns writes and works in."""
+        import torch
+
+        def room(need):
+            return torch.empty(need, dtype=torch.uint8, device=self.x.device)
+        self.columns = abi.matrix(self.x[:, FEATURES:])
+        self.fam_off = abi.family_offsets(fam_off)
+        self.dz, self.dx = torch.empty_like(self.eta), torch.empty_like(self.x)
+        self.rows_grad, self.columns_grad = abi.gated_grad(x=self.dx), abi.matrix(self.dx[:, FEATURES:])
+        self.order = abi.id_order(len(self.eta), self.categories, self.x.device)
+        self.sort_ws = room(abi.ks_embed_sort_workspace_bytes(self.order))
+        self.back_ws = room(abi.ks_embed_backward_workspace_bytes(self.order, self.columns_grad))
+        self.loss_ws = room(abi.ks_eta_loss_workspace_bytes(self.fam_off))
+
+    def sort(self):
+        """The order of the ids; to be called again when they have changed."""
+        import torch
+        with torch.cuda.device(self.x.device):
+            abi.ks_embed_sort(self.ids.data_ptr(), self.order, self.sort_ws.data_ptr(), self.sort_ws.numel(),
+                              abi.current_stream())
+
+    def noise(self):
+        """Rows for a fit that drops features: theirs but the constant one are written by
+        each step."""
+        if self.noisy is None:
+            features = (FEATURES if self.categories else self.x.shape[1]) - 1
+            self.noisy = self.x.clone()
+            self.noisy_rows = abi.feature_rows(self.noisy, list(self.rows.fam_off))
+            self.noisy_columns = abi.matrix(self.noisy[:, FEATURES:]) if self.categories else None
+            self.noise_pair = abi.matrix(self.x[:, :features]), abi.matrix(self.noisy[:, :features])
 
 
 class GatedFit:
     """Gated heads under AdamW: fp32 parameters, states of ``state_bits`` (32 or 8),
-    and for precision "bf16" the bf16 copies that the heads read."""
+    and for precision "bf16" the bf16 copies that the heads read.  categories: how many
+    there are learned columns for (0: none; else in_dim is 32); dropout: of their
+    elements, feature_dropout: of the features but the constant one."""
 
     def __init__(self, in_dim: int = 16, hidden: int = 64, precision: str = "f32", seed: int = 0, lr: float = 3e-3,
-                 weight_decay: float = 0.0, state_bits: int = 32, device="cuda"):
+                 weight_decay: float = 0.0, state_bits: int = 32, device="cuda", categories: int = 0, dropout: float = 0.0,
+                 feature_dropout: float = 0.0):
         import torch
+        if categories < 0 or (dropout and not categories):
+            raise ValueError(f"{categories} categories, dropout of learned columns {dropout}")
+        if not (0.0 <= dropout < 1.0 and 0.0 <= feature_dropout < 1.0):
+            raise ValueError(f"dropout {dropout} or feature_dropout {feature_dropout} outside [0, 1)")
+        in_dim = 2 * FEATURES if categories else in_dim
         g = torch.Generator().manual_seed(seed)
         n = abi.NFAM
         # gates and ups of order 1 for features of order 1; b3 = 0 puts eta at 2
@@ -62,14 +133,21 @@ class GatedFit:
                       "w2": torch.randn(n, hidden, in_dim, generator=g) * (2.0 / in_dim) ** 0.5,
                       "w3": torch.randn(n, hidden, generator=g) * (1.0 / hidden) ** 0.5,
                       "b3": torch.zeros(n)}
+        if categories:   # (small: at first the rows differ by their features)
+            self.param["table"] = torch.randn(categories, FEATURES, generator=g) * 0.1
         self.param = {k: v.to(device) for k, v in self.param.items()}
         low = precision == "bf16"
         self.weights = {k: v.bfloat16() if low else v for k, v in self.param.items()}
         self.heads = abi.gated_heads(*(self.weights[k] for k in ("w1", "w2", "w3", "b3")))
         self.grad = {k: torch.zeros_like(v) for k, v in self.param.items()}
-        self.grad_struct = abi.gated_grad(**self.grad)
         self.loss = torch.zeros(n, device=device)
         self.count = torch.zeros(1, dtype=torch.int32, device=device)
+        self.grad_struct = abi.gated_grad(**{k: self.grad[k] for k in ("w1", "w2", "w3", "b3")})
+        self.drop = abi.drop(dropout, seed, 1, step_dev=self.count) if dropout else None
+        self.feature_drop = abi.drop(feature_dropout, seed, 0, step_dev=self.count) if feature_dropout else None
+        if categories:
+            self.table, self.table_grad = abi.matrix(self.weights["table"]), abi.matrix(self.grad["table"])
+        self.categories = categories
         self.state = {}
         tensors = []
         for k, v in self.param.items():
@@ -97,12 +175,16 @@ class GatedFit:
         if data.x.device != like.device or data.x.dtype != like.dtype or data.x.shape[1] != self.heads.in_dim:
             raise ValueError(f"rows are {data.x.dtype} [{data.x.shape[1]}] on {data.x.device}, "
                              f"not {like.dtype} [{self.heads.in_dim}] on {like.device}")
+        if data.categories != self.categories:
+            raise ValueError(f"rows of {data.categories} categories for a fit of {self.categories}")
         need = abi.ks_gated_workspace_bytes(self.heads, data.rows)
         if need == 0:
             raise abi.KsError(abi.KS_EINVAL, abi.ks_last_error())
         if self.ws is None or self.ws.numel() < need:
             self.ws = torch.empty(need, dtype=torch.uint8, device=self.loss.device)
             self.rooms.append(self.ws)
+        if self.feature_drop is not None:
+            data.noise()
         return need
 
     def gradients(self, data: Measurements):
@@ -111,8 +193,23 @@ class GatedFit:
         import torch
         need = self.workspace(data)
         with torch.cuda.device(self.loss.device):
-            abi.ks_gated_loss(self.heads, data.rows, data.target, self.loss.data_ptr(), None, self.grad_struct,
-                              self.ws.data_ptr(), need, abi.current_stream())
+            s, ws = abi.current_stream(), self.ws.data_ptr()
+            rows = data.rows
+            if self.feature_drop is not None:
+                rows = data.noisy_rows
+                abi.ks_dropout(self.feature_drop, *data.noise_pair, s)
+            if not self.categories:
+                abi.ks_gated_loss(self.heads, rows, data.target, self.loss.data_ptr(), None, self.grad_struct, ws, need, s)
+                return self.loss
+            columns, dz = data.columns if rows is data.rows else data.noisy_columns, data.dz.data_ptr()
+            abi.ks_embed(self.table, 1.0, data.ids.data_ptr(), self.drop, columns, s)
+            abi.ks_gated_forward(self.heads, rows, dz, s)
+            abi.ks_eta_loss(data.fam_off, dz, data.target, self.loss.data_ptr(), dz, data.loss_ws.data_ptr(),
+                            data.loss_ws.numel(), s)
+            abi.ks_gated_backward(self.heads, rows, dz, self.grad_struct, ws, need, s)
+            abi.ks_gated_backward(self.heads, rows, dz, data.rows_grad, ws, need, s)
+            abi.ks_embed_backward(data.order, 1.0, data.columns_grad, self.drop, self.table_grad, data.back_ws.data_ptr(),
+                                  data.back_ws.numel(), s)
         return self.loss
 
     def step(self, data: Measurements):
@@ -122,3 +219,24 @@ class GatedFit:
         with torch.cuda.device(loss.device):
             abi.ks_adamw(self.config, self.tensors, abi.current_stream())
         return loss
+
+    def heads_for(self, category: int | None = None, bounded=None, grid=None) -> abi.ks_heads:
+        """Heads of 16 features for one category (None: its learned columns are 0, as for
+        rows without one): feature 15 is 1, so what the learned columns e add to gates and
+        ups, W[:, 16:] e, goes to their column 15.  The weights as of now, in tensors that
+        stay with the struct (``weights``); bounded, grid: as for ``abi.gated_heads``."""
+        if not self.categories:
+            raise ValueError("a fit without categories: its heads are ``heads``")
+        if category is not None and not 0 <= category < self.categories:
+            raise ValueError(f"category {category} outside 0 .. {self.categories - 1}")
+        w = {k: self.weights[k].float() for k in ("w1", "w2")}
+        out = {k: v[:, :, :FEATURES].clone() for k, v in w.items()}
+        if category is not None:
+            e = self.weights["table"][category].float()
+            for k, v in w.items():
+                out[k][:, :, FEATURES - 1] += (v[:, :, FEATURES:] * e).sum(-1)
+        like = self.weights["w3"]
+        out = {k: v.to(like.dtype) for k, v in out.items()} | {k: self.weights[k].clone() for k in ("w3", "b3")}
+        heads = abi.gated_heads(out["w1"], out["w2"], out["w3"], out["b3"], bounded, grid)
+        heads.weights = out
+        return heads

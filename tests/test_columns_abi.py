@@ -342,3 +342,70 @@ def test_matrices_of_views():
     m = abi.matrix(buf[::2, 3:7])
     assert (m.n_rows, m.n_cols, m.ld) == (3, 4, 64)
     assert abi.matrix(buf[:0]).p is None and abi.matrix(buf[1:2, :4]).ld == 4
+
+
+# ------------------------------------------------------------------ the fit's refusals and its chain
+def test_fit_refuses_rows_that_do_not_go_together():
+    import torch
+    from paper_2606_28565_amd import fit
+    x, eta = torch.zeros(6, 16), torch.ones(6)
+    off = [0] * NFAM + [6]
+    ids = torch.zeros(6, dtype=torch.int32)
+    for bad in (dict(ids=ids.long(), categories=2), dict(ids=ids[:5], categories=2), dict(ids=ids, categories=0),
+                dict(ids=torch.zeros(12, dtype=torch.int32)[::2], categories=2)):
+        with pytest.raises(ValueError):
+            fit.Measurements(x, off, eta, **bad)
+    with pytest.raises(ValueError):
+        fit.Measurements(torch.zeros(6, 32), off, eta, ids=ids, categories=2)
+    for bad in (dict(dropout=0.1), dict(categories=-1), dict(categories=2, dropout=1.0), dict(feature_dropout=-0.1)):
+        with pytest.raises(ValueError):
+            fit.GatedFit(16, 8, device="cpu", **bad)
+    plain, learned = fit.GatedFit(32, 8, device="cpu"), fit.GatedFit(16, 8, device="cpu", categories=2)
+    assert learned.heads.in_dim == 32
+    with pytest.raises(ValueError):
+        learned.workspace(fit.Measurements(torch.zeros(6, 32), off, eta))
+    with pytest.raises(ValueError):
+        plain.heads_for(0)
+    for category in (-1, 2):
+        with pytest.raises(ValueError):
+            learned.heads_for(category)
+
+
+def test_heads_of_a_category_on_the_cpu():
+    """W[:, 16:] e goes to column 15, None leaves the 16 features' weights."""
+    import torch
+    from paper_2606_28565_amd import fit
+    ft = fit.GatedFit(16, 8, device="cpu", categories=3, precision="bf16")
+    h = ft.heads_for(1)
+    w, e = ft.weights["w2"].float(), ft.weights["table"][1].float()
+    want = w[:, :, 15] + (w[:, :, 16:] * e).sum(-1)
+    assert torch.equal(h.weights["w2"][:, :, 15], want.bfloat16()) and torch.equal(h.weights["w2"][:, :, :15], ft.weights["w2"][:, :, :15])
+    assert torch.equal(ft.heads_for().weights["w1"], ft.weights["w1"][:, :, :16]) and (h.hidden, h.in_dim) == (8, 16)
+
+
+def test_the_chain_against_differences():
+    """The loss by one element of the table at a time, through dropout, lookup, block and
+    loss: the gradients that a fit's step goes through."""
+    rng = np.random.default_rng(8)
+    n, c, hid = 12, 3, 5
+    x16, table = rng.random((n, 16)), rng.standard_normal((c, 16)) * 0.3
+    w1, w2, w3 = (rng.standard_normal(s) * 0.3 for s in ((hid, 32), (hid, 32), (hid,)))
+    ids = rng.integers(-1, c, n)
+    eta = 1 + np.exp(rng.standard_normal(n))
+    drop = (0.3, 99, 1, 4)
+
+    def chain(table):
+        x = np.concatenate([oc_drop, o.embed(table, 1.0, ids, drop)], 1)
+        z, k = of.block(x, w1, w2, w3, 0.1)
+        loss, dz = of.eta_loss(z, eta, None, 0.4)
+        return loss, x, dz, k
+    oc_drop = np.concatenate([o.drop(x16[:, :15], 0.2, 99, 0, 4), x16[:, 15:]], 1)
+    loss, x, dz, k = chain(table)
+    dx = of.gradients(x, w1, w2, w3, dz, k, 1)[0]["x"]
+    grad = o.embed_back(ids, c, dx[:, 16:], 1.0, drop)[0]
+    for v in range(c):
+        for j in range(16):
+            up, down = table.copy(), table.copy()
+            up[v, j] += 1e-5
+            down[v, j] -= 1e-5
+            assert abs((chain(up)[0] - chain(down)[0]) / 2e-5 - grad[v, j]) < 1e-8
