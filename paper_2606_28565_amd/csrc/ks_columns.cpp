@@ -154,20 +154,19 @@ OrderRoom room_of(const ks::OrderParams &p) {
   return r;
 }
 
-// The rows of ids with few rows by blocks of the table, the others by runs of places: 16
-// rows a thread, more where that is over 4096 workgroups for a tile of columns, kBackRun
-// places at most.
+// 16 places of the order for each group of lanes, more where that is over 2048 workgroups,
+// 4096 at most (64 runs of 64 additions).
 void plan(ks::EmbedBackParams &p, const ks_id_order *o, int64_t n_cols) {
   std::memset(&p, 0, sizeof p);
   p.n_rows = o->n_rows;
   p.n_ids = (uint32_t)o->n_ids;
   p.cols = cols_of(n_cols);
-  p.short_wgs = (o->n_ids * (int64_t)p.cols.blocks + ks::kBackThreads - 1) / ks::kBackThreads;
-  p.tiles = (p.cols.blocks + ks::kBackThreads - 1) / ks::kBackThreads;
-  if (o->n_rows <= (int64_t)ks::kBackShort) return;   // (no id has many rows)
-  const int64_t groups = ks::kBackThreads / std::min<int64_t>(p.cols.blocks, ks::kBackThreads);
-  const int64_t run = std::max<int64_t>({64, 16 * groups, (o->n_rows + 4095) / 4096});
-  p.run = (uint32_t)std::min<int64_t>((run + 63) / 64 * 64, ks::kBackRun);
+  p.fill_wgs = (o->n_ids * (int64_t)p.cols.blocks + ks::kBackThreads - 1) / ks::kBackThreads;
+  p.wide = std::min<uint32_t>(p.cols.blocks, ks::kBackThreads);
+  p.tiles = (p.cols.blocks + p.wide - 1) / p.wide;
+  const int64_t groups = ks::kBackThreads / p.wide, most = 2048 * 16 * groups;
+  p.each = (uint32_t)std::min<int64_t>(16 * std::max<int64_t>(1, (o->n_rows * p.tiles + most - 1) / most), 4096);
+  p.run = p.each * (uint32_t)groups;
   p.runs = (uint32_t)((o->n_rows + p.run - 1) / p.run);
 }
 size_t part_bytes(const ks::EmbedBackParams &p) {

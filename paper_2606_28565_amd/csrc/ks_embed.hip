@@ -2,8 +2,7 @@
 //
 //   k_embed        dst_i = drop(factor src_i), src_i the table's row of id i (the
 //                  lookup) or row i itself (dropout)
-//   k_embed_back   rows of the table's gradient: of ids with few rows, and the sums
-//                  over parts of the order of the others
+//   k_embed_back   rows of the table's gradient, of parts of the order
 //   k_embed_join   the sums of ids that have rows in more than one part
 //
 // A lane's work is a block of eight columns of one row: 16 bytes of bfloat16, 32 of
@@ -42,56 +41,67 @@ struct Eight {
   }
 };
 
-// the first `rem` of a row's last block (1 .. 7; the same in all lanes), or eight
+// Where block b of a row of `cols` columns is loaded from: its own place, or, where it is
+// the row's last one and not whole, the row's last eight columns, which `align8` moves
+// down.  One load for all lanes, where loads of four, two and one element wait for each
+// other.  (Rows of fewer than eight columns have no such place: `load_few`.)
+struct Place {
+  int64_t at;        // element in the row
+  bool part;         // not whole
+};
+__device__ __forceinline__ Place place_of(const Cols &c, uint32_t b) {
+  const bool part = c.rem != 0 && b + 1 == c.blocks;
+  return {8 * (int64_t)b - (part && c.blocks > 1 ? 8 - c.rem : 0), part};
+}
+
 template <bool B16>
-__device__ __forceinline__ Eight<B16> load8(const void *base, int64_t at, bool whole, uint32_t rem) {
+__device__ __forceinline__ Eight<B16> load_few(const void *base, int64_t at, uint32_t rem) {
   Eight<B16> o;
-  if constexpr (B16) {
-    const char *p = (const char *)base + 2 * at;
-    if (whole) {
-      o.w[0] = *(const any_u32x4 *)p;
-      return o;
-    }
-    o.w[0] = u32x4{0, 0, 0, 0};
-    if (rem & 4) {
-      const u32x2 v = *(const any_u32x2 *)p;
-      o.w[0][0] = v[0];
-      o.w[0][1] = v[1];
-    }
-    if (rem & 2) {
-      const uint32_t v = *(const any_u32 *)(p + 2 * (rem & 4));
-      if (rem & 4) o.w[0][2] = v;
-      else o.w[0][0] = v;
-    }
-    if (rem & 1) {
-      const uint32_t v = *(const uint16_t *)(p + 2 * (rem & 6));
+  o.w[0] = u32x4{0, 0, 0, 0};
+  if constexpr (!B16) o.w[1] = u32x4{0, 0, 0, 0};
 #pragma unroll
-      for (uint32_t j = 0; j < 4; ++j) o.w[0][j] = rem / 2 == j ? v : o.w[0][j];
-    }
-  } else {
-    const uint32_t *p = (const uint32_t *)base + at;
-    if (whole) {
-      o.w[0] = *(const any_u32x4 *)p;
-      o.w[1] = *(const any_u32x4 *)(p + 4);
-      return o;
-    }
-    o.w[0] = o.w[1] = u32x4{0, 0, 0, 0};
-    u32x4 v = {0, 0, 0, 0};
-    if (rem & 4) o.w[0] = *(const any_u32x4 *)p;
-    if (rem & 2) {
-      const u32x2 h = *(const any_u32x2 *)(p + (rem & 4));
-      v[0] = h[0];
-      v[1] = h[1];
-    }
-    if (rem & 1) {
-      const uint32_t h = p[rem & 6];
-      v[0] = rem & 2 ? v[0] : h;
-      v[2] = rem & 2 ? h : 0;
-    }
-    if (rem & 4) o.w[1] = v;
-    else o.w[0] = v;
+  for (uint32_t j = 0; j < 7; ++j) {
+    if (j >= rem) break;
+    if constexpr (B16) o.w[0][j / 2] |= (uint32_t)((const uint16_t *)base)[at + j] << (16 * (j & 1));
+    else o.w[j / 4][j % 4] = ((const uint32_t *)base)[at + j];
   }
   return o;
+}
+
+template <bool B16>
+__device__ __forceinline__ Eight<B16> load8(const void *base, int64_t at, const Cols &c) {
+  if (c.blocks == 1 && c.rem) return load_few<B16>(base, at, c.rem);
+  Eight<B16> o;
+  const char *p = (const char *)base + (B16 ? 2 : 4) * at;
+  o.w[0] = *(const any_u32x4 *)p;
+  if constexpr (!B16) o.w[1] = *(const any_u32x4 *)(p + 16);
+  return o;
+}
+
+// the last rem of eight elements down to the first places (with `part`; behind them stays
+// anything)
+template <bool B16>
+__device__ __forceinline__ void align8(Eight<B16> &x, const Cols &c, bool part) {
+  if (c.rem == 0 || c.blocks == 1) return;
+  const uint32_t by = 8 - c.rem;
+  if constexpr (B16) {
+    u32x4 &w = x.w[0];
+    if (by & 1)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = part ? __builtin_amdgcn_alignbit(j < 3 ? w[j < 3 ? j + 1 : 3] : 0u, w[j], 16) : w[j];
+    if (by & 2)
+#pragma unroll
+      for (int j = 0; j < 3; ++j) w[j] = part ? w[j + 1] : w[j];
+    if (by & 4)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) w[j] = part ? w[j + 2] : w[j];
+  } else {
+#pragma unroll
+    for (int s = 1; s < 8; s *= 2)
+      if (by & s)
+#pragma unroll
+        for (int j = 0; j + s < 8; ++j) x.w[j / 4][j % 4] = part ? x.w[(j + s) / 4][(j + s) % 4] : x.w[j / 4][j % 4];
+  }
 }
 
 __device__ __forceinline__ uint32_t pair(float lo, float hi) {
@@ -146,20 +156,26 @@ __device__ __forceinline__ Draws philox(const Drop &d, uint64_t block, uint32_t 
 }
 __device__ __forceinline__ uint32_t step_of(const Drop &d) { return d.step_dev ? *d.step_dev : d.step; }
 
-// row and block of the l-th block from row 0 on; l < 2^31
+// l / blocks and, in b, the rest; l < 2^32.  (ceil(2^32 / blocks) is at most blocks - 1 too
+// large: one too many, where l is large)
 __device__ __forceinline__ uint32_t row_in(const Cols &c, uint32_t l, uint32_t &b) {
   uint32_t q = c.magic ? __umulhi(l, c.magic) : l;
-  // (ceil(2^32 / blocks) is at most blocks - 1 over: one too many, where l is large)
-  if (c.magic && q * c.blocks > l) --q;
+  if (c.magic && (uint64_t)q * c.blocks > l) --q;
   b = l - q * c.blocks;
   return q;
 }
-// ... of the workgroup's lane l: the workgroup starts at block `first` of all
+// row and block of the workgroup's lane l: the workgroup starts at block `first` of all
 __device__ __forceinline__ int64_t row_of(const Cols &c, int64_t first, uint32_t l, uint32_t &b) {
-  const int64_t row = (uint64_t)first < (uint64_t(1) << 32) ? (int64_t)((uint32_t)first / c.blocks) : first / c.blocks;
-  return row + row_in(c, (uint32_t)(first - row * c.blocks) + l, b);
+  uint32_t b0;
+  int64_t row;
+  if ((uint64_t)first >> 32) {
+    row = first / c.blocks;
+    b0 = (uint32_t)(first - row * c.blocks);
+  } else {
+    row = row_in(c, (uint32_t)first, b0);
+  }
+  return row + row_in(c, b0 + l, b);
 }
-__device__ __forceinline__ bool whole(const Cols &c, uint32_t b) { return c.rem == 0 || b + 1 < c.blocks; }
 
 // ------------------------------------------------------------ lookup and dropout
 template <bool S16, bool D16, bool DROP>
@@ -168,11 +184,12 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams a) {
   const int64_t first = (a.wg0 + blockIdx.x) * kThreads;
   const int64_t i = row_of(a.cols, first, threadIdx.x, b);
   if (i >= a.n_rows) return;
-  const bool all = whole(a.cols, b);
+  const Place at = place_of(a.cols, b);
   const int64_t id = a.ids ? (int64_t)a.ids[i] : i;
   f32x8 v = {};
   if (!a.ids || id < a.n_ids) {
-    const Eight<S16> x = load8<S16>(a.src, id * a.src_ld + 8 * (int64_t)b, all, a.cols.rem);
+    Eight<S16> x = load8<S16>(a.src, id * a.src_ld + at.at, a.cols);
+    align8<S16>(x, a.cols, at.part);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = x[j] * a.factor;
   }
@@ -181,127 +198,181 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = d[j] >= a.drop.least ? v[j] : 0.0f;
   }
-  store8<D16>(a.dst, i * a.dst_ld + 8 * (int64_t)b, v, all, a.cols.rem);
+  store8<D16>(a.dst, i * a.dst_ld + 8 * (int64_t)b, v, !at.part, a.cols.rem);
 }
 
 // ------------------------------------------------------------ the table's gradient
-// acc += drop(dy of the row at place p of the order), columns of block b
-template <bool B16, bool DROP>
-__device__ __forceinline__ void add_row(f32x8 &acc, const EmbedBackParams &a, uint32_t p, uint32_t b, bool all, uint32_t step) {
-  const uint32_t i = a.row[p];
-  if (i >= a.n_rows) return;
-  const Eight<B16> x = load8<B16>(a.dy, (int64_t)i * a.ld + 8 * (int64_t)b, all, a.cols.rem);
-  if constexpr (DROP) {
-    const Draws d = philox(a.drop, (uint64_t)i * a.cols.blocks + b, step);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] += d[j] >= a.drop.least ? x[j] : 0.0f;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] += x[j];
-  }
-}
-
-// the places of id v
-__device__ __forceinline__ void places(const EmbedBackParams &a, uint32_t v, uint32_t &begin, uint32_t &end) {
-  const uint32_t n = (uint32_t)a.n_rows;
-  begin = min(a.off[v], n);
-  end = min(a.off[v + 1], n);
-}
-
+// The order's places are split evenly, whatever ids they have: a group of `wide` lanes
+// (the blocks of a row) walks `each` places in a row and adds up rows until the id
+// changes; `groups` of them, one behind the other, are a workgroup.  An id that begins and
+// ends in a group's places is written there.  Of the others a group keeps what ends in
+// it (head) and what goes on behind it (out), which a scan over the workgroup's groups
+// joins; what goes on beyond the workgroup k_embed_join joins.  The order of all sums
+// goes by sizes alone.
+//
+// A thread's sum: 64 additions in a row, then one for each such run.
 template <bool B16, bool DROP>
 __global__ __launch_bounds__(kBackThreads) void k_embed_back(EmbedBackParams a) {
-  const uint32_t step = DROP ? step_of(a.drop) : 0;
-  const int64_t at = a.wg0 + blockIdx.x;
-  if (at < a.short_wgs) {
+  const int64_t wg = a.wg0 + blockIdx.x;
+  const uint32_t n = min(a.off[a.n_ids], (uint32_t)a.n_rows);   // (behind: rows without an id)
+  if (wg >= (int64_t)a.runs * a.tiles) {
+    // ids without rows
     uint32_t b;
-    const int64_t v = row_of(a.cols, at * kBackThreads, threadIdx.x, b);
-    if (v >= a.n_ids) return;
-    uint32_t p, end;
-    places(a, (uint32_t)v, p, end);
-    if (end > p && end - p > kBackShort) return;
-    const bool all = whole(a.cols, b);
-    f32x8 acc = {};
-    for (; p < end; ++p) add_row<B16, DROP>(acc, a, p, b, all, step);
-    acc *= a.factor;
-    store8<false>(a.grad, v * a.grad_ld + 8 * (int64_t)b, acc, all, a.cols.rem);
+    const int64_t v = row_of(a.cols, (wg - (int64_t)a.runs * a.tiles) * kBackThreads, threadIdx.x, b);
+    if (v >= a.n_ids || a.off[v] < a.off[v + 1]) return;
+    store8<false>(a.grad, v * a.grad_ld + 8 * (int64_t)b, f32x8{}, !place_of(a.cols, b).part, a.cols.rem);
     return;
   }
-  // the ids with many rows that have some among this workgroup's places
-  __shared__ uint32_t begins[kBackMost], n_begins;
-  __shared__ float red[kBackThreads][8];
-  const uint32_t wg = (uint32_t)(at - a.short_wgs), part = wg / a.tiles, tile = wg % a.tiles;
-  const uint32_t n = (uint32_t)a.n_rows, lo = part * a.run, hi = n - lo < a.run ? n : lo + a.run;
-  if (threadIdx.x == 0) n_begins = 0;
-  __syncthreads();
-  for (uint32_t p = lo + threadIdx.x; p < hi; p += kBackThreads) {
-    const uint32_t v = a.id[p];
-    if (v >= a.n_ids || (p > lo && a.id[p - 1] == v)) continue;
-    uint32_t s, e;
-    places(a, v, s, e);
-    if (e > s && e - s > kBackShort) {
-      const uint32_t k = atomicAdd(&n_begins, 1u);   // (in any order: their sums do not meet)
-      if (k < kBackMost) begins[k] = p;
-    }
-  }
-  __syncthreads();
-  const uint32_t many = min(n_begins, (uint32_t)kBackMost);
-  const uint32_t wide = min(a.cols.blocks, (uint32_t)kBackThreads), groups = kBackThreads / wide;
+  constexpr uint32_t kBatch = B16 ? 8 : 4;
+  __shared__ float val[kBackThreads][8];
+  __shared__ uint32_t stop[kBackThreads];
+  const uint32_t step = DROP ? step_of(a.drop) : 0;
+  const uint32_t part = (uint32_t)(wg / a.tiles), tile = (uint32_t)(wg % a.tiles), lo = part * a.run;
+  if (lo >= n) return;
+  const uint32_t wide = a.wide, groups = kBackThreads / wide;
   const uint32_t g = threadIdx.x / wide, b = tile * wide + threadIdx.x % wide;
   const bool in = g < groups && b < a.cols.blocks;
-  const bool all = whole(a.cols, b);
-  for (uint32_t k = 0; k < many; ++k) {
-    const uint32_t v = a.id[begins[k]];
-    uint32_t s, e;
-    places(a, v, s, e);
-    const uint32_t from = max(s, lo), to = min(e, hi);
-    f32x8 acc = {};
-    if (in) {
-      // by runs of 64 rows a thread: 64 additions in a row, then one for each run
-      for (uint32_t p = from + g; p < to;) {
-        f32x8 sum = {};
-        for (int i = 0; i < 64 && p < to; ++i, p += groups) add_row<B16, DROP>(sum, a, p, b, all, step);
-        acc += sum;
+  const Place at = place_of(a.cols, min(b, a.cols.blocks - 1));
+  const uint32_t p0 = min(lo + g * a.each, n), p1 = g < groups ? min(p0 + a.each, n) : p0;
+  auto write = [&](uint32_t v, f32x8 s) {
+    if (!in || v >= a.n_ids) return;
+    s *= a.factor;
+    store8<false>(a.grad, (int64_t)v * a.grad_ld + 8 * (int64_t)b, s, !at.part, a.cols.rem);
+  };
+
+  f32x8 head = {}, out = {};
+  bool has_head = false, has_out = false, through = false;   // through: what goes on came from before
+  uint32_t head_id = 0;
+  if (p0 < p1) {
+    uint32_t cur = a.id[p0];
+    bool from_before = p0 > 0 && a.id[p0 - 1] == cur;
+    f32x8 acc = {}, sum = {};
+    uint32_t since = 0;
+    for (uint32_t p = p0; p < p1; p += kBatch) {
+      uint32_t id[kBatch], row[kBatch];
+      Eight<B16> x[kBatch];
+#pragma unroll
+      for (uint32_t u = 0; u < kBatch; ++u) {
+        const uint32_t q = min(p + u, p1 - 1);
+        id[u] = a.id[q];
+        row[u] = a.row[q];
+      }
+#pragma unroll
+      for (uint32_t u = 0; u < kBatch; ++u)
+        x[u] = load8<B16>(a.dy, (int64_t)min(row[u], (uint32_t)a.n_rows - 1) * a.ld + at.at, a.cols);
+#pragma unroll
+      for (uint32_t u = 0; u < kBatch; ++u) {
+        if (p + u >= p1) break;
+        if (id[u] != cur) {
+          acc += sum;
+          if (from_before) {
+            head = acc;
+            head_id = cur;
+            has_head = true;
+          } else {
+            write(cur, acc);
+          }
+          acc = sum = f32x8{};
+          since = 0;
+          cur = id[u];
+          from_before = false;
+        }
+        align8<B16>(x[u], a.cols, at.part);
+        if (row[u] < a.n_rows) {
+          if constexpr (DROP) {
+            const Draws d = philox(a.drop, (uint64_t)row[u] * a.cols.blocks + b, step);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += d[j] >= a.drop.least ? x[u][j] : 0.0f;
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += x[u][j];
+          }
+        }
+        if (++since == 64) {
+          acc += sum;
+          sum = f32x8{};
+          since = 0;
+        }
       }
     }
-    for (uint32_t half = 128; half > 0; half /= 2) {
-      if (half >= groups) continue;
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < 8; ++j) red[threadIdx.x][j] = acc[j];
-      __syncthreads();
-      if (in && g < half && g + half < groups) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] += red[threadIdx.x + half * wide][j];
-      }
-    }
-    if (!in || g > 0) continue;
-    if (s >= lo && e <= hi) {
-      acc *= a.factor;
-      store8<false>(a.grad, (int64_t)v * a.grad_ld + 8 * (int64_t)b, acc, all, a.cols.rem);
+    acc += sum;
+    const bool goes_on = p1 < n && a.id[p1] == cur;
+    if (goes_on) {
+      out = acc;
+      has_out = true;
+      through = from_before;
+    } else if (from_before) {
+      head = acc;
+      head_id = cur;
+      has_head = true;
     } else {
-      float *o = a.part + ((int64_t)(2 * part + (s >= lo)) * a.cols.blocks + b) * 8;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = acc[j];
+      write(cur, acc);
     }
   }
+  // out of the groups before that goes on through them: to each group, what enters it
+  f32x8 carry = out;
+  bool begun = !(has_out && through);   // the id that goes on has begun in this workgroup
+  for (uint32_t d = 1; d < groups; d *= 2) {
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) val[threadIdx.x][j] = carry[j];
+    stop[threadIdx.x] = begun;
+    __syncthreads();
+    if (g >= d && g < groups && !begun) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) carry[j] += val[threadIdx.x - d * wide][j];
+      begun = stop[threadIdx.x - d * wide];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 8; ++j) val[threadIdx.x][j] = carry[j];
+  stop[threadIdx.x] = begun;
+  __syncthreads();
+  if (!in) return;
+  float *slot = a.part + ((int64_t)(2 * part) * a.cols.blocks + b) * 8;
+  auto keep = [&](const f32x8 &s, int which) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) slot[(int64_t)which * a.cols.blocks * 8 + j] = s[j];
+  };
+  if (has_head) {
+    bool here = false;
+    if (g > 0) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) head[j] = val[threadIdx.x - wide][j] + head[j];
+      here = stop[threadIdx.x - wide];
+    }
+    if (here) write(head_id, head);
+    else keep(head, 0);
+  }
+  if (has_out && g == groups - 1) keep(carry, begun ? 1 : 0);   // what goes on beyond the workgroup
 }
 
 // An id that begins in this part and goes on: its sum here, then those of the parts
-// that it goes on in, in order
+// that it goes on in; `lanes` threads a column, each every lanes-th part, joined in 64 bits
 __global__ __launch_bounds__(kBackThreads) void k_embed_join(EmbedBackParams a, uint32_t tiles) {
+  __shared__ double room[kBackThreads];
   const int64_t at = a.wg0 + blockIdx.x;
   const uint32_t part = (uint32_t)(at / tiles), tile = (uint32_t)(at % tiles);
+  const uint32_t n = min(a.off[a.n_ids], (uint32_t)a.n_rows);
   const uint32_t next = (part + 1) * a.run;   // (not the last part: in the order)
+  if (next >= n) return;
   const uint32_t v = a.id[next - 1];
-  if (v >= a.n_ids) return;
-  uint32_t s, e;
-  places(a, v, s, e);
-  if (s < part * a.run || s >= next || e <= next || e - s <= kBackShort) return;
-  const uint32_t last = min((e - 1) / a.run, a.runs - 1);
-  const uint32_t cols = a.cols.blocks * 8, c = tile * kBackThreads + threadIdx.x;
-  if (c >= (a.cols.rem ? cols - 8 + a.cols.rem : cols)) return;
-  double sum = a.part[(int64_t)(2 * part + 1) * cols + c];
-  for (uint32_t k = part + 1; k <= last; ++k) sum += a.part[(int64_t)(2 * k) * cols + c];
+  if (v >= a.n_ids || a.id[next] != v || a.off[v] < part * a.run || a.off[v] >= next) return;
+  const uint32_t last = min((max(a.off[v + 1], next + 1) - 1) / a.run, a.runs - 1);
+  const uint32_t cols = a.cols.blocks * 8, width = a.cols.rem ? cols - 8 + a.cols.rem : cols;
+  const uint32_t wide = min(width, (uint32_t)kBackThreads), lanes = kBackThreads / wide;
+  const uint32_t l = threadIdx.x / wide, c = tile * wide + threadIdx.x % wide;
+  double sum = 0.0;
+  if (l < lanes && c < width) {
+    if (l == 0) sum = a.part[(int64_t)(2 * part + 1) * cols + c];
+#pragma unroll 8
+    for (uint32_t k = part + 1 + l; k <= last; k += lanes) sum += a.part[(int64_t)(2 * k) * cols + c];
+  }
+  room[threadIdx.x] = sum;
+  __syncthreads();
+  if (l > 0 || c >= width) return;
+  for (uint32_t k = 1; k < lanes; ++k) sum += room[k * wide + threadIdx.x];
   a.grad[(int64_t)v * a.grad_ld + c] = (float)(sum * a.factor);
 }
 
@@ -328,13 +399,14 @@ hipError_t embed(EmbedParams p, hipStream_t s) {
 
 template <bool B16>
 hipError_t embed_back(EmbedBackParams p, hipStream_t s) {
-  hipError_t e = in_launches(p.short_wgs + (int64_t)p.runs * p.tiles, [&](int64_t at, uint32_t wgs) {
+  hipError_t e = in_launches((int64_t)p.runs * p.tiles + p.fill_wgs, [&](int64_t at, uint32_t wgs) {
     p.wg0 = at;
     if (p.drop.least) hipLaunchKernelGGL((k_embed_back<B16, true>), dim3(wgs), dim3(kBackThreads), 0, s, p);
     else hipLaunchKernelGGL((k_embed_back<B16, false>), dim3(wgs), dim3(kBackThreads), 0, s, p);
   });
   if (e == hipSuccess && p.runs > 1) {
-    const uint32_t tiles = (p.cols.blocks * 8 + kBackThreads - 1) / kBackThreads;
+    const uint32_t width = (p.cols.blocks - (p.cols.rem ? 1 : 0)) * 8 + p.cols.rem;
+    const uint32_t tiles = (width + kBackThreads - 1) / kBackThreads;
     e = in_launches((int64_t)(p.runs - 1) * tiles, [&](int64_t at, uint32_t wgs) {
       p.wg0 = at;
       hipLaunchKernelGGL(k_embed_join, dim3(wgs), dim3(kBackThreads), 0, s, p, tiles);

@@ -359,13 +359,10 @@ struct EmbedParams {
 };
 hipError_t launch_embed(const EmbedParams &p, bool src16, bool dst16, hipStream_t s);
 
-// Ids with at most kBackShort rows are summed by the lanes that write their rows of the
-// table, those with more by workgroups over `run` places of the order each, which leave a
-// sum for the run that began before their places (0) and for the one that goes on behind
-// them (1).
+// A workgroup of k_embed_back takes `run` places of the order, `each` of them for each of
+// its 256 / wide groups of lanes, and leaves a sum of the id that began before its places
+// (0) and of the one that began in them and goes on behind (1).
 constexpr int kBackThreads = 256;
-constexpr uint32_t kBackShort = 128, kBackRun = 8192;   // places a workgroup, at most
-constexpr uint32_t kBackMost = kBackRun / kBackShort + 2;   // ids with many rows among them, at most
 struct EmbedBackParams {
   const void *dy;
   int64_t ld, n_rows;
@@ -376,8 +373,8 @@ struct EmbedBackParams {
   float factor;
   Cols cols;
   Drop drop;
-  int64_t short_wgs;
-  uint32_t run, runs, tiles;         // places a workgroup, parts of the order, tiles of columns
+  uint32_t wide, each, run, runs, tiles;   // runs parts of the order, tiles of `wide` blocks
+  int64_t fill_wgs;                  // ... and for the ids without rows
   float *part;                       // [runs][2][8 blocks]
   int64_t wg0;                       // of a launch (set by it)
 };
