@@ -164,41 +164,59 @@ __device__ __forceinline__ uint32_t row_in(const Cols &c, uint32_t l, uint32_t &
   b = l - q * c.blocks;
   return q;
 }
-// row and block of the workgroup's lane l: the workgroup starts at block `first` of all
-__device__ __forceinline__ int64_t row_of(const Cols &c, int64_t first, uint32_t l, uint32_t &b) {
-  uint32_t b0;
-  int64_t row;
+// the row of block `first` of all (the same in all lanes) and, in b, its block there
+__device__ __forceinline__ int64_t row_of(const Cols &c, int64_t first, uint32_t &b) {
   if ((uint64_t)first >> 32) {
-    row = first / c.blocks;
-    b0 = (uint32_t)(first - row * c.blocks);
-  } else {
-    row = row_in(c, (uint32_t)first, b0);
+    const int64_t row = first / c.blocks;
+    b = (uint32_t)(first - row * c.blocks);
+    return row;
   }
-  return row + row_in(c, b0 + l, b);
+  return row_in(c, (uint32_t)first, b);
 }
 
 // ------------------------------------------------------------ lookup and dropout
-template <bool S16, bool D16, bool DROP>
+// U blocks a lane, their ids and then their elements on the way together: two of a bfloat16
+// table from 2^20 blocks on, one else.  512 MB written and looked up in rows of 256 to
+// 4096 columns: bf16 43-48 us with two, 49-52 with one, 41-50 with four; fp32 (two loads
+// a block anyway) 87-94, 83-87, 85-99; a dropout of 134M bf16 elements 104, 93 and 110.
+template <bool S16, bool D16, bool DROP, int U>
 __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams a) {
-  uint32_t b;
-  const int64_t first = (a.wg0 + blockIdx.x) * kThreads;
-  const int64_t i = row_of(a.cols, first, threadIdx.x, b);
-  if (i >= a.n_rows) return;
-  const Place at = place_of(a.cols, b);
-  const int64_t id = a.ids ? (int64_t)a.ids[i] : i;
-  f32x8 v = {};
-  if (!a.ids || id < a.n_ids) {
-    Eight<S16> x = load8<S16>(a.src, id * a.src_ld + at.at, a.cols);
-    align8<S16>(x, a.cols, at.part);
+  const int64_t first = (a.wg0 + blockIdx.x) * (kThreads * U);
+  uint32_t b0;
+  const int64_t row0 = row_of(a.cols, first, b0);
+  const uint32_t step = DROP ? step_of(a.drop) : 0;
+  int64_t row[U], id[U];
+  uint32_t b[U];
+  bool in[U], known[U];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = x[j] * a.factor;
+  for (int u = 0; u < U; ++u) {
+    row[u] = row0 + row_in(a.cols, b0 + u * kThreads + threadIdx.x, b[u]);
+    in[u] = row[u] < a.n_rows;
+    id[u] = row[u];
+    if (a.ids && in[u]) id[u] = a.ids[row[u]];
   }
-  if constexpr (DROP) {
-    const Draws d = philox(a.drop, (uint64_t)(first + threadIdx.x), step_of(a.drop));
+  Eight<S16> x[U];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = d[j] >= a.drop.least ? v[j] : 0.0f;
+  for (int u = 0; u < U; ++u) {
+    known[u] = in[u] && (!a.ids || id[u] < a.n_ids);
+    x[u] = {};
+    if (known[u]) x[u] = load8<S16>(a.src, id[u] * a.src_ld + place_of(a.cols, b[u]).at, a.cols);
   }
-  store8<D16>(a.dst, i * a.dst_ld + 8 * (int64_t)b, v, !at.part, a.cols.rem);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (!in[u]) continue;
+    const bool part = place_of(a.cols, b[u]).part;
+    align8<S16>(x[u], a.cols, part);
+    f32x8 v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = known[u] ? x[u][j] * a.factor : 0.0f;
+    if constexpr (DROP) {
+      const Draws d = philox(a.drop, (uint64_t)(first + u * kThreads + threadIdx.x), step);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = d[j] >= a.drop.least ? v[j] : 0.0f;
+    }
+    store8<D16>(a.dst, row[u] * a.dst_ld + 8 * (int64_t)b[u], v, !part, a.cols.rem);
+  }
 }
 
 // ------------------------------------------------------------ the table's gradient
@@ -218,7 +236,8 @@ __global__ __launch_bounds__(kBackThreads) void k_embed_back(EmbedBackParams a) 
   if (wg >= (int64_t)a.runs * a.tiles) {
     // ids without rows
     uint32_t b;
-    const int64_t v = row_of(a.cols, (wg - (int64_t)a.runs * a.tiles) * kBackThreads, threadIdx.x, b);
+    int64_t v = row_of(a.cols, (wg - (int64_t)a.runs * a.tiles) * kBackThreads, b);
+    v += row_in(a.cols, b + threadIdx.x, b);
     if (v >= a.n_ids || a.off[v] < a.off[v + 1]) return;
     store8<false>(a.grad, v * a.grad_ld + 8 * (int64_t)b, f32x8{}, !place_of(a.cols, b).part, a.cols.rem);
     return;
@@ -349,31 +368,48 @@ __global__ __launch_bounds__(kBackThreads) void k_embed_back(EmbedBackParams a) 
 }
 
 // An id that begins in this part and goes on: its sum here, then those of the parts
-// that it goes on in; `lanes` threads a column, each every lanes-th part, joined in 64 bits
+// that it goes on in.  A thread has four columns; `lanes` threads share them, each with
+// every lanes-th part, joined in 64 bits.
+constexpr int kJoinCols = 4;
 __global__ __launch_bounds__(kBackThreads) void k_embed_join(EmbedBackParams a, uint32_t tiles) {
-  __shared__ double room[kBackThreads];
+  __shared__ double room[kBackThreads][kJoinCols];
   const int64_t at = a.wg0 + blockIdx.x;
   const uint32_t part = (uint32_t)(at / tiles), tile = (uint32_t)(at % tiles);
-  const uint32_t n = min(a.off[a.n_ids], (uint32_t)a.n_rows);
   const uint32_t next = (part + 1) * a.run;   // (not the last part: in the order)
-  if (next >= n) return;
-  const uint32_t v = a.id[next - 1];
-  if (v >= a.n_ids || a.id[next] != v || a.off[v] < part * a.run || a.off[v] >= next) return;
-  const uint32_t last = min((max(a.off[v + 1], next + 1) - 1) / a.run, a.runs - 1);
-  const uint32_t cols = a.cols.blocks * 8, width = a.cols.rem ? cols - 8 + a.cols.rem : cols;
-  const uint32_t wide = min(width, (uint32_t)kBackThreads), lanes = kBackThreads / wide;
-  const uint32_t l = threadIdx.x / wide, c = tile * wide + threadIdx.x % wide;
-  double sum = 0.0;
-  if (l < lanes && c < width) {
-    if (l == 0) sum = a.part[(int64_t)(2 * part + 1) * cols + c];
-#pragma unroll 8
-    for (uint32_t k = part + 1 + l; k <= last; k += lanes) sum += a.part[(int64_t)(2 * k) * cols + c];
+  const uint32_t n = min(a.off[a.n_ids], (uint32_t)a.n_rows), v = a.id[next - 1], after = a.id[next];
+  if (next >= n || v != after || v >= a.n_ids) return;
+  const uint32_t begin = a.off[v], end = a.off[v + 1];
+  if (begin < part * a.run || begin >= next) return;
+  const uint32_t last = min((max(end, next + 1) - 1) / a.run, a.runs - 1);
+  const uint32_t quads = a.cols.blocks * 8 / kJoinCols, wide = min(quads, (uint32_t)kBackThreads), lanes = kBackThreads / wide;
+  const uint32_t l = threadIdx.x / wide, q = tile * wide + threadIdx.x % wide;
+  double sum[kJoinCols] = {};
+  auto add = [&](int64_t slot) {
+    const f32x4 p = *(const f32x4 *)(a.part + (slot * quads + q) * kJoinCols);
+#pragma unroll
+    for (int j = 0; j < kJoinCols; ++j) sum[j] += (double)p[j];
+  };
+  if (l < lanes && q < quads) {
+    if (l == 0) add(2 * (int64_t)part + 1);
+#pragma unroll 4
+    for (uint32_t k = part + 1 + l; k <= last; k += lanes) add(2 * (int64_t)k);
   }
-  room[threadIdx.x] = sum;
-  __syncthreads();
-  if (l > 0 || c >= width) return;
-  for (uint32_t k = 1; k < lanes; ++k) sum += room[k * wide + threadIdx.x];
-  a.grad[(int64_t)v * a.grad_ld + c] = (float)(sum * a.factor);
+  for (uint32_t half = kBackThreads / 2; half > 0; half /= 2) {
+    if (half >= lanes) continue;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kJoinCols; ++j) room[threadIdx.x][j] = sum[j];
+    __syncthreads();
+    if (l < half && l + half < lanes) {
+#pragma unroll
+      for (int j = 0; j < kJoinCols; ++j) sum[j] += room[threadIdx.x + half * wide][j];
+    }
+  }
+  if (l > 0) return;
+  const uint32_t width = a.cols.rem ? a.cols.blocks * 8 - 8 + a.cols.rem : a.cols.blocks * 8;
+#pragma unroll
+  for (int j = 0; j < kJoinCols; ++j)
+    if (kJoinCols * q + j < width) a.grad[(int64_t)v * a.grad_ld + kJoinCols * q + j] = (float)(sum[j] * a.factor);
 }
 
 // launch(first workgroup, workgroups): as many as a launch takes at a time
@@ -388,13 +424,21 @@ hipError_t in_launches(int64_t wgs, F &&launch) {
   return hipSuccess;
 }
 
-template <bool S16, bool D16>
-hipError_t embed(EmbedParams p, hipStream_t s) {
-  return in_launches((p.n_rows * (int64_t)p.cols.blocks + kThreads - 1) / kThreads, [&](int64_t at, uint32_t wgs) {
+template <bool S16, bool D16, int U>
+hipError_t embed(EmbedParams p, int64_t blocks, hipStream_t s) {
+  return in_launches((blocks + kThreads * U - 1) / (kThreads * U), [&](int64_t at, uint32_t wgs) {
     p.wg0 = at;
-    if (p.drop.least) hipLaunchKernelGGL((k_embed<S16, D16, true>), dim3(wgs), dim3(kThreads), 0, s, p);
-    else hipLaunchKernelGGL((k_embed<S16, D16, false>), dim3(wgs), dim3(kThreads), 0, s, p);
+    if (p.drop.least) hipLaunchKernelGGL((k_embed<S16, D16, true, U>), dim3(wgs), dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL((k_embed<S16, D16, false, U>), dim3(wgs), dim3(kThreads), 0, s, p);
   });
+}
+
+template <bool S16, bool D16>
+hipError_t embed(const EmbedParams &p, hipStream_t s) {
+  const int64_t blocks = p.n_rows * (int64_t)p.cols.blocks;
+  if constexpr (S16)
+    if (p.ids && blocks >= (int64_t(1) << 20)) return embed<S16, D16, 2>(p, blocks, s);
+  return embed<S16, D16, 1>(p, blocks, s);
 }
 
 template <bool B16>
@@ -405,8 +449,7 @@ hipError_t embed_back(EmbedBackParams p, hipStream_t s) {
     else hipLaunchKernelGGL((k_embed_back<B16, false>), dim3(wgs), dim3(kBackThreads), 0, s, p);
   });
   if (e == hipSuccess && p.runs > 1) {
-    const uint32_t width = (p.cols.blocks - (p.cols.rem ? 1 : 0)) * 8 + p.cols.rem;
-    const uint32_t tiles = (width + kBackThreads - 1) / kBackThreads;
+    const uint32_t quads = p.cols.blocks * 8 / kJoinCols, tiles = (quads + kBackThreads - 1) / kBackThreads;
     e = in_launches((int64_t)(p.runs - 1) * tiles, [&](int64_t at, uint32_t wgs) {
       p.wg0 = at;
       hipLaunchKernelGGL(k_embed_join, dim3(wgs), dim3(kBackThreads), 0, s, p, tiles);

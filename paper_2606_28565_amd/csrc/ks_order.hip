@@ -6,6 +6,7 @@
 //   k_order_place   each key to its place: its digit's first one, the chunk's before it,
 //                   and its rank among the chunk's equal ones
 //   k_order_off     off[] from the sorted ids, where more than one pass made them
+//   k_order_small   all passes for up to 16,384 keys, which one workgroup holds
 //
 // The rank comes from one ballot per bit: the lanes with the same digit are a mask, and
 // what the wave had before stands in its own counters in LDS.  No atomic's order enters.
@@ -51,19 +52,93 @@ __device__ __forceinline__ uint32_t before(uint32_t v, uint32_t (&room)[kWaves])
 }
 
 // A wave's rank of `digit` among its keys so far, and the count that it leaves for the next
-__device__ __forceinline__ uint32_t rank_of(uint32_t *count, uint32_t digit, bool in, int bits) {
+template <class T>
+__device__ __forceinline__ uint32_t rank_of(T *count, uint32_t digit, bool in, int bits) {
   const uint64_t m = same_lanes(digit, in, bits);
   const int lane = threadIdx.x & 63;
   uint32_t rank = 0;
   if (in) {
     const uint32_t had = count[digit];
     rank = had + (uint32_t)__popcll(m & ((uint64_t(1) << lane) - 1));
-    if (m >> lane == 1) count[digit] = had + (uint32_t)__popcll(m);   // the last of them
+    if (m >> lane == 1) count[digit] = (T)(had + (uint32_t)__popcll(m));   // the last of them
   }
   // (a lane reads next what another one has written)
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
   return rank;
+}
+
+// K keys a thread; keys and rows pass through LDS between two digits.  (Places and counts
+// of 16,384 keys fit 16 bits.)
+constexpr uint32_t kOffHere = 4096;   // ids up to which the offsets are found here
+template <int K>
+__global__ __launch_bounds__(kThreads) void k_order_small(OrderParams a) {
+  __shared__ uint32_t keys[kThreads * K], room[kWaves];
+  __shared__ uint16_t rows[kThreads * K], count[kWaves][kBins];
+  const uint32_t bins = 1u << a.bits, n = a.n_rows;
+  const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63, from = wave * (64 * K) + lane;
+  uint32_t k[K], row[K], rank[K];
+#pragma unroll
+  for (int r = 0; r < K; ++r) {
+    const uint32_t p = from + 64 * r;
+    row[r] = p;
+    k[r] = p < n ? key_of(a.ids[p], a.n_ids) : 0;
+  }
+  for (int pass = 0; pass < a.passes; ++pass) {
+    const int shift = pass * a.bits;
+    for (uint32_t i = threadIdx.x; i < kWaves * bins; i += kThreads) count[i >> a.bits][i & (bins - 1)] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < K; ++r)
+      if (wave * (64 * K) + 64 * r < n) rank[r] = rank_of(count[wave], k[r] >> shift & (bins - 1), from + 64 * r < n, a.bits);
+    __syncthreads();
+    {
+      const uint32_t d = threadIdx.x;
+      uint32_t total = 0;
+      if (d < bins)
+        for (int w = 0; w < kWaves; ++w) {
+          const uint32_t c = count[w][d];
+          count[w][d] = (uint16_t)total;
+          total += c;
+        }
+      const uint32_t first = before(total, room);
+      if (d < bins)
+        for (int w = 0; w < kWaves; ++w) count[w][d] = (uint16_t)(count[w][d] + first);
+      if (a.passes == 1 && d < bins && d <= a.n_ids) a.off[d] = first;
+    }
+    __syncthreads();
+    const bool last = pass + 1 == a.passes;
+#pragma unroll
+    for (int r = 0; r < K; ++r) {
+      if (from + 64 * r >= n) continue;
+      const uint32_t at = count[wave][k[r] >> shift & (bins - 1)] + rank[r];
+      keys[at] = k[r];
+      if (last) {
+        a.id[at] = k[r];
+        a.row[at] = row[r];
+      } else {
+        rows[at] = (uint16_t)row[r];
+      }
+    }
+    __syncthreads();
+    if (last) break;
+#pragma unroll
+    for (int r = 0; r < K; ++r) {
+      if (from + 64 * r >= n) continue;
+      k[r] = keys[from + 64 * r];
+      row[r] = rows[from + 64 * r];
+    }
+  }
+  if (a.passes == 1 || a.n_ids > kOffHere) return;
+  for (uint32_t v = threadIdx.x; v <= a.n_ids; v += kThreads) {
+    uint32_t lo = 0, hi = n;
+    while (lo < hi) {
+      const uint32_t mid = (lo + hi) / 2;
+      if (keys[mid] < v) lo = mid + 1;
+      else hi = mid;
+    }
+    a.off[v] = lo;
+  }
 }
 
 __global__ __launch_bounds__(kThreads) void k_order_count(OrderParams a, const uint32_t *key, int shift) {
@@ -150,7 +225,13 @@ __global__ __launch_bounds__(256) void k_order_off(OrderParams a) {
 hipError_t launch_order(const OrderParams &p, hipStream_t s) {
   const uint32_t *key = p.ids, *row = nullptr;
   const dim3 wg(kThreads);
-  for (int i = 0; i < p.passes && p.n_rows > 0; ++i) {
+  const bool small = p.n_rows > 0 && p.n_rows <= kThreads * 16;
+  if (small) {
+    if (p.n_rows <= kThreads * 4) hipLaunchKernelGGL(k_order_small<4>, dim3(1), wg, 0, s, p);
+    else if (p.n_rows <= kThreads * 8) hipLaunchKernelGGL(k_order_small<8>, dim3(1), wg, 0, s, p);
+    else hipLaunchKernelGGL(k_order_small<16>, dim3(1), wg, 0, s, p);
+  }
+  for (int i = 0; i < p.passes && p.n_rows > 0 && !small; ++i) {
     const bool last = (p.passes - 1 - i) % 2 == 0;
     uint32_t *to_key = last ? p.id : p.tmp_id, *to_row = last ? p.row : p.tmp_row;
     hipLaunchKernelGGL(k_order_count, dim3(p.chunks), wg, 0, s, p, key, i * p.bits);
@@ -159,7 +240,8 @@ hipError_t launch_order(const OrderParams &p, hipStream_t s) {
     key = to_key;
     row = to_row;
   }
-  if (p.passes > 1 || p.n_rows == 0) hipLaunchKernelGGL(k_order_off, dim3(p.n_ids / 256 + 1), dim3(256), 0, s, p);
+  if (p.n_rows == 0 || (p.passes > 1 && !(small && p.n_ids <= kOffHere)))
+    hipLaunchKernelGGL(k_order_off, dim3(p.n_ids / 256 + 1), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
