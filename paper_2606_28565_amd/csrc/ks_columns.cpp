@@ -90,10 +90,10 @@ ks::Drop drop_of(const ks_drop *d, double *up) {
   return o;
 }
 
-ks::Cols cols_of(int64_t n) {
+ks::Cols cols_of(int64_t n, int64_t width = 8) {
   ks::Cols c;
-  c.blocks = (uint32_t)((n + 7) / 8);
-  c.rem = (uint32_t)(n % 8);
+  c.blocks = (uint32_t)((n + width - 1) / width);
+  c.rem = (uint32_t)(n % width);
   c.magic = c.blocks > 1 ? (uint32_t)(((uint64_t(1) << 32) + c.blocks - 1) / c.blocks) : 0;
   return c;
 }
@@ -127,7 +127,8 @@ ks_status check_order(const ks_id_order *o) {
   return KS_OK;
 }
 
-// Chunks of the keys: at most 4096, so that the counts of a digit stay short
+// Chunks of the keys: at most 512, so that the counts of a digit stay short, while that is
+// no more than 2^20 keys in each
 void plan(ks::OrderParams &p, const ks_id_order *o) {
   std::memset(&p, 0, sizeof p);
   p.n_rows = (uint32_t)o->n_rows;
@@ -135,9 +136,9 @@ void plan(ks::OrderParams &p, const ks_id_order *o) {
   int bits = 0;
   while (bits < 32 && (uint64_t)o->n_ids >> bits) ++bits;   // (n_ids is a key too)
   p.passes = (bits + ks::kOrderBits - 1) / ks::kOrderBits;
-  p.bits = (bits + p.passes - 1) / p.passes;
-  const int64_t most = int64_t(4096) * ks::kOrderKeys;
-  p.chunk = (uint32_t)(ks::kOrderKeys * std::max<int64_t>(1, (o->n_rows + most - 1) / most));
+  p.bits = p.passes * ks::kOrderFew >= bits ? ks::kOrderFew : ks::kOrderBits;
+  const int64_t most = int64_t(512) * ks::kOrderKeys;
+  p.chunk = (uint32_t)(ks::kOrderKeys * std::min<int64_t>(512, std::max<int64_t>(1, (o->n_rows + most - 1) / most)));
   p.chunks = (uint32_t)((o->n_rows + p.chunk - 1) / p.chunk);
 }
 
@@ -161,7 +162,9 @@ void plan(ks::EmbedBackParams &p, const ks_id_order *o, int64_t n_cols) {
   p.n_rows = o->n_rows;
   p.n_ids = (uint32_t)o->n_ids;
   p.cols = cols_of(n_cols);
-  p.fill_wgs = (o->n_ids * (int64_t)p.cols.blocks + ks::kBackThreads - 1) / ks::kBackThreads;
+  p.quads = cols_of(n_cols, 4);
+  const int64_t fill = ks::kBackThreads * ks::kBackFill;
+  p.fill_wgs = (o->n_ids * (int64_t)p.quads.blocks + fill - 1) / fill;
   p.wide = std::min<uint32_t>(p.cols.blocks, ks::kBackThreads);
   p.tiles = (p.cols.blocks + p.wide - 1) / p.wide;
   const int64_t groups = ks::kBackThreads / p.wide, most = 2048 * 16 * groups;

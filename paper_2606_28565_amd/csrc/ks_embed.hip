@@ -235,11 +235,18 @@ __global__ __launch_bounds__(kBackThreads) void k_embed_back(EmbedBackParams a) 
   const uint32_t n = min(a.off[a.n_ids], (uint32_t)a.n_rows);   // (behind: rows without an id)
   if (wg >= (int64_t)a.runs * a.tiles) {
     // ids without rows
-    uint32_t b;
-    int64_t v = row_of(a.cols, (wg - (int64_t)a.runs * a.tiles) * kBackThreads, b);
-    v += row_in(a.cols, b + threadIdx.x, b);
-    if (v >= a.n_ids || a.off[v] < a.off[v + 1]) return;
-    store8<false>(a.grad, v * a.grad_ld + 8 * (int64_t)b, f32x8{}, !place_of(a.cols, b).part, a.cols.rem);
+    uint32_t q0;
+    const int64_t v0 = row_of(a.quads, (wg - (int64_t)a.runs * a.tiles) * (kBackThreads * kBackFill), q0);
+#pragma unroll
+    for (int u = 0; u < kBackFill; ++u) {
+      uint32_t q;
+      const int64_t v = v0 + row_in(a.quads, q0 + u * kBackThreads + threadIdx.x, q);
+      if (v >= a.n_ids || a.off[v] < a.off[v + 1]) continue;
+      float *o = a.grad + v * a.grad_ld + 4 * (int64_t)q;
+      if (a.quads.rem == 0 || q + 1 < a.quads.blocks) *(any_f32x4 *)o = f32x4{};
+      else
+        for (uint32_t j = 0; j < a.quads.rem; ++j) o[j] = 0.0f;
+    }
     return;
   }
   constexpr uint32_t kBatch = B16 ? 8 : 4;
@@ -391,7 +398,7 @@ __global__ __launch_bounds__(kBackThreads) void k_embed_join(EmbedBackParams a, 
   };
   if (l < lanes && q < quads) {
     if (l == 0) add(2 * (int64_t)part + 1);
-#pragma unroll 4
+#pragma unroll 16
     for (uint32_t k = part + 1 + l; k <= last; k += lanes) add(2 * (int64_t)k);
   }
   for (uint32_t half = kBackThreads / 2; half > 0; half /= 2) {

@@ -362,7 +362,7 @@ hipError_t launch_embed(const EmbedParams &p, bool src16, bool dst16, hipStream_
 // A workgroup of k_embed_back takes `run` places of the order, `each` of them for each of
 // its 256 / wide groups of lanes, and leaves a sum of the id that began before its places
 // (0) and of the one that began in them and goes on behind (1).
-constexpr int kBackThreads = 256;
+constexpr int kBackThreads = 256, kBackFill = 4;   // quads of columns a thread, for ids without rows
 struct EmbedBackParams {
   const void *dy;
   int64_t ld, n_rows;
@@ -371,7 +371,7 @@ struct EmbedBackParams {
   float *grad;
   int64_t grad_ld;
   float factor;
-  Cols cols;
+  Cols cols, quads;                  // quads: of four columns
   Drop drop;
   uint32_t wide, each, run, runs, tiles;   // runs parts of the order, tiles of `wide` blocks
   int64_t fill_wgs;                  // ... and for the ids without rows
@@ -380,9 +380,9 @@ struct EmbedBackParams {
 };
 hipError_t launch_embed_back(const EmbedBackParams &p, bool dy16, hipStream_t s);
 
-constexpr int kOrderThreads = 1024;  // of a workgroup that ranks keys
-constexpr int kOrderKeys = 4096;     // keys ranked at a time
-constexpr int kOrderBits = 10;       // of a digit, at most
+constexpr int kOrderThreads = 512;   // of a workgroup that ranks keys
+constexpr int kOrderKeys = 2048;     // keys ranked at a time
+constexpr int kOrderFew = 8, kOrderBits = 10;   // of a digit: fewer where that takes no more passes
 struct OrderParams {
   const uint32_t *ids;
   uint32_t n_rows, n_ids;

@@ -18,32 +18,46 @@ namespace ks {
 
 namespace {
 
-constexpr int kThreads = kOrderThreads, kWaves = kThreads / 64, kRounds = kOrderKeys / kThreads;
-constexpr int kBins = 1 << kOrderBits;
+constexpr int kRounds = kOrderKeys / kOrderThreads;
+constexpr int kSmallThreads = 1024;
 
 __device__ __forceinline__ uint32_t key_of(uint32_t id, uint32_t n_ids) { return id < n_ids ? id : n_ids; }
 
-// the lanes that hold the same digit, among those with `in`
-__device__ __forceinline__ uint64_t same_lanes(uint32_t digit, bool in, int bits) {
-  uint64_t m = __ballot(in);
-  for (int b = 0; b < bits; ++b) {
-    const bool set = digit >> b & 1;
-    const uint64_t s = __ballot(set);
-    m &= set ? s : ~s;
+// Keys behind the last one have all bits set: they come last in each pass, behind the keys
+// of their digit, so that all lanes always hold a key.
+constexpr uint32_t kBehind = 0xFFFFFFFFu;
+
+// the lanes that hold the same digit: for each of its bits those that have it set or not as
+// this one has
+template <int BITS>
+__device__ __forceinline__ uint64_t same_lanes(uint32_t digit) {
+  uint32_t lo = 0xFFFFFFFFu, hi = 0xFFFFFFFFu;
+#pragma unroll
+  for (int b = 0; b < BITS; ++b) {
+    const uint32_t set = (uint32_t)((int32_t)(digit << (31 - b)) >> 31);
+    const uint64_t s = __ballot(set != 0);
+    lo &= ~((uint32_t)s ^ set);
+    hi &= ~((uint32_t)(s >> 32) ^ set);
   }
-  return m;
+  return (uint64_t)hi << 32 | lo;
 }
 
-// exclusive prefix sums over the workgroup's threads
-__device__ __forceinline__ uint32_t before(uint32_t v, uint32_t (&room)[kWaves]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t sum = v;
+// inclusive prefix sums over a wave
+__device__ __forceinline__ uint32_t prefix(uint32_t v) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
-    const uint32_t o = __shfl_up(sum, d);
-    if (lane >= d) sum += o;
+    const uint32_t o = __shfl_up(v, d);
+    if (lane >= d) v += o;
   }
-  __syncthreads();
+  return v;
+}
+
+// exclusive prefix sums over a workgroup's W waves
+template <int W>
+__device__ __forceinline__ uint32_t before(uint32_t v, uint32_t (&room)[W]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t sum = prefix(v);
   if (lane == 63) room[wave] = sum;
   __syncthreads();
   uint32_t base = 0;
@@ -51,86 +65,83 @@ __device__ __forceinline__ uint32_t before(uint32_t v, uint32_t (&room)[kWaves])
   return base + sum - v;
 }
 
-// A wave's rank of `digit` among its keys so far, and the count that it leaves for the next
-template <class T>
-__device__ __forceinline__ uint32_t rank_of(T *count, uint32_t digit, bool in, int bits) {
-  const uint64_t m = same_lanes(digit, in, bits);
-  const int lane = threadIdx.x & 63;
-  uint32_t rank = 0;
-  if (in) {
-    const uint32_t had = count[digit];
-    rank = had + (uint32_t)__popcll(m & ((uint64_t(1) << lane) - 1));
-    if (m >> lane == 1) count[digit] = (T)(had + (uint32_t)__popcll(m));   // the last of them
+// The ranks of K keys a lane, 64 consecutive ones at a time, among the wave's keys of the same
+// digit; count: the wave's counters, which keep how many of each digit it has
+template <int BITS, int K, class T>
+__device__ __forceinline__ void ranks(uint32_t (&rank)[K], const uint32_t (&key)[K], T *count, int shift) {
+#pragma unroll
+  for (int r = 0; r < K; ++r) {
+    const uint32_t digit = key[r] >> shift & ((1u << BITS) - 1);
+    const uint64_t m = same_lanes<BITS>(digit);
+    const uint32_t lo = (uint32_t)m, hi = (uint32_t)(m >> 32), all = __popc(lo) + __popc(hi);
+    const uint32_t had = count[digit], below = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
+    rank[r] = had + below;
+    if (below + 1 == all) count[digit] = (T)(had + all);   // the last of them
+    // (a lane reads next what another one has written)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
-  // (a lane reads next what another one has written)
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  return rank;
 }
 
 // K keys a thread; keys and rows pass through LDS between two digits.  (Places and counts
 // of 16,384 keys fit 16 bits.)
 constexpr uint32_t kOffHere = 4096;   // ids up to which the offsets are found here
-template <int K>
-__global__ __launch_bounds__(kThreads) void k_order_small(OrderParams a) {
-  __shared__ uint32_t keys[kThreads * K], room[kWaves];
-  __shared__ uint16_t rows[kThreads * K], count[kWaves][kBins];
-  const uint32_t bins = 1u << a.bits, n = a.n_rows;
+template <int BITS, int K>
+__global__ __launch_bounds__(kSmallThreads) void k_order_small(OrderParams a) {
+  constexpr uint32_t kBins = 1u << BITS, bins = kBins;
+  __shared__ uint32_t keys[kSmallThreads * K], room[kSmallThreads / 64];
+  __shared__ uint16_t rows[kSmallThreads * K], count[kSmallThreads / 64][kBins];
+  const uint32_t n = a.n_rows;
   const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63, from = wave * (64 * K) + lane;
   uint32_t k[K], row[K], rank[K];
 #pragma unroll
   for (int r = 0; r < K; ++r) {
     const uint32_t p = from + 64 * r;
     row[r] = p;
-    k[r] = p < n ? key_of(a.ids[p], a.n_ids) : 0;
+    k[r] = p < n ? key_of(a.ids[p], a.n_ids) : kBehind;
   }
   for (int pass = 0; pass < a.passes; ++pass) {
-    const int shift = pass * a.bits;
-    for (uint32_t i = threadIdx.x; i < kWaves * bins; i += kThreads) count[i >> a.bits][i & (bins - 1)] = 0;
+    const int shift = pass * BITS;
+    for (uint32_t i = threadIdx.x; i < kSmallThreads / 64 * bins; i += kSmallThreads) count[i >> BITS][i & (bins - 1)] = 0;
     __syncthreads();
-#pragma unroll
-    for (int r = 0; r < K; ++r)
-      if (wave * (64 * K) + 64 * r < n) rank[r] = rank_of(count[wave], k[r] >> shift & (bins - 1), from + 64 * r < n, a.bits);
+    ranks<BITS>(rank, k, count[wave], shift);
     __syncthreads();
     {
       const uint32_t d = threadIdx.x;
       uint32_t total = 0;
       if (d < bins)
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < kSmallThreads / 64; ++w) {
           const uint32_t c = count[w][d];
           count[w][d] = (uint16_t)total;
           total += c;
         }
       const uint32_t first = before(total, room);
       if (d < bins)
-        for (int w = 0; w < kWaves; ++w) count[w][d] = (uint16_t)(count[w][d] + first);
+        for (int w = 0; w < kSmallThreads / 64; ++w) count[w][d] = (uint16_t)(count[w][d] + first);
       if (a.passes == 1 && d < bins && d <= a.n_ids) a.off[d] = first;
     }
     __syncthreads();
-    const bool last = pass + 1 == a.passes;
 #pragma unroll
     for (int r = 0; r < K; ++r) {
-      if (from + 64 * r >= n) continue;
       const uint32_t at = count[wave][k[r] >> shift & (bins - 1)] + rank[r];
       keys[at] = k[r];
-      if (last) {
-        a.id[at] = k[r];
-        a.row[at] = row[r];
-      } else {
-        rows[at] = (uint16_t)row[r];
-      }
+      rows[at] = (uint16_t)row[r];
     }
     __syncthreads();
-    if (last) break;
 #pragma unroll
     for (int r = 0; r < K; ++r) {
-      if (from + 64 * r >= n) continue;
       k[r] = keys[from + 64 * r];
       row[r] = rows[from + 64 * r];
     }
   }
+#pragma unroll
+  for (int r = 0; r < K; ++r) {
+    if (from + 64 * r >= n) continue;
+    a.id[from + 64 * r] = k[r];
+    a.row[from + 64 * r] = row[r];
+  }
   if (a.passes == 1 || a.n_ids > kOffHere) return;
-  for (uint32_t v = threadIdx.x; v <= a.n_ids; v += kThreads) {
+  for (uint32_t v = threadIdx.x; v <= a.n_ids; v += kSmallThreads) {
     uint32_t lo = 0, hi = n;
     while (lo < hi) {
       const uint32_t mid = (lo + hi) / 2;
@@ -141,54 +152,88 @@ __global__ __launch_bounds__(kThreads) void k_order_small(OrderParams a) {
   }
 }
 
-__global__ __launch_bounds__(kThreads) void k_order_count(OrderParams a, const uint32_t *key, int shift) {
+template <int BITS>
+__global__ __launch_bounds__(kOrderThreads) void k_order_count(OrderParams a, const uint32_t *key, int shift) {
+  constexpr uint32_t kBins = 1u << BITS, bins = kBins;
   __shared__ uint32_t count[kBins];
-  const uint32_t bins = 1u << a.bits;
-  for (uint32_t d = threadIdx.x; d < bins; d += kThreads) count[d] = 0;
+  for (uint32_t d = threadIdx.x; d < bins; d += kOrderThreads) count[d] = 0;
   __syncthreads();
   const uint32_t lo = blockIdx.x * a.chunk, hi = a.n_rows - lo < a.chunk ? a.n_rows : lo + a.chunk;
-  for (uint32_t p = lo + threadIdx.x; p < hi; p += kThreads) atomicAdd(&count[key_of(key[p], a.n_ids) >> shift & (bins - 1)], 1u);
+  for (uint32_t p = lo + threadIdx.x; p < hi; p += kOrderThreads)
+    atomicAdd(&count[key_of(key[p], a.n_ids) >> shift & (bins - 1)], 1u);
   __syncthreads();
-  for (uint32_t d = threadIdx.x; d < bins; d += kThreads) a.hist[(size_t)d * a.chunks + blockIdx.x] = count[d];
+  for (uint32_t d = threadIdx.x; d < bins; d += kOrderThreads) a.hist[(size_t)d * a.chunks + blockIdx.x] = count[d];
 }
 
-__global__ __launch_bounds__(kThreads) void k_order_sum(OrderParams a) {
-  __shared__ uint32_t room[kWaves];
-  uint32_t *h = a.hist + (size_t)blockIdx.x * a.chunks, sum = 0;
-  for (uint32_t c0 = 0; c0 < a.chunks; c0 += kThreads) {
-    const uint32_t c = c0 + threadIdx.x, v = c < a.chunks ? h[c] : 0;
-    const uint32_t at = before(v, room);
-    if (c < a.chunks) h[c] = sum + at;
-    for (int w = 0; w < kWaves; ++w) sum += room[w];
+// a wave per digit; with few chunks k_order_place adds up their counts itself (65,536 keys
+// of 32,000 ids: 27 us in five launches, 29 in seven; 16,381: 23 and 28)
+constexpr uint32_t kFewChunks = 32;
+__global__ __launch_bounds__(256) void k_order_sum(OrderParams a) {
+  const uint32_t d = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (d >> a.bits) return;
+  uint32_t *h = a.hist + (size_t)d * a.chunks, sum = 0;
+  for (uint32_t c0 = 0; c0 < a.chunks; c0 += 64) {
+    const uint32_t c = c0 + lane, v = c < a.chunks ? h[c] : 0, upto = prefix(v);
+    if (c < a.chunks) h[c] = sum + upto - v;
+    sum += __shfl(upto, 63);
   }
-  if (threadIdx.x == 0) a.total[blockIdx.x] = sum;
+  if (lane == 0) a.total[d] = sum;
 }
 
-__global__ __launch_bounds__(kThreads) void k_order_place(OrderParams a, const uint32_t *key, const uint32_t *row, uint32_t *to_key,
-                                                          uint32_t *to_row, int shift, bool only) {
-  __shared__ uint32_t count[kWaves][kBins], base[kBins], room[kWaves];
-  const uint32_t bins = 1u << a.bits;
+template <int BITS>
+__global__ __launch_bounds__(kOrderThreads) void k_order_place(OrderParams a, const uint32_t *key, const uint32_t *row, uint32_t *to_key,
+                                                               uint32_t *to_row, int shift, bool only) {
+  constexpr uint32_t kBins = 1u << BITS, bins = kBins;
+  constexpr int W = kOrderThreads / 64;
+  __shared__ uint32_t count[W][kBins], base[kBins], room[W];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   {
-    const uint32_t d = threadIdx.x, first = before(d < bins ? a.total[d] : 0, room);
-    if (d < bins) base[d] = first + a.hist[(size_t)d * a.chunks + blockIdx.x];
-    if (only && blockIdx.x == 0 && d <= a.n_ids && d < bins) a.off[d] = first;
+    // consecutive digits a thread
+    constexpr int D = kBins < kOrderThreads ? 1 : kBins / kOrderThreads;
+    uint32_t total[D], chunks_before[D], sum = 0;
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+      const uint32_t d = threadIdx.x * D + i;
+      total[i] = chunks_before[i] = 0;
+      if (d < bins) {
+        const uint32_t *h = a.hist + (size_t)d * a.chunks;
+        if (a.chunks > kFewChunks) {
+          total[i] = a.total[d];
+          chunks_before[i] = h[blockIdx.x];
+        } else {
+#pragma unroll 8
+          for (uint32_t c = 0; c < a.chunks; ++c) {
+            const uint32_t v = h[c];
+            total[i] += v;
+            chunks_before[i] += c < blockIdx.x ? v : 0;
+          }
+        }
+      }
+      sum += total[i];
+    }
+    uint32_t first = before(sum, room);
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+      const uint32_t d = threadIdx.x * D + i;
+      if (d < bins) base[d] = first + chunks_before[i];
+      if (only && blockIdx.x == 0 && d <= a.n_ids && d < bins) a.off[d] = first;
+      first += total[i];
+    }
   }
   const uint32_t lo = blockIdx.x * a.chunk, hi = a.n_rows - lo < a.chunk ? a.n_rows : lo + a.chunk;
   for (uint32_t from = lo; from < hi; from += kOrderKeys) {
-    for (uint32_t d = threadIdx.x; d < kWaves * bins; d += kThreads) count[d >> a.bits][d & (bins - 1)] = 0;
-    __syncthreads();
+    for (uint32_t d = threadIdx.x; d < W * bins; d += kOrderThreads) count[d >> BITS][d & (bins - 1)] = 0;
     uint32_t k[kRounds], rank[kRounds];
+    const uint32_t p0 = from + wave * (64 * kRounds) + lane;
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-      const uint32_t p = from + wave * (64 * kRounds) + 64 * r + lane;
-      k[r] = p < hi ? key_of(key[p], a.n_ids) : 0;
-      rank[r] = rank_of(count[wave], k[r] >> shift & (bins - 1), p < hi, a.bits);
-    }
+    for (int r = 0; r < kRounds; ++r) k[r] = p0 + 64 * r < hi ? key_of(key[p0 + 64 * r], a.n_ids) : kBehind;
     __syncthreads();
-    for (uint32_t d = threadIdx.x; d < bins; d += kThreads) {
+    ranks<BITS>(rank, k, count[wave], shift);
+    __syncthreads();
+    for (uint32_t d = threadIdx.x; d < bins; d += kOrderThreads) {
       uint32_t at = base[d];
-      for (int w = 0; w < kWaves; ++w) {
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
         const uint32_t c = count[w][d];
         count[w][d] = at;
         at += c;
@@ -198,7 +243,7 @@ __global__ __launch_bounds__(kThreads) void k_order_place(OrderParams a, const u
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) {
-      const uint32_t p = from + wave * (64 * kRounds) + 64 * r + lane;
+      const uint32_t p = p0 + 64 * r;
       if (p >= hi) continue;
       const uint32_t at = count[wave][k[r] >> shift & (bins - 1)] + rank[r];
       to_key[at] = k[r];
@@ -220,29 +265,33 @@ __global__ __launch_bounds__(256) void k_order_off(OrderParams a) {
   a.off[v] = lo;
 }
 
-}  // namespace
-
-hipError_t launch_order(const OrderParams &p, hipStream_t s) {
+template <int BITS>
+hipError_t order(const OrderParams &p, hipStream_t s) {
   const uint32_t *key = p.ids, *row = nullptr;
-  const dim3 wg(kThreads);
-  const bool small = p.n_rows > 0 && p.n_rows <= kThreads * 16;
+  const dim3 wg(kOrderThreads), small_wg(kSmallThreads);
+  const bool small = p.n_rows > 0 && p.n_rows <= kSmallThreads * 8;
   if (small) {
-    if (p.n_rows <= kThreads * 4) hipLaunchKernelGGL(k_order_small<4>, dim3(1), wg, 0, s, p);
-    else if (p.n_rows <= kThreads * 8) hipLaunchKernelGGL(k_order_small<8>, dim3(1), wg, 0, s, p);
-    else hipLaunchKernelGGL(k_order_small<16>, dim3(1), wg, 0, s, p);
+    if (p.n_rows <= kSmallThreads * 4) hipLaunchKernelGGL((k_order_small<BITS, 4>), dim3(1), small_wg, 0, s, p);
+    else hipLaunchKernelGGL((k_order_small<BITS, 8>), dim3(1), small_wg, 0, s, p);
   }
   for (int i = 0; i < p.passes && p.n_rows > 0 && !small; ++i) {
     const bool last = (p.passes - 1 - i) % 2 == 0;
     uint32_t *to_key = last ? p.id : p.tmp_id, *to_row = last ? p.row : p.tmp_row;
-    hipLaunchKernelGGL(k_order_count, dim3(p.chunks), wg, 0, s, p, key, i * p.bits);
-    hipLaunchKernelGGL(k_order_sum, dim3(1u << p.bits), wg, 0, s, p);
-    hipLaunchKernelGGL(k_order_place, dim3(p.chunks), wg, 0, s, p, key, row, to_key, to_row, i * p.bits, p.passes == 1);
+    hipLaunchKernelGGL((k_order_count<BITS>), dim3(p.chunks), wg, 0, s, p, key, i * BITS);
+    if (p.chunks > kFewChunks) hipLaunchKernelGGL(k_order_sum, dim3((1u << BITS) / 4), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((k_order_place<BITS>), dim3(p.chunks), wg, 0, s, p, key, row, to_key, to_row, i * BITS, p.passes == 1);
     key = to_key;
     row = to_row;
   }
   if (p.n_rows == 0 || (p.passes > 1 && !(small && p.n_ids <= kOffHere)))
     hipLaunchKernelGGL(k_order_off, dim3(p.n_ids / 256 + 1), dim3(256), 0, s, p);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_order(const OrderParams &p, hipStream_t s) {
+  return p.bits == kOrderFew ? order<kOrderFew>(p, s) : order<kOrderBits>(p, s);
 }
 
 }  // namespace ks
