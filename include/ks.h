@@ -622,8 +622,8 @@ ks_status ks_dropout(const ks_drop *drop, const ks_matrix *x, const ks_matrix *y
 
 /* y_i = drop(scale table_{ids_i}) for every row of y: ids device [y.n_rows], table one row
  * per id, as many columns as y.  An id at or beyond table.n_rows (2^32 - 1 among them: no
- * category, padding) gives zeros.  Computed in fp32, rounded once to y's type; scale finite
- * in fp32.  drop: NULL for none. */
+ * category, padding) gives zeros.  Computed in fp32, rounded once to y's type; scale, and scale
+ * / (1 - p), finite in fp32.  drop: NULL for none. */
 ks_status ks_embed(const ks_matrix *table, double scale, const uint32_t *ids, const ks_drop *drop, const ks_matrix *y,
                    hipStream_t stream);
 

@@ -648,6 +648,8 @@ def step_outputs(n_steps: int, n_specs: int, device="cuda"):
 
 def current_stream() -> int:
     import torch
+    if torch.cuda.is_initialized():   # (without a torch.cuda.Stream around it: 3 us less)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return torch.cuda.current_stream().cuda_stream
 
 

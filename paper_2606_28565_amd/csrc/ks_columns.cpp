@@ -155,20 +155,22 @@ OrderRoom room_of(const ks::OrderParams &p) {
   return r;
 }
 
-// 16 places of the order for each group of lanes, more where that is over 2048 workgroups,
-// 4096 at most (64 runs of 64 additions).
+// Four places of the order for each group of lanes, more where that is over 1024 workgroups,
+// 4096 at most (64 runs of 64 additions).  Few places are a short way through a small call
+// (4099 rows of 16 columns: 11 us with 4, 13 with 8, 19 with 16).  More workgroups leave
+// more sums of ids that go on for the join: 16,381 rows of 2048 columns 90 us with 512, 96
+// with 1024, 125 with 2048; 300,007 of 67 columns 33, 31, 32; 2,000,003 of 16 65, 64, 62.
 void plan(ks::EmbedBackParams &p, const ks_id_order *o, int64_t n_cols) {
   std::memset(&p, 0, sizeof p);
   p.n_rows = o->n_rows;
   p.n_ids = (uint32_t)o->n_ids;
   p.cols = cols_of(n_cols);
   p.quads = cols_of(n_cols, 4);
-  const int64_t fill = ks::kBackThreads * ks::kBackFill;
-  p.fill_wgs = (o->n_ids * (int64_t)p.quads.blocks + fill - 1) / fill;
   p.wide = std::min<uint32_t>(p.cols.blocks, ks::kBackThreads);
   p.tiles = (p.cols.blocks + p.wide - 1) / p.wide;
-  const int64_t groups = ks::kBackThreads / p.wide, most = 2048 * 16 * groups;
-  p.each = (uint32_t)std::min<int64_t>(16 * std::max<int64_t>(1, (o->n_rows * p.tiles + most - 1) / most), 4096);
+  const int64_t fill = ks::kBackThreads * ks::kBackFill, groups = ks::kBackThreads / p.wide, most = 1024 * 4 * groups;
+  p.fill_wgs = (o->n_ids * (int64_t)p.quads.blocks + fill - 1) / fill;
+  p.each = (uint32_t)std::min<int64_t>(4 * std::max<int64_t>(1, (o->n_rows * p.tiles + most - 1) / most), 4096);
   p.run = p.each * (uint32_t)groups;
   p.runs = (uint32_t)((o->n_rows + p.run - 1) / p.run);
 }
@@ -189,6 +191,9 @@ ks_status check_offsets(const int64_t *off) {
 void plan(ks::EtaParams &p, const int64_t *off) {
   std::memset(&p, 0, sizeof p);
   std::copy(off, off + KS_NFAM + 1, p.fam_off);
+  int64_t most = 0;
+  for (int f = 0; f < KS_NFAM; ++f) most = std::max(most, off[f + 1] - off[f]);
+  if (most <= 8 * ks::kEtaWide) return;
   p.rows = std::max<int64_t>(1024, (off[KS_NFAM] + 1023) / 1024);
   for (int f = 0; f < KS_NFAM; ++f) p.wg[f + 1] = p.wg[f] + (int32_t)((off[f + 1] - off[f] + p.rows - 1) / p.rows);
 }
@@ -250,6 +255,7 @@ ks_status ks_embed(const ks_matrix *table, double scale, const uint32_t *ids, co
   p.ids = ids;
   p.n_ids = (uint32_t)table->n_rows;
   p.factor = (float)(scale * up);
+  if (!std::isfinite(p.factor)) return set_error(KS_EINVAL, "scale %g / (1 - p) not finite in fp32", scale);
   p.cols = cols_of(y->n_cols);
   return hip_error(ks::launch_embed(p, table->type == KS_BF16, y->type == KS_BF16, stream), "lookup launch");
 }
@@ -331,6 +337,7 @@ ks_status ks_embed_backward(const ks_id_order *order, double scale, const ks_mat
   p.grad = static_cast<float *>(grad->p);
   p.grad_ld = grad->ld;
   p.factor = (float)(scale * up);
+  if (!std::isfinite(p.factor)) return set_error(KS_EINVAL, "scale %g / (1 - p) not finite in fp32", scale);
   p.part = static_cast<float *>(ws);
   return hip_error(ks::launch_embed_back(p, dy->type == KS_BF16, stream), "table's gradient launch");
 }

@@ -78,34 +78,37 @@ __device__ __forceinline__ Eight<B16> load8(const void *base, int64_t at, const 
   return o;
 }
 
+// b where the mask is set, else a (one instruction; a choice between elements of a vector
+// would become a choice of the index)
+__device__ __forceinline__ uint32_t choose(uint32_t mask, uint32_t b, uint32_t a) { return (mask & b) | (~mask & a); }
+
 // the last rem of eight elements down to the first places (with `part`; behind them stays
 // anything)
 template <bool B16>
 __device__ __forceinline__ void align8(Eight<B16> &x, const Cols &c, bool part) {
   if (c.rem == 0 || c.blocks == 1) return;
-  const uint32_t by = 8 - c.rem;
-  if constexpr (B16) {
-    u32x4 &w = x.w[0];
-    if (by & 1)
+  const uint32_t by = 8 - c.rem, mask = part ? 0xFFFFFFFFu : 0u;
+  constexpr int N = B16 ? 4 : 8;
+  uint32_t w[N];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = part ? __builtin_amdgcn_alignbit(j < 3 ? w[j < 3 ? j + 1 : 3] : 0u, w[j], 16) : w[j];
-    if (by & 2)
+  for (int j = 0; j < N; ++j) w[j] = x.w[j / 4][j % 4];
+  if (B16 && (by & 1)) {
 #pragma unroll
-      for (int j = 0; j < 3; ++j) w[j] = part ? w[j + 1] : w[j];
-    if (by & 4)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) w[j] = part ? w[j + 2] : w[j];
-  } else {
-#pragma unroll
-    for (int s = 1; s < 8; s *= 2)
-      if (by & s)
-#pragma unroll
-        for (int j = 0; j + s < 8; ++j) x.w[j / 4][j % 4] = part ? x.w[(j + s) / 4][(j + s) % 4] : x.w[j / 4][j % 4];
+    for (int j = 0; j < N; ++j) w[j] = choose(mask, __builtin_amdgcn_alignbit(j + 1 < N ? w[j + 1 < N ? j + 1 : 0] : 0u, w[j], 16), w[j]);
   }
+#pragma unroll
+  for (int s = 1; s < N; s *= 2)
+    if (by & (B16 ? 2 * s : s)) {
+#pragma unroll
+      for (int j = 0; j + s < N; ++j) w[j] = choose(mask, w[j + s], w[j]);
+    }
+#pragma unroll
+  for (int j = 0; j < N; ++j) x.w[j / 4][j % 4] = w[j];
 }
 
 __device__ __forceinline__ uint32_t pair(float lo, float hi) {
-  return __builtin_bit_cast(uint16_t, (__bf16)lo) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)hi) << 16;
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
 }
 
 template <bool B16>
@@ -139,15 +142,18 @@ struct Draws {
   uint32_t w[4];
   __device__ __forceinline__ uint32_t operator[](int j) const { return j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu; }
 };
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) {
+  return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96);   // (one instruction; the compiler makes two)
+}
 __device__ __forceinline__ Draws philox(const Drop &d, uint64_t block, uint32_t step) {
   uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = step, c3 = d.site;
   uint32_t k0 = d.key0, k1 = d.key1;
 #pragma unroll
   for (int i = 0; i < 10; ++i) {
     const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
-    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+    c0 = xor3((uint32_t)(b >> 32), c1, k0);
     c1 = (uint32_t)b;
-    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+    c2 = xor3((uint32_t)(a >> 32), c3, k1);
     c3 = (uint32_t)a;
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
@@ -175,48 +181,32 @@ __device__ __forceinline__ int64_t row_of(const Cols &c, int64_t first, uint32_t
 }
 
 // ------------------------------------------------------------ lookup and dropout
-// U blocks a lane, their ids and then their elements on the way together: two of a bfloat16
-// table from 2^20 blocks on, one else.  512 MB written and looked up in rows of 256 to
-// 4096 columns: bf16 43-48 us with two, 49-52 with one, 41-50 with four; fp32 (two loads
-// a block anyway) 87-94, 83-87, 85-99; a dropout of 134M bf16 elements 104, 93 and 110.
-template <bool S16, bool D16, bool DROP, int U>
+// One block a lane: the waves in flight hide the way from the id to its row.  (Two or four
+// blocks a lane, on their way together: 16,381 rows of 4096 bf16 columns 51 us, one 48;
+// dropout of 134M bf16 elements 104 and 110, one 86.)
+template <bool S16, bool D16, bool DROP>
 __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams a) {
-  const int64_t first = (a.wg0 + blockIdx.x) * (kThreads * U);
-  uint32_t b0;
-  const int64_t row0 = row_of(a.cols, first, b0);
-  const uint32_t step = DROP ? step_of(a.drop) : 0;
-  int64_t row[U], id[U];
-  uint32_t b[U];
-  bool in[U], known[U];
+  const int64_t first = (a.wg0 + blockIdx.x) * kThreads;
+  uint32_t b;
+  int64_t i = row_of(a.cols, first, b);
+  i += row_in(a.cols, b + threadIdx.x, b);
+  if (i >= a.n_rows) return;
+  const Place at = place_of(a.cols, b);
+  const int64_t id = a.ids ? (int64_t)a.ids[i] : i;
+  const bool known = !a.ids || id < a.n_ids;
+  Eight<S16> x = {};
+  if (known) x = load8<S16>(a.src, id * a.src_ld + at.at, a.cols);
+  Draws d;
+  if constexpr (DROP) d = philox(a.drop, (uint64_t)(first + threadIdx.x), step_of(a.drop));
+  align8<S16>(x, a.cols, at.part);
+  const float factor = known ? a.factor : 0.0f;   // (x is 0 then: 0 times any factor might be -0)
+  f32x8 v;
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    row[u] = row0 + row_in(a.cols, b0 + u * kThreads + threadIdx.x, b[u]);
-    in[u] = row[u] < a.n_rows;
-    id[u] = row[u];
-    if (a.ids && in[u]) id[u] = a.ids[row[u]];
+  for (int j = 0; j < 8; ++j) {
+    v[j] = x[j] * factor;
+    if constexpr (DROP) v[j] = d[j] >= a.drop.least ? v[j] : 0.0f;
   }
-  Eight<S16> x[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    known[u] = in[u] && (!a.ids || id[u] < a.n_ids);
-    x[u] = {};
-    if (known[u]) x[u] = load8<S16>(a.src, id[u] * a.src_ld + place_of(a.cols, b[u]).at, a.cols);
-  }
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (!in[u]) continue;
-    const bool part = place_of(a.cols, b[u]).part;
-    align8<S16>(x[u], a.cols, part);
-    f32x8 v;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = known[u] ? x[u][j] * a.factor : 0.0f;
-    if constexpr (DROP) {
-      const Draws d = philox(a.drop, (uint64_t)(first + u * kThreads + threadIdx.x), step);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = d[j] >= a.drop.least ? v[j] : 0.0f;
-    }
-    store8<D16>(a.dst, row[u] * a.dst_ld + 8 * (int64_t)b[u], v, !part, a.cols.rem);
-  }
+  store8<D16>(a.dst, i * a.dst_ld + 8 * (int64_t)b, v, !at.part, a.cols.rem);
 }
 
 // ------------------------------------------------------------ the table's gradient
@@ -391,15 +381,25 @@ __global__ __launch_bounds__(kBackThreads) void k_embed_join(EmbedBackParams a, 
   const uint32_t quads = a.cols.blocks * 8 / kJoinCols, wide = min(quads, (uint32_t)kBackThreads), lanes = kBackThreads / wide;
   const uint32_t l = threadIdx.x / wide, q = tile * wide + threadIdx.x % wide;
   double sum[kJoinCols] = {};
-  auto add = [&](int64_t slot) {
-    const f32x4 p = *(const f32x4 *)(a.part + (slot * quads + q) * kJoinCols);
-#pragma unroll
-    for (int j = 0; j < kJoinCols; ++j) sum[j] += (double)p[j];
-  };
   if (l < lanes && q < quads) {
-    if (l == 0) add(2 * (int64_t)part + 1);
-#pragma unroll 16
-    for (uint32_t k = part + 1 + l; k <= last; k += lanes) add(2 * (int64_t)k);
+    const float *base = a.part + (int64_t)q * kJoinCols;
+    auto at = [&](int64_t slot) { return *(const f32x4 *)(base + slot * quads * kJoinCols); };
+    if (l == 0) {
+      const f32x4 p = at(2 * (int64_t)part + 1);
+#pragma unroll
+      for (int j = 0; j < kJoinCols; ++j) sum[j] = (double)p[j];
+    }
+    // sixteen on their way at a time, the last time too
+    constexpr uint32_t kAhead = 16;
+    for (uint32_t k = part + 1 + l; k <= last; k += kAhead * lanes) {
+      f32x4 p[kAhead];
+#pragma unroll
+      for (uint32_t u = 0; u < kAhead; ++u) p[u] = at(2 * (int64_t)min(k + u * lanes, last));
+#pragma unroll
+      for (uint32_t u = 0; u < kAhead; ++u)
+#pragma unroll
+        for (int j = 0; j < kJoinCols; ++j) sum[j] += k + u * lanes <= last ? (double)p[u][j] : 0.0;
+    }
   }
   for (uint32_t half = kBackThreads / 2; half > 0; half /= 2) {
     if (half >= lanes) continue;
@@ -431,21 +431,13 @@ hipError_t in_launches(int64_t wgs, F &&launch) {
   return hipSuccess;
 }
 
-template <bool S16, bool D16, int U>
-hipError_t embed(EmbedParams p, int64_t blocks, hipStream_t s) {
-  return in_launches((blocks + kThreads * U - 1) / (kThreads * U), [&](int64_t at, uint32_t wgs) {
-    p.wg0 = at;
-    if (p.drop.least) hipLaunchKernelGGL((k_embed<S16, D16, true, U>), dim3(wgs), dim3(kThreads), 0, s, p);
-    else hipLaunchKernelGGL((k_embed<S16, D16, false, U>), dim3(wgs), dim3(kThreads), 0, s, p);
-  });
-}
-
 template <bool S16, bool D16>
-hipError_t embed(const EmbedParams &p, hipStream_t s) {
-  const int64_t blocks = p.n_rows * (int64_t)p.cols.blocks;
-  if constexpr (S16)
-    if (p.ids && blocks >= (int64_t(1) << 20)) return embed<S16, D16, 2>(p, blocks, s);
-  return embed<S16, D16, 1>(p, blocks, s);
+hipError_t embed(EmbedParams p, hipStream_t s) {
+  return in_launches((p.n_rows * (int64_t)p.cols.blocks + kThreads - 1) / kThreads, [&](int64_t at, uint32_t wgs) {
+    p.wg0 = at;
+    if (p.drop.least) hipLaunchKernelGGL((k_embed<S16, D16, true>), dim3(wgs), dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL((k_embed<S16, D16, false>), dim3(wgs), dim3(kThreads), 0, s, p);
+  });
 }
 
 template <bool B16>

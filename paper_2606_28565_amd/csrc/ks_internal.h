@@ -395,10 +395,11 @@ struct OrderParams {
 hipError_t launch_order(const OrderParams &p, hipStream_t s);
 
 // ---- the loss at given z (ks_eta.hip)
+constexpr int kEtaWide = 1024;        // threads of a workgroup that takes a whole family
 struct EtaParams {
   int64_t fam_off[KS_NFAM + 1];
   int64_t rows;                      // of a workgroup
-  int32_t wg[KS_NFAM + 1];
+  int32_t wg[KS_NFAM + 1];           // none: a workgroup for each family
   const float *z, *eta, *weight;
   float huber;
   float *loss, *dz;

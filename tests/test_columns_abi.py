@@ -191,6 +191,10 @@ def test_bad_scale(scale):
     assert [embed(scale=scale), backward(scale=scale)] == [abi.KS_EINVAL] * 2
 
 
+def test_scale_that_overflows_with_dropout():
+    assert [f(scale=2e38, drop=dropping(0.5)) for f in (embed, backward)] == [abi.KS_EINVAL] * 2
+
+
 def test_shapes_that_do_not_go_together():
     assert dropout(drop=None) == abi.KS_EINVAL
     for other in (dict(n_rows=99), dict(n_cols=21), dict(type=abi.KS_BF16)):
