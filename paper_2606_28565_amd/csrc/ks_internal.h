@@ -388,7 +388,7 @@ struct OrderParams {
   uint32_t n_rows, n_ids;
   uint32_t *row, *id, *off;
   uint32_t *tmp_row, *tmp_id;        // [n_rows]; null with one pass
-  uint32_t *hist, *total;            // [2^bits][chunks], [2^bits]
+  uint32_t *hist, *total;            // [chunks][2^bits], [2^bits]
   uint32_t chunk, chunks;            // keys of a workgroup, a multiple of kOrderKeys
   int32_t bits, passes;
 };

@@ -162,22 +162,39 @@ __global__ __launch_bounds__(kOrderThreads) void k_order_count(OrderParams a, co
   for (uint32_t p = lo + threadIdx.x; p < hi; p += kOrderThreads)
     atomicAdd(&count[key_of(key[p], a.n_ids) >> shift & (bins - 1)], 1u);
   __syncthreads();
-  for (uint32_t d = threadIdx.x; d < bins; d += kOrderThreads) a.hist[(size_t)d * a.chunks + blockIdx.x] = count[d];
+  for (uint32_t d = threadIdx.x; d < bins; d += kOrderThreads) a.hist[(size_t)blockIdx.x * bins + d] = count[d];
 }
 
-// a wave per digit; with few chunks k_order_place adds up their counts itself (65,536 keys
-// of 32,000 ids: 27 us in five launches, 29 in seven; 16,381: 23 and 28)
+// A lane per digit, a wave per sixteenth of the chunks.  With few chunks k_order_place adds up
+// their counts itself (65,536 keys of 32,000 ids: 27 us in five launches, 29 in seven;
+// 16,381: 23 and 28).
 constexpr uint32_t kFewChunks = 32;
-__global__ __launch_bounds__(256) void k_order_sum(OrderParams a) {
-  const uint32_t d = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (d >> a.bits) return;
-  uint32_t *h = a.hist + (size_t)d * a.chunks, sum = 0;
-  for (uint32_t c0 = 0; c0 < a.chunks; c0 += 64) {
-    const uint32_t c = c0 + lane, v = c < a.chunks ? h[c] : 0, upto = prefix(v);
-    if (c < a.chunks) h[c] = sum + upto - v;
-    sum += __shfl(upto, 63);
+constexpr int kSumWaves = 16;
+template <int BITS>
+__global__ __launch_bounds__(64 * kSumWaves) void k_order_sum(OrderParams a) {
+  constexpr uint32_t bins = 1u << BITS;
+  __shared__ uint32_t room[kSumWaves][64];
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = blockIdx.x * 64 + lane;
+  const uint32_t per = (a.chunks + kSumWaves - 1) / kSumWaves, lo = min(wave * per, a.chunks), hi = min(lo + per, a.chunks);
+  uint32_t *h = a.hist + d;
+  uint32_t sum = 0;
+#pragma unroll 8
+  for (uint32_t c = lo; c < hi; ++c) sum += h[(size_t)c * bins];
+  room[wave][lane] = sum;
+  __syncthreads();
+  uint32_t at = 0, total = 0;
+#pragma unroll
+  for (uint32_t w = 0; w < kSumWaves; ++w) {
+    at += w < wave ? room[w][lane] : 0;
+    total += room[w][lane];
   }
-  if (lane == 0) a.total[d] = sum;
+  if (wave == 0) a.total[d] = total;
+#pragma unroll 8
+  for (uint32_t c = lo; c < hi; ++c) {
+    const uint32_t v = h[(size_t)c * bins];
+    h[(size_t)c * bins] = at;
+    at += v;
+  }
 }
 
 template <int BITS>
@@ -196,14 +213,14 @@ __global__ __launch_bounds__(kOrderThreads) void k_order_place(OrderParams a, co
       const uint32_t d = threadIdx.x * D + i;
       total[i] = chunks_before[i] = 0;
       if (d < bins) {
-        const uint32_t *h = a.hist + (size_t)d * a.chunks;
+        const uint32_t *h = a.hist + d;
         if (a.chunks > kFewChunks) {
           total[i] = a.total[d];
-          chunks_before[i] = h[blockIdx.x];
+          chunks_before[i] = h[(size_t)blockIdx.x * bins];
         } else {
 #pragma unroll 8
           for (uint32_t c = 0; c < a.chunks; ++c) {
-            const uint32_t v = h[c];
+            const uint32_t v = h[(size_t)c * bins];
             total[i] += v;
             chunks_before[i] += c < blockIdx.x ? v : 0;
           }
@@ -278,7 +295,7 @@ hipError_t order(const OrderParams &p, hipStream_t s) {
     const bool last = (p.passes - 1 - i) % 2 == 0;
     uint32_t *to_key = last ? p.id : p.tmp_id, *to_row = last ? p.row : p.tmp_row;
     hipLaunchKernelGGL((k_order_count<BITS>), dim3(p.chunks), wg, 0, s, p, key, i * BITS);
-    if (p.chunks > kFewChunks) hipLaunchKernelGGL(k_order_sum, dim3((1u << BITS) / 4), dim3(256), 0, s, p);
+    if (p.chunks > kFewChunks) hipLaunchKernelGGL((k_order_sum<BITS>), dim3((1u << BITS) / 64), dim3(64 * kSumWaves), 0, s, p);
     hipLaunchKernelGGL((k_order_place<BITS>), dim3(p.chunks), wg, 0, s, p, key, row, to_key, to_row, i * BITS, p.passes == 1);
     key = to_key;
     row = to_row;
