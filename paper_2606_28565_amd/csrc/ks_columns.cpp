@@ -223,6 +223,7 @@ ks_status ks_dropout(const ks_drop *drop, const ks_matrix *x, const ks_matrix *y
   p.src_ld = x->ld;
   p.dst_ld = y->ld;
   p.n_rows = y->n_rows;
+  p.n_ids = 1;
   p.factor = (float)up;
   p.cols = cols_of(y->n_cols);
   return hip_error(ks::launch_embed(p, x->type == KS_BF16, y->type == KS_BF16, stream), "dropout launch");

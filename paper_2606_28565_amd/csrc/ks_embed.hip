@@ -41,40 +41,41 @@ struct Eight {
   }
 };
 
-// Where block b of a row of `cols` columns is loaded from: its own place, or, where it is
-// the row's last one and not whole, the row's last eight columns, which `align8` moves
-// down.  One load for all lanes, where loads of four, two and one element wait for each
-// other.  (Rows of fewer than eight columns have no such place: `load_few`.)
+// Where a row's last block is not whole (kPart), it is loaded with the row's last eight
+// columns, which `align8` moves down: one load for all lanes, where loads of four, two and
+// one element wait for each other.  Rows of fewer than eight columns (kFew) have no such
+// place.
+enum Kind { kWhole, kPart, kFew };
+
 struct Place {
   int64_t at;        // element in the row
   bool part;         // not whole
 };
+template <int KIND>
 __device__ __forceinline__ Place place_of(const Cols &c, uint32_t b) {
-  const bool part = c.rem != 0 && b + 1 == c.blocks;
-  return {8 * (int64_t)b - (part && c.blocks > 1 ? 8 - c.rem : 0), part};
+  if constexpr (KIND == kWhole) return {8 * (int64_t)b, false};
+  if constexpr (KIND == kFew) return {0, true};
+  const bool part = b + 1 == c.blocks;
+  return {8 * (int64_t)b - (part ? 8 - c.rem : 0), part};
 }
 
-template <bool B16>
-__device__ __forceinline__ Eight<B16> load_few(const void *base, int64_t at, uint32_t rem) {
-  Eight<B16> o;
-  o.w[0] = u32x4{0, 0, 0, 0};
-  if constexpr (!B16) o.w[1] = u32x4{0, 0, 0, 0};
-#pragma unroll
-  for (uint32_t j = 0; j < 7; ++j) {
-    if (j >= rem) break;
-    if constexpr (B16) o.w[0][j / 2] |= (uint32_t)((const uint16_t *)base)[at + j] << (16 * (j & 1));
-    else o.w[j / 4][j % 4] = ((const uint32_t *)base)[at + j];
-  }
-  return o;
-}
-
-template <bool B16>
+template <bool B16, int KIND>
 __device__ __forceinline__ Eight<B16> load8(const void *base, int64_t at, const Cols &c) {
-  if (c.blocks == 1 && c.rem) return load_few<B16>(base, at, c.rem);
   Eight<B16> o;
-  const char *p = (const char *)base + (B16 ? 2 : 4) * at;
-  o.w[0] = *(const any_u32x4 *)p;
-  if constexpr (!B16) o.w[1] = *(const any_u32x4 *)(p + 16);
+  if constexpr (KIND == kFew) {
+    o.w[0] = u32x4{0, 0, 0, 0};
+    if constexpr (!B16) o.w[1] = u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (uint32_t j = 0; j < 7; ++j) {
+      if (j >= c.rem) break;
+      if constexpr (B16) o.w[0][j / 2] |= (uint32_t)((const uint16_t *)base)[at + j] << (16 * (j & 1));
+      else o.w[j / 4][j % 4] = ((const uint32_t *)base)[at + j];
+    }
+  } else {
+    const char *p = (const char *)base + (B16 ? 2 : 4) * at;
+    o.w[0] = *(const any_u32x4 *)p;
+    if constexpr (!B16) o.w[1] = *(const any_u32x4 *)(p + 16);
+  }
   return o;
 }
 
@@ -84,9 +85,9 @@ __device__ __forceinline__ uint32_t choose(uint32_t mask, uint32_t b, uint32_t a
 
 // the last rem of eight elements down to the first places (with `part`; behind them stays
 // anything)
-template <bool B16>
+template <bool B16, int KIND>
 __device__ __forceinline__ void align8(Eight<B16> &x, const Cols &c, bool part) {
-  if (c.rem == 0 || c.blocks == 1) return;
+  if constexpr (KIND != kPart) return;
   const uint32_t by = 8 - c.rem, mask = part ? 0xFFFFFFFFu : 0u;
   constexpr int N = B16 ? 4 : 8;
   uint32_t w[N];
@@ -111,8 +112,9 @@ __device__ __forceinline__ uint32_t pair(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
 }
 
-template <bool B16>
-__device__ __forceinline__ void store8(void *base, int64_t at, f32x8 v, bool whole, uint32_t rem) {
+template <bool B16, int KIND>
+__device__ __forceinline__ void store8(void *base, int64_t at, f32x8 v, bool part, uint32_t rem) {
+  const bool whole = KIND == kWhole || (KIND == kPart && !part);
   if constexpr (B16) {
     char *p = (char *)base + 2 * at;
     const u32x4 w = {pair(v[0], v[1]), pair(v[2], v[3]), pair(v[4], v[5]), pair(v[6], v[7])};
@@ -170,43 +172,53 @@ __device__ __forceinline__ uint32_t row_in(const Cols &c, uint32_t l, uint32_t &
   b = l - q * c.blocks;
   return q;
 }
-// the row of block `first` of all (the same in all lanes) and, in b, its block there
-__device__ __forceinline__ int64_t row_of(const Cols &c, int64_t first, uint32_t &b) {
-  if ((uint64_t)first >> 32) {
-    const int64_t row = first / c.blocks;
-    b = (uint32_t)(first - row * c.blocks);
-    return row;
-  }
-  return row_in(c, (uint32_t)first, b);
-}
-
 // ------------------------------------------------------------ lookup and dropout
-// One block a lane: the waves in flight hide the way from the id to its row.  (Two or four
-// blocks a lane, on their way together: 16,381 rows of 4096 bf16 columns 51 us, one 48;
-// dropout of 134M bf16 elements 104 and 110, one 86.)
-template <bool S16, bool D16, bool DROP>
+// U blocks a lane: their ids, then their rows on the way together, the draws made
+// meanwhile (2,000,003 rows of 16 fp32 columns in rows of 32: 34 us; with the draws
+// before the rows' loads 56).  Two where bfloat16 is looked up or written, else one:
+// lookups of 2^25 bf16 elements in rows of 256 to 4096 columns take 22 to 26 us with two,
+// 24 to 27 with one, 22 to 27 with four; of fp32 ones 47 to 51, 45 to 49, 48 to 54; dropout
+// of as many bf16 elements 27, 24 and 29.
+template <bool LOOKUP, bool S16, bool D16>
+constexpr int kAhead = LOOKUP && (S16 || D16) ? 2 : 1;
+
+template <bool LOOKUP, bool S16, bool D16, bool DROP, int KIND>
 __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams a) {
-  const int64_t first = (a.wg0 + blockIdx.x) * kThreads;
-  uint32_t b;
-  int64_t i = row_of(a.cols, first, b);
-  i += row_in(a.cols, b + threadIdx.x, b);
-  if (i >= a.n_rows) return;
-  const Place at = place_of(a.cols, b);
-  const int64_t id = a.ids ? (int64_t)a.ids[i] : i;
-  const bool known = !a.ids || id < a.n_ids;
-  Eight<S16> x = {};
-  if (known) x = load8<S16>(a.src, id * a.src_ld + at.at, a.cols);
-  Draws d;
-  if constexpr (DROP) d = philox(a.drop, (uint64_t)(first + threadIdx.x), step_of(a.drop));
-  align8<S16>(x, a.cols, at.part);
-  const float factor = known ? a.factor : 0.0f;   // (x is 0 then: 0 times any factor might be -0)
-  f32x8 v;
+  constexpr int U = kAhead<LOOKUP, S16, D16>;
+  const uint32_t l = blockIdx.x * (kThreads * U) + threadIdx.x;
+  int64_t row[U];
+  uint32_t b[U], id[U];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    v[j] = x[j] * factor;
-    if constexpr (DROP) v[j] = d[j] >= a.drop.least ? v[j] : 0.0f;
+  for (int u = 0; u < U; ++u) {
+    row[u] = a.row0 + row_in(a.cols, a.block0 + l + u * kThreads, b[u]);
+    if constexpr (LOOKUP) id[u] = a.ids[min(row[u], a.n_rows - 1)];
   }
-  store8<D16>(a.dst, i * a.dst_ld + 8 * (int64_t)b, v, !at.part, a.cols.rem);
+  // an id beyond the table reads its last row, to no use; a table without rows none
+  Eight<S16> x[U];
+  bool known[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    known[u] = !LOOKUP || id[u] < a.n_ids;
+    const int64_t at = LOOKUP ? (int64_t)min(id[u], a.n_ids - 1) : min(row[u], a.n_rows - 1);
+    if (a.n_ids) x[u] = load8<S16, KIND>(a.src, at * a.src_ld + place_of<KIND>(a.cols, b[u]).at, a.cols);
+  }
+  Draws d[U];
+  if constexpr (DROP) {
+    const uint32_t step = step_of(a.drop);
+#pragma unroll
+    for (int u = 0; u < U; ++u) d[u] = philox(a.drop, a.first + l + u * kThreads, step);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (row[u] >= a.n_rows) break;
+    const bool part = place_of<KIND>(a.cols, b[u]).part;
+    align8<S16, KIND>(x[u], a.cols, part);
+    const uint32_t least = known[u] ? a.drop.least : 1u << 16;   // (no draw is as large)
+    f32x8 v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (DROP ? d[u][j] >= least : known[u]) ? x[u][j] * a.factor : 0.0f;
+    store8<D16, KIND>(a.dst, row[u] * a.dst_ld + 8 * (int64_t)b[u], v, part, a.cols.rem);
+  }
 }
 
 // ------------------------------------------------------------ the table's gradient
@@ -219,18 +231,17 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams a) {
 // goes by sizes alone.
 //
 // A thread's sum: 64 additions in a row, then one for each such run.
-template <bool B16, bool DROP>
+template <bool B16, bool DROP, int KIND>
 __global__ __launch_bounds__(kBackThreads) void k_embed_back(EmbedBackParams a) {
   const int64_t wg = a.wg0 + blockIdx.x;
   const uint32_t n = min(a.off[a.n_ids], (uint32_t)a.n_rows);   // (behind: rows without an id)
   if (wg >= (int64_t)a.runs * a.tiles) {
     // ids without rows
-    uint32_t q0;
-    const int64_t v0 = row_of(a.quads, (wg - (int64_t)a.runs * a.tiles) * (kBackThreads * kBackFill), q0);
+    const uint32_t l = (uint32_t)(wg - a.fill_wg0) * (kBackThreads * kBackFill) + threadIdx.x;
 #pragma unroll
     for (int u = 0; u < kBackFill; ++u) {
       uint32_t q;
-      const int64_t v = v0 + row_in(a.quads, q0 + u * kBackThreads + threadIdx.x, q);
+      const int64_t v = a.fill_row0 + row_in(a.quads, a.fill_quad0 + l + u * kBackThreads, q);
       if (v >= a.n_ids || a.off[v] < a.off[v + 1]) continue;
       float *o = a.grad + v * a.grad_ld + 4 * (int64_t)q;
       if (a.quads.rem == 0 || q + 1 < a.quads.blocks) *(any_f32x4 *)o = f32x4{};
@@ -248,12 +259,12 @@ __global__ __launch_bounds__(kBackThreads) void k_embed_back(EmbedBackParams a) 
   const uint32_t wide = a.wide, groups = kBackThreads / wide;
   const uint32_t g = threadIdx.x / wide, b = tile * wide + threadIdx.x % wide;
   const bool in = g < groups && b < a.cols.blocks;
-  const Place at = place_of(a.cols, min(b, a.cols.blocks - 1));
+  const Place at = place_of<KIND>(a.cols, min(b, a.cols.blocks - 1));
   const uint32_t p0 = min(lo + g * a.each, n), p1 = g < groups ? min(p0 + a.each, n) : p0;
   auto write = [&](uint32_t v, f32x8 s) {
     if (!in || v >= a.n_ids) return;
     s *= a.factor;
-    store8<false>(a.grad, (int64_t)v * a.grad_ld + 8 * (int64_t)b, s, !at.part, a.cols.rem);
+    store8<false, KIND>(a.grad, (int64_t)v * a.grad_ld + 8 * (int64_t)b, s, at.part, a.cols.rem);
   };
 
   f32x8 head = {}, out = {};
@@ -275,7 +286,7 @@ __global__ __launch_bounds__(kBackThreads) void k_embed_back(EmbedBackParams a) 
       }
 #pragma unroll
       for (uint32_t u = 0; u < kBatch; ++u)
-        x[u] = load8<B16>(a.dy, (int64_t)min(row[u], (uint32_t)a.n_rows - 1) * a.ld + at.at, a.cols);
+        x[u] = load8<B16, KIND>(a.dy, (int64_t)min(row[u], (uint32_t)a.n_rows - 1) * a.ld + at.at, a.cols);
 #pragma unroll
       for (uint32_t u = 0; u < kBatch; ++u) {
         if (p + u >= p1) break;
@@ -293,7 +304,7 @@ __global__ __launch_bounds__(kBackThreads) void k_embed_back(EmbedBackParams a) 
           cur = id[u];
           from_before = false;
         }
-        align8<B16>(x[u], a.cols, at.part);
+        align8<B16, KIND>(x[u], a.cols, at.part);
         if (row[u] < a.n_rows) {
           if constexpr (DROP) {
             const Draws d = philox(a.drop, (uint64_t)row[u] * a.cols.blocks + b, step);
@@ -422,7 +433,7 @@ __global__ __launch_bounds__(kBackThreads) void k_embed_join(EmbedBackParams a, 
 // launch(first workgroup, workgroups): as many as a launch takes at a time
 template <class F>
 hipError_t in_launches(int64_t wgs, F &&launch) {
-  constexpr int64_t kMost = int64_t(1) << 23;
+  constexpr int64_t kMost = int64_t(1) << 20;
   for (int64_t at = 0; at < wgs; at += kMost) {
     launch(at, (uint32_t)(wgs - at < kMost ? wgs - at : kMost));
     const hipError_t e = hipGetLastError();
@@ -431,22 +442,55 @@ hipError_t in_launches(int64_t wgs, F &&launch) {
   return hipSuccess;
 }
 
-template <bool S16, bool D16>
+int kind_of(const Cols &c) { return c.rem == 0 ? kWhole : c.blocks > 1 ? kPart : kFew; }
+
+template <bool LOOKUP, bool S16, bool D16, bool DROP, int KIND>
 hipError_t embed(EmbedParams p, hipStream_t s) {
-  return in_launches((p.n_rows * (int64_t)p.cols.blocks + kThreads - 1) / kThreads, [&](int64_t at, uint32_t wgs) {
+  constexpr int kBlocks = kThreads * kAhead<LOOKUP, S16, D16>;
+  return in_launches((p.n_rows * (int64_t)p.cols.blocks + kBlocks - 1) / kBlocks, [&](int64_t at, uint32_t wgs) {
+    p.first = (uint64_t)at * kBlocks;
+    p.row0 = (int64_t)(p.first / p.cols.blocks);
+    p.block0 = (uint32_t)(p.first % p.cols.blocks);
+    hipLaunchKernelGGL((k_embed<LOOKUP, S16, D16, DROP, KIND>), dim3(wgs), dim3(kThreads), 0, s, p);
+  });
+}
+
+template <bool LOOKUP, bool S16, bool D16, bool DROP>
+hipError_t embed_kind(const EmbedParams &p, hipStream_t s) {
+  const int kind = kind_of(p.cols);
+  return kind == kWhole ? embed<LOOKUP, S16, D16, DROP, kWhole>(p, s)
+                        : kind == kPart ? embed<LOOKUP, S16, D16, DROP, kPart>(p, s) : embed<LOOKUP, S16, D16, DROP, kFew>(p, s);
+}
+
+template <bool S16, bool D16>
+hipError_t lookup(const EmbedParams &p, hipStream_t s) {
+  return p.drop.least ? embed_kind<true, S16, D16, true>(p, s) : embed_kind<true, S16, D16, false>(p, s);
+}
+
+template <bool B16>
+hipError_t dropout(const EmbedParams &p, hipStream_t s) {
+  return p.drop.least ? embed_kind<false, B16, B16, true>(p, s) : embed_kind<false, B16, B16, false>(p, s);
+}
+
+template <bool B16, bool DROP>
+hipError_t embed_back_parts(EmbedBackParams p, hipStream_t s) {
+  const int kind = kind_of(p.cols);
+  const int64_t parts = (int64_t)p.runs * p.tiles;
+  return in_launches(parts + p.fill_wgs, [&](int64_t at, uint32_t wgs) {
     p.wg0 = at;
-    if (p.drop.least) hipLaunchKernelGGL((k_embed<S16, D16, true>), dim3(wgs), dim3(kThreads), 0, s, p);
-    else hipLaunchKernelGGL((k_embed<S16, D16, false>), dim3(wgs), dim3(kThreads), 0, s, p);
+    p.fill_wg0 = at > parts ? at : parts;   // the launch's first one for ids without rows
+    const int64_t quads = (p.fill_wg0 - parts) * (kBackThreads * kBackFill);
+    p.fill_row0 = quads / p.quads.blocks;
+    p.fill_quad0 = (uint32_t)(quads % p.quads.blocks);
+    if (kind == kWhole) hipLaunchKernelGGL((k_embed_back<B16, DROP, kWhole>), dim3(wgs), dim3(kBackThreads), 0, s, p);
+    else if (kind == kPart) hipLaunchKernelGGL((k_embed_back<B16, DROP, kPart>), dim3(wgs), dim3(kBackThreads), 0, s, p);
+    else hipLaunchKernelGGL((k_embed_back<B16, DROP, kFew>), dim3(wgs), dim3(kBackThreads), 0, s, p);
   });
 }
 
 template <bool B16>
 hipError_t embed_back(EmbedBackParams p, hipStream_t s) {
-  hipError_t e = in_launches((int64_t)p.runs * p.tiles + p.fill_wgs, [&](int64_t at, uint32_t wgs) {
-    p.wg0 = at;
-    if (p.drop.least) hipLaunchKernelGGL((k_embed_back<B16, true>), dim3(wgs), dim3(kBackThreads), 0, s, p);
-    else hipLaunchKernelGGL((k_embed_back<B16, false>), dim3(wgs), dim3(kBackThreads), 0, s, p);
-  });
+  hipError_t e = p.drop.least ? embed_back_parts<B16, true>(p, s) : embed_back_parts<B16, false>(p, s);
   if (e == hipSuccess && p.runs > 1) {
     const uint32_t quads = p.cols.blocks * 8 / kJoinCols, tiles = (quads + kBackThreads - 1) / kBackThreads;
     e = in_launches((int64_t)(p.runs - 1) * tiles, [&](int64_t at, uint32_t wgs) {
@@ -460,8 +504,9 @@ hipError_t embed_back(EmbedBackParams p, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_embed(const EmbedParams &p, bool src16, bool dst16, hipStream_t s) {
-  if (src16) return dst16 ? embed<true, true>(p, s) : embed<true, false>(p, s);
-  return dst16 ? embed<false, true>(p, s) : embed<false, false>(p, s);
+  if (!p.ids) return src16 ? dropout<true>(p, s) : dropout<false>(p, s);
+  if (src16) return dst16 ? lookup<true, true>(p, s) : lookup<true, false>(p, s);
+  return dst16 ? lookup<false, true>(p, s) : lookup<false, false>(p, s);
 }
 
 hipError_t launch_embed_back(const EmbedBackParams &p, bool dy16, hipStream_t s) {

@@ -351,11 +351,13 @@ struct EmbedParams {
   void *dst;
   int64_t src_ld, dst_ld, n_rows;
   const uint32_t *ids;               // null: row i of src is i
-  uint32_t n_ids;
+  uint32_t n_ids;                    // (1 without ids)
   float factor;
   Cols cols;
   Drop drop;
-  int64_t wg0;                       // of a launch (set by it)
+  uint64_t first;                    // of a launch (set by it): its first block of all,
+  int64_t row0;                      // that one's row
+  uint32_t block0;                   // and block there
 };
 hipError_t launch_embed(const EmbedParams &p, bool src16, bool dst16, hipStream_t s);
 
@@ -376,7 +378,8 @@ struct EmbedBackParams {
   uint32_t wide, each, run, runs, tiles;   // runs parts of the order, tiles of `wide` blocks
   int64_t fill_wgs;                  // ... and for the ids without rows
   float *part;                       // [runs][2][8 blocks]
-  int64_t wg0;                       // of a launch (set by it)
+  int64_t wg0, fill_wg0, fill_row0;  // of a launch (set by it): its first workgroup, the first
+  uint32_t fill_quad0;               // for ids without rows, and where that one begins
 };
 hipError_t launch_embed_back(const EmbedBackParams &p, bool dy16, hipStream_t s);
 
