@@ -72,7 +72,7 @@ def order(ids, n_ids):
 def embed_back(ids, n_ids, dy, scale, dropout=None):
     """The table's gradient and a bound on its error in fp32: the additions that one
     term goes through, at most those of an id's rows; a longer sum goes by 64 in a row,
-    then at most 128 such, then at most 8 joinings, all beyond in 64 bits.  scale times
+    then at most 64 such, then at most 9 joinings, all beyond in 64 bits.  scale times
     1 / (1 - p) is rounded once, its product with the sum once, the sum from 64 bits once."""
     row, _, off = order(ids, n_ids)
     d = np.asarray(dy, np.float64)
@@ -84,7 +84,7 @@ def embed_back(ids, n_ids, dy, scale, dropout=None):
         return np.asarray(c[ends[1]] - c[ends[0]], np.float64)
     count = (ends[1] - ends[0])[:, None]
     big = sums(np.abs(d)) * abs(scale)
-    return sums(d) * scale, (np.minimum(count, 64 + 128 + 8) + 3) * EPS * big
+    return sums(d) * scale, (np.minimum(count, 64 + 64 + 9) + 3) * EPS * big
 
 
 def eta_bounds(z, eta, weight, huber, loss, dz):

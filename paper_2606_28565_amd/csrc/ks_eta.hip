@@ -7,6 +7,10 @@
 // A workgroup works on rows of one family.  z, eta and the weight are read once and dz is
 // written twice and read once, from the caches where it fits them: two exponentials, two
 // logarithms and a reciprocal a row are dear enough to keep what they give.
+//
+// 2,000,003 rows with weights: 16 us (32 MB: 7 at the rate of a copy; two launches are 8
+// with few rows).  4099 rows in one launch: 5 us, as long as the call takes on the host;
+// in two 8.  32,000 rows in one launch 11, in two 8: one up to 8192 rows of a family.
 #include <hip/hip_runtime.h>
 
 #include "ks_gated.h"
@@ -19,7 +23,7 @@ namespace {
 using gated::EtaTerm;
 using gated::eta_term;
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 256;
 constexpr int kRows = 4;   // of a thread, on their way together
 
 __device__ __forceinline__ int family_of(const EtaParams &p, int wg) {

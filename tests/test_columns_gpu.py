@@ -221,8 +221,8 @@ def run_order(ids, v, stream=None):
     return order
 
 
-@pytest.mark.parametrize("n", [0, 1, 2, 63, 64, 65, 1023, 1024, 1025, 4095, 4096, 4097, 8192, 8193, 20_011, 300_007])
-@pytest.mark.parametrize("v", [1, 2, 67, 1023, 1024, 5000, 131_072, (1 << 20) + 3])
+@pytest.mark.parametrize("n", [0, 1, 2, 63, 64, 65, 1023, 1024, 1025, 4095, 4096, 4097, 8192, 8193, 20_011, 65_536, 65_537, 300_007, 1_100_003])
+@pytest.mark.parametrize("v", [1, 2, 67, 255, 256, 1023, 1024, 5000, 131_072, (1 << 20) + 3])
 def test_order(n, v):
     ids = make_ids(n, v, n + v)
     got = run_order(ids, v)
@@ -606,7 +606,21 @@ def test_more_blocks_than_a_launch_takes():
     assert abs(share - 0.5) < 5 * 0.5 / np.sqrt(n)
 
 
-def test_current_device_and_row_of_tables_far_apart():
+def test_gradient_of_a_far_table():
+    """A gradient of more than 2^32 elements: rows of the last ids, and zeros between."""
+    import torch
+    v, dim = 70_000, 1 << 16
+    ids = torch.tensor([v - 1, 65_536, 65_537, v - 1, 0], dtype=torch.int32, device="cuda")
+    dy = torch.arange(1, 6, device="cuda", dtype=torch.float32)[:, None].expand(5, dim).contiguous()
+    grad = torch.full((v, dim), float("nan"), device="cuda")
+    run_back(run_order(ids, v), dy, grad)
+    want = torch.zeros(v, device="cuda")
+    want[[0, 65_536, 65_537, v - 1]] = torch.tensor([5.0, 2.0, 3.0, 5.0], device="cuda")
+    for lo in range(0, v, 10_000):
+        assert (grad[lo:lo + 10_000] == want[lo:lo + 10_000, None]).all()
+
+
+def test_tables_of_more_than_32_bits():
     """A table of more than 2^32 elements."""
     import torch
     v, dim = 70_000, 1 << 16
