@@ -136,7 +136,7 @@ void plan(ks::OrderParams &p, const ks_id_order *o) {
   int bits = 0;
   while (bits < 32 && (uint64_t)o->n_ids >> bits) ++bits;   // (n_ids is a key too)
   p.passes = (bits + ks::kOrderBits - 1) / ks::kOrderBits;
-  p.bits = p.passes * ks::kOrderFew >= bits ? ks::kOrderFew : ks::kOrderBits;
+  p.bits = std::max(ks::kOrderFew, (bits + p.passes - 1) / p.passes);
   const int64_t most = int64_t(512) * ks::kOrderKeys;
   p.chunk = (uint32_t)(ks::kOrderKeys * std::min<int64_t>(512, std::max<int64_t>(1, (o->n_rows + most - 1) / most)));
   p.chunks = (uint32_t)((o->n_rows + p.chunk - 1) / p.chunk);

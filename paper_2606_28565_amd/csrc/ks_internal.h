@@ -385,7 +385,7 @@ hipError_t launch_embed_back(const EmbedBackParams &p, bool dy16, hipStream_t s)
 
 constexpr int kOrderThreads = 512;   // of a workgroup that ranks keys
 constexpr int kOrderKeys = 2048;     // keys ranked at a time
-constexpr int kOrderFew = 8, kOrderBits = 10;   // of a digit: fewer where that takes no more passes
+constexpr int kOrderFew = 8, kOrderBits = 10;   // of a digit: the fewest that take no more passes
 struct OrderParams {
   const uint32_t *ids;
   uint32_t n_rows, n_ids;

@@ -1,4 +1,4 @@
-// The rows by id (ks.h, ks_embed_sort): a stable counting sort by digits of at most
+// The rows by id (ks.h, ks_embed_sort): a stable counting sort by digits of 8 to
 // 10 bits, the low ones first.  An id at or beyond n_ids sorts as n_ids.
 //
 //   k_order_count   how often each digit occurs in each chunk of the keys
@@ -171,30 +171,27 @@ __global__ __launch_bounds__(kOrderThreads) void k_order_count(OrderParams a, co
   for (uint32_t d = threadIdx.x; d < bins; d += kOrderThreads) a.hist[(size_t)blockIdx.x * bins + d] = count[d];
 }
 
-// A lane per digit, a wave per sixteenth of the chunks.  With few chunks k_order_place adds up
-// their counts itself (65,536 keys of 32,000 ids: 27 us in five launches, 29 in seven;
-// 16,381: 23 and 28).
+// Sixteen digits a workgroup, their chunks in 64 slices.  With few chunks k_order_place adds
+// up their counts itself (65,536 keys of 32,000 ids: 27 us in five launches, 29 in
+// seven; 16,381: 23 and 28).
 constexpr uint32_t kFewChunks = 32;
-constexpr int kSumWaves = 16;
+constexpr uint32_t kSumDigits = 16, kSumSlices = 64;
 template <int BITS>
-__global__ __launch_bounds__(64 * kSumWaves) void k_order_sum(OrderParams a) {
+__global__ __launch_bounds__(kSumDigits * kSumSlices) void k_order_sum(OrderParams a) {
   constexpr uint32_t bins = 1u << BITS;
-  __shared__ uint32_t room[kSumWaves][64];
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = blockIdx.x * 64 + lane;
-  const uint32_t per = (a.chunks + kSumWaves - 1) / kSumWaves, lo = min(wave * per, a.chunks), hi = min(lo + per, a.chunks);
+  __shared__ uint32_t room[kSumSlices][kSumDigits];
+  const uint32_t i = threadIdx.x % kSumDigits, slice = threadIdx.x / kSumDigits, d = blockIdx.x * kSumDigits + i;
+  const uint32_t per = (a.chunks + kSumSlices - 1) / kSumSlices, lo = min(slice * per, a.chunks), hi = min(lo + per, a.chunks);
   uint32_t *h = a.hist + d;
   uint32_t sum = 0;
 #pragma unroll 8
   for (uint32_t c = lo; c < hi; ++c) sum += h[(size_t)c * bins];
-  room[wave][lane] = sum;
+  room[slice][i] = sum;
   __syncthreads();
-  uint32_t at = 0, total = 0;
-#pragma unroll
-  for (uint32_t w = 0; w < kSumWaves; ++w) {
-    at += w < wave ? room[w][lane] : 0;
-    total += room[w][lane];
-  }
-  if (wave == 0) a.total[d] = total;
+  uint32_t at = 0;
+#pragma unroll 8
+  for (uint32_t s = 0; s < slice; ++s) at += room[s][i];
+  if (slice == kSumSlices - 1) a.total[d] = at + sum;
 #pragma unroll 8
   for (uint32_t c = lo; c < hi; ++c) {
     const uint32_t v = h[(size_t)c * bins];
@@ -209,6 +206,10 @@ __global__ __launch_bounds__(kOrderThreads) void k_order_place(OrderParams a, co
   constexpr uint32_t kBins = 1u << BITS, bins = kBins;
   constexpr int W = kOrderThreads / 64;
   __shared__ uint32_t count[W][kBins], base[kBins], room[W];
+  // workgroups go to the eight dies in turn: consecutive chunks, whose keys of one digit go
+  // to consecutive places, to the same one, so that few lines are written by two
+  const uint32_t per = (a.chunks + 7) / 8, chunk = blockIdx.x % 8 * per + blockIdx.x / 8;
+  if (chunk >= a.chunks) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   {
     // consecutive digits a thread
@@ -222,13 +223,13 @@ __global__ __launch_bounds__(kOrderThreads) void k_order_place(OrderParams a, co
         const uint32_t *h = a.hist + d;
         if (a.chunks > kFewChunks) {
           total[i] = a.total[d];
-          chunks_before[i] = h[(size_t)blockIdx.x * bins];
+          chunks_before[i] = h[(size_t)chunk * bins];
         } else {
 #pragma unroll 8
           for (uint32_t c = 0; c < a.chunks; ++c) {
             const uint32_t v = h[(size_t)c * bins];
             total[i] += v;
-            chunks_before[i] += c < blockIdx.x ? v : 0;
+            chunks_before[i] += c < chunk ? v : 0;
           }
         }
       }
@@ -239,11 +240,11 @@ __global__ __launch_bounds__(kOrderThreads) void k_order_place(OrderParams a, co
     for (int i = 0; i < D; ++i) {
       const uint32_t d = threadIdx.x * D + i;
       if (d < bins) base[d] = first + chunks_before[i];
-      if (only && blockIdx.x == 0 && d <= a.n_ids && d < bins) a.off[d] = first;
+      if (only && chunk == 0 && d <= a.n_ids && d < bins) a.off[d] = first;
       first += total[i];
     }
   }
-  const uint32_t lo = blockIdx.x * a.chunk, hi = a.n_rows - lo < a.chunk ? a.n_rows : lo + a.chunk;
+  const uint32_t lo = chunk * a.chunk, hi = a.n_rows - lo < a.chunk ? a.n_rows : lo + a.chunk;
   for (uint32_t from = lo; from < hi; from += kOrderKeys) {
     for (uint32_t d = threadIdx.x; d < W * bins; d += kOrderThreads) count[d >> BITS][d & (bins - 1)] = 0;
     uint32_t k[kRounds], rank[kRounds];
@@ -301,8 +302,8 @@ hipError_t order(const OrderParams &p, hipStream_t s) {
     const bool last = (p.passes - 1 - i) % 2 == 0;
     uint32_t *to_key = last ? p.id : p.tmp_id, *to_row = last ? p.row : p.tmp_row;
     hipLaunchKernelGGL((k_order_count<BITS>), dim3(p.chunks), wg, 0, s, p, key, i * BITS);
-    if (p.chunks > kFewChunks) hipLaunchKernelGGL((k_order_sum<BITS>), dim3((1u << BITS) / 64), dim3(64 * kSumWaves), 0, s, p);
-    hipLaunchKernelGGL((k_order_place<BITS>), dim3(p.chunks), wg, 0, s, p, key, row, to_key, to_row, i * BITS, p.passes == 1);
+    if (p.chunks > kFewChunks) hipLaunchKernelGGL((k_order_sum<BITS>), dim3((1u << BITS) / kSumDigits), dim3(kSumDigits * kSumSlices), 0, s, p);
+    hipLaunchKernelGGL((k_order_place<BITS>), dim3((p.chunks + 7) / 8 * 8), wg, 0, s, p, key, row, to_key, to_row, i * BITS, p.passes == 1);
     key = to_key;
     row = to_row;
   }
@@ -314,7 +315,8 @@ hipError_t order(const OrderParams &p, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_order(const OrderParams &p, hipStream_t s) {
-  return p.bits == kOrderFew ? order<kOrderFew>(p, s) : order<kOrderBits>(p, s);
+  static_assert(kOrderBits == kOrderFew + 2, "one of these");
+  return p.bits == kOrderFew ? order<kOrderFew>(p, s) : p.bits == kOrderBits ? order<kOrderBits>(p, s) : order<kOrderFew + 1>(p, s);
 }
 
 }  // namespace ks
