@@ -8,7 +8,7 @@
 #include <cstring>
 
 #include "ks.h"
-#include "ks_internal.h"
+#include "ks_columns.h"
 
 using ks::set_error;
 

@@ -9,16 +9,16 @@
 // fp32, and exactly one Philox block's draws.  Each element is read and written once, and
 // bytes bound all three: the draws (20 multiplications to 64 bits a block) are made
 // while loads are on their way, and a dropout takes as long as a copy by the same kernel.
-// Memory moves lines of 128 bytes: 16 of 32 fp32 columns cost what 32 do, and a line
-// that is written in part, off the 64-byte grid, is read first.
+// Reads fetch lines of 128 bytes, needed or not, and stores off the 64-byte grid cost
+// more than their bytes: 2,000,003 rows of 32 fp32 columns pass in 91 us, 16 of the 32
+// in 86, 15 in 127 (260 MB fetched, 128 written).
 //
-// 16,381 rows of 4096 bf16 columns looked up: 46 us (213 MB, 4.7 TB/s; a copy of 4 GiB
-// 4.7).  2,000,003 rows of 16 fp32 columns in rows of 32, with dropout: 35 us.  Dropout of 134M
-// bf16 elements: 86 us (6.2 TB/s), of 15 of 32 fp32 columns of 2,000,003 rows: 127 us
-// (768 MB of lines, 6.0 TB/s).
+// 16,381 rows of 4096 bf16 columns looked up: 45 us (123 MB fetched, 134 written: 5.7
+// TB/s).  2,000,003 rows of 16 fp32 columns in rows of 32, with dropout: 34 us (136 MB).  Dropout
+// of 134M bf16 elements: 86 us (537 MB, 6.2 TB/s; a copy of 4 GiB reaches 4.7).
 #include <hip/hip_runtime.h>
 
-#include "ks_internal.h"
+#include "ks_columns.h"
 
 namespace ks {
 
@@ -242,10 +242,11 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams a) {
 //
 // A thread's sum: 64 additions in a row, then one for each such run.
 //
-// 2,000,003 rows of 16 fp32 columns in rows of 32, 67 ids: 57 us (272 MB of lines, 4.8 TB/s)
-// and the join 5.  16,381 rows of 2048 bf16 columns, 32,000 ids: 74 us (329 MB, most of
+// 2,000,003 rows of 16 fp32 columns in rows of 32, 67 ids: 55 us (318 MB fetched, 5.8 TB/s)
+// and the join 5.  16,381 rows of 2048 bf16 columns, 32,000 ids: 74 us (334 MB, most of
 // them zeros for ids without rows, 4.5 TB/s) and the join 8.  By ids instead of places (a
-// group for an id of up to 128 rows, workgroups for longer ones) they were 152 and 147.
+// group for an id of up to 128 rows, workgroups for longer ones) they were 152 and 147 us
+// with the join.
 template <bool B16, bool DROP, int KIND>
 __global__ __launch_bounds__(kBackThreads) void k_embed_back(EmbedBackParams a) {
   const int64_t wg = a.wg0 + blockIdx.x;

@@ -13,8 +13,8 @@
 // in two 8.  32,000 rows in one launch 11, in two 8: one up to 8192 rows of a family.
 #include <hip/hip_runtime.h>
 
+#include "ks_columns.h"
 #include "ks_gated.h"
-#include "ks_internal.h"
 
 namespace ks {
 

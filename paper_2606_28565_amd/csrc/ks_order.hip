@@ -17,7 +17,7 @@
 // at least, 5 us: what is left is the counting's way through LDS, a pass at a time).
 #include <hip/hip_runtime.h>
 
-#include "ks_internal.h"
+#include "ks_columns.h"
 
 namespace ks {
 

@@ -15,7 +15,7 @@
 #include <numeric>
 #include <vector>
 
-#include "ks_internal.h"
+#include "ks_columns.h"
 
 namespace ks {
 
