@@ -3,6 +3,7 @@ counts; struct layouts; refused calls (fake device addresses: nothing is read)."
 from __future__ import annotations
 
 import ctypes as C
+import os
 import shutil
 import subprocess
 
@@ -12,9 +13,10 @@ import pytest
 from oracle import ks_columns as o
 from oracle import ks_fit as of
 from paper_2606_28565_amd import abi
-from tests.test_host_asan import ROCM_INCLUDE, ROOT
 
 NFAM = abi.NFAM
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+ROCM_INCLUDE = "/opt/rocm/include"
 A = 0x100000          # fake device addresses, 1 GiB apart
 GIB = 1 << 30
 
