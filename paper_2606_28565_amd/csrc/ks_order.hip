@@ -7,14 +7,16 @@
 //   k_order_place   each key to its place: its digit's first one, the chunk's before it,
 //                   and its rank among the chunk's equal ones
 //   k_order_off     off[] from the sorted ids, where more than one pass made them
+//   k_order_within  for few keys of two digits, placed by the high one: a workgroup for each
+//                   high digit places its keys by the low one, and knows its ids' offsets
 //   k_order_small   all passes for up to 8192 keys, which one workgroup holds
 //
 // The rank comes from one ballot per bit: the lanes with the same digit are a mask, and
 // what the wave had before stands in its own counters in LDS.  No atomic's order enters.
 //
-// Launches bound small calls: 4099 rows of 67 ids take 7 us, of 32,000 17, 16,381 rows 8 and
-// 23.  300,007 rows of 1009 ids take 18 us, 2,000,003 of 67 29, of 131,072 100 (24 MB a pass
-// at least, 5 us: what is left is the counting's way through LDS, a pass at a time).
+// Launches bound small calls: 4099 rows of 67 ids take 7 us, of 32,000 15, 16,381 rows 8 and
+// 18.  300,007 rows of 1009 ids take 15 us, 2,000,003 of 67 26, of 131,072 75 (24 MB a pass
+// at least, 5 us: what is left is scattered stores and the counting's way through LDS).
 #include <hip/hip_runtime.h>
 
 #include "ks_columns.h"
@@ -89,8 +91,8 @@ __device__ __forceinline__ void ranks(uint32_t (&rank)[K], const uint32_t (&key)
 }
 
 // K keys a thread; keys and rows pass through LDS between two digits.  (Places and counts
-// of so few keys fit 16 bits.)  4099 keys in two digits take 17 us so, in five launches of
-// the kernels below 24; 16,381 would take 29, and 23.
+// of so few keys fit 16 bits.)  4000 keys in two digits take 13 us so, and the offsets; in five
+// launches of the kernels below 20.
 constexpr uint32_t kOffHere = 4096;   // ids up to which the offsets are found here
 template <int BITS, int K>
 __global__ __launch_bounds__(kSmallThreads) void k_order_small(OrderParams a) {
@@ -200,6 +202,46 @@ __global__ __launch_bounds__(kSumDigits * kSumSlices) void k_order_sum(OrderPara
   }
 }
 
+// Keys [lo, hi) to their places: base[d] is where the next key with digit d goes (shared;
+// a barrier before the call), count room for the waves' counters
+template <int BITS, int W>
+__device__ __forceinline__ void place_keys(uint32_t n_ids, const uint32_t *key, const uint32_t *row, uint32_t *to_key, uint32_t *to_row,
+                                           uint32_t lo, uint32_t hi, int shift, uint32_t (&base)[1 << BITS],
+                                           uint32_t (&count)[W][1 << BITS]) {
+  constexpr uint32_t kBins = 1u << BITS;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  for (uint32_t from = lo; from < hi; from += 64 * W * kRounds) {
+    for (uint32_t d = threadIdx.x; d < W * kBins; d += 64 * W) count[d >> BITS][d & (kBins - 1)] = 0;
+    uint32_t k[kRounds], rank[kRounds];
+    const uint32_t p0 = from + wave * (64 * kRounds) + lane;
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) k[r] = p0 + 64 * r < hi ? key_of(key[p0 + 64 * r], n_ids) : kBehind;
+    __syncthreads();
+    ranks<BITS>(rank, k, count[wave], shift);
+    __syncthreads();
+    for (uint32_t d = threadIdx.x; d < kBins; d += 64 * W) {
+      uint32_t at = base[d];
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        const uint32_t c = count[w][d];
+        count[w][d] = at;
+        at += c;
+      }
+      base[d] = at;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      const uint32_t p = p0 + 64 * r;
+      if (p >= hi) continue;
+      const uint32_t at = count[wave][k[r] >> shift & (kBins - 1)] + rank[r];
+      to_key[at] = k[r];
+      to_row[at] = row ? row[p] : p;
+    }
+    __syncthreads();
+  }
+}
+
 template <int BITS>
 __global__ __launch_bounds__(kOrderThreads) void k_order_place(OrderParams a, const uint32_t *key, const uint32_t *row, uint32_t *to_key,
                                                                uint32_t *to_row, int shift, bool only) {
@@ -210,7 +252,6 @@ __global__ __launch_bounds__(kOrderThreads) void k_order_place(OrderParams a, co
   // to consecutive places, to the same one, so that few lines are written by two
   const uint32_t per = (a.chunks + 7) / 8, chunk = blockIdx.x % 8 * per + blockIdx.x / 8;
   if (chunk >= a.chunks) return;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   {
     // consecutive digits a thread
     constexpr int D = kBins < kOrderThreads ? 1 : kBins / kOrderThreads;
@@ -245,36 +286,61 @@ __global__ __launch_bounds__(kOrderThreads) void k_order_place(OrderParams a, co
     }
   }
   const uint32_t lo = chunk * a.chunk, hi = a.n_rows - lo < a.chunk ? a.n_rows : lo + a.chunk;
-  for (uint32_t from = lo; from < hi; from += kOrderKeys) {
-    for (uint32_t d = threadIdx.x; d < W * bins; d += kOrderThreads) count[d >> BITS][d & (bins - 1)] = 0;
-    uint32_t k[kRounds], rank[kRounds];
-    const uint32_t p0 = from + wave * (64 * kRounds) + lane;
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) k[r] = p0 + 64 * r < hi ? key_of(key[p0 + 64 * r], a.n_ids) : kBehind;
-    __syncthreads();
-    ranks<BITS>(rank, k, count[wave], shift);
-    __syncthreads();
-    for (uint32_t d = threadIdx.x; d < bins; d += kOrderThreads) {
-      uint32_t at = base[d];
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-        const uint32_t c = count[w][d];
-        count[w][d] = at;
-        at += c;
-      }
-      base[d] = at;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-      const uint32_t p = p0 + 64 * r;
-      if (p >= hi) continue;
-      const uint32_t at = count[wave][k[r] >> shift & (bins - 1)] + rank[r];
-      to_key[at] = k[r];
-      to_row[at] = row ? row[p] : p;
-    }
-    __syncthreads();
+  place_keys<BITS>(a.n_ids, key, row, to_key, to_row, lo, hi, shift, base, count);
+}
+
+// From 4097 keys to kWithin: 16,381 of 32,000 ids, a fifth of them under one high digit, take 18 us
+// so, 23 by the low digit first in five launches; all under one, in one workgroup, 42.
+// 3000 take 14, 13 in k_order_small.
+constexpr uint32_t kWithin = 16384;
+template <int BITS>
+__global__ __launch_bounds__(kSmallThreads) void k_order_within(OrderParams a) {
+  constexpr uint32_t kBins = 1u << BITS;
+  constexpr int W = kSmallThreads / 64, D = kBins < kSmallThreads ? 1 : kBins / kSmallThreads;
+  __shared__ uint32_t count[W][kBins], base[kBins], room[W], ends[2];
+  // where this high digit's keys are: how many lower ones there are, and how many of its own
+  const uint32_t high = blockIdx.x;
+  uint32_t lower = 0, own = 0;
+  for (uint32_t i = threadIdx.x; i < a.chunks << BITS; i += kSmallThreads) {
+    const uint32_t v = a.hist[i], d = i & (kBins - 1);
+    lower += d < high ? v : 0;
+    own += d == high ? v : 0;
   }
+  for (uint32_t d = threadIdx.x; d < kBins; d += kSmallThreads) base[d] = 0;
+  if (threadIdx.x < 2) ends[threadIdx.x] = 0;
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) {
+    lower += __shfl_xor(lower, d);
+    own += __shfl_xor(own, d);
+  }
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) {
+    atomicAdd(&ends[0], lower);
+    atomicAdd(&ends[1], own);
+  }
+  __syncthreads();
+  const uint32_t lo = ends[0], hi = min(lo + ends[1], a.n_rows);
+  for (uint32_t p = lo + threadIdx.x; p < hi; p += kSmallThreads) atomicAdd(&base[a.tmp_id[p] & (kBins - 1)], 1u);
+  __syncthreads();
+  uint32_t total[D], sum = 0;
+#pragma unroll
+  for (int i = 0; i < D; ++i) {
+    const uint32_t d = threadIdx.x * D + i;
+    total[i] = d < kBins ? base[d] : 0;
+    sum += total[i];
+  }
+  uint32_t first = lo + before(sum, room);   // (a barrier between the reads and the writes)
+#pragma unroll
+  for (int i = 0; i < D; ++i) {
+    const uint32_t d = threadIdx.x * D + i;
+    if (d < kBins) {
+      base[d] = first;
+      if ((high << BITS) + d <= a.n_ids) a.off[(high << BITS) + d] = first;
+    }
+    first += total[i];
+  }
+  __syncthreads();
+  place_keys<BITS>(a.n_ids, a.tmp_id, a.tmp_row, a.id, a.row, lo, hi, 0, base, count);
 }
 
 __global__ __launch_bounds__(256) void k_order_off(OrderParams a) {
@@ -293,7 +359,14 @@ template <int BITS>
 hipError_t order(const OrderParams &p, hipStream_t s) {
   const uint32_t *key = p.ids, *row = nullptr;
   const dim3 wg(kOrderThreads), small_wg(kSmallThreads);
-  const bool small = p.n_rows > 0 && p.n_rows <= kSmallThreads * 8;
+  const bool within = p.passes == 2 && p.n_ids > kOffHere && p.n_rows > kSmallThreads * 4 && p.n_rows <= kWithin;
+  const bool small = !within && p.n_rows > 0 && p.n_rows <= kSmallThreads * 8;
+  if (within) {
+    hipLaunchKernelGGL((k_order_count<BITS>), dim3(p.chunks), wg, 0, s, p, key, BITS);
+    hipLaunchKernelGGL((k_order_place<BITS>), dim3((p.chunks + 7) / 8 * 8), wg, 0, s, p, key, row, p.tmp_id, p.tmp_row, BITS, false);
+    hipLaunchKernelGGL((k_order_within<BITS>), dim3((p.n_ids >> BITS) + 1), small_wg, 0, s, p);
+    return hipGetLastError();
+  }
   if (small) {
     if (p.n_rows <= kSmallThreads * 4) hipLaunchKernelGGL((k_order_small<BITS, 4>), dim3(1), small_wg, 0, s, p);
     else hipLaunchKernelGGL((k_order_small<BITS, 8>), dim3(1), small_wg, 0, s, p);

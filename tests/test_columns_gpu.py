@@ -221,7 +221,7 @@ def run_order(ids, v, stream=None):
     return order
 
 
-@pytest.mark.parametrize("n", [0, 1, 2, 63, 64, 65, 1023, 1024, 1025, 4095, 4096, 4097, 8192, 8193, 20_011, 65_536, 65_537, 300_007, 1_100_003])
+@pytest.mark.parametrize("n", [0, 1, 2, 63, 64, 65, 1023, 1024, 1025, 4095, 4096, 4097, 8192, 8193, 16_384, 16_385, 20_011, 65_536, 65_537, 300_007, 1_100_003])
 @pytest.mark.parametrize("v", [1, 2, 67, 255, 256, 1023, 1024, 5000, 131_072, (1 << 20) + 3])
 def test_order(n, v):
     ids = make_ids(n, v, n + v)
@@ -232,7 +232,7 @@ def test_order(n, v):
 
 
 @pytest.mark.parametrize("kind", ["one", "none", "all"])
-@pytest.mark.parametrize("n,v", [(5000, 9), (50_000, 3000), (9000, 1 << 22)])
+@pytest.mark.parametrize("n,v", [(5000, 9), (50_000, 3000), (9000, 1 << 22), (16_384, 20_000), (4097, 5000)])
 def test_order_of_other_ids(kind, n, v):
     ids = make_ids(n, v, 1, kind)
     got = run_order(ids, v)
