@@ -175,7 +175,7 @@ __global__ __launch_bounds__(kOrderThreads) void k_order_count(OrderParams a, co
 
 // Sixteen digits a workgroup, their chunks in 64 slices.  With few chunks k_order_place adds
 // up their counts itself (65,536 keys of 32,000 ids: 27 us in five launches, 29 in
-// seven; 16,381: 23 and 28).
+// seven).
 constexpr uint32_t kFewChunks = 32;
 constexpr uint32_t kSumDigits = 16, kSumSlices = 64;
 template <int BITS>

@@ -138,7 +138,7 @@ class GatedFit:
         self.param = {k: v.to(device) for k, v in self.param.items()}
         low = precision == "bf16"
         self.weights = {k: v.bfloat16() if low else v for k, v in self.param.items()}
-        self.heads = abi.gated_heads(*(self.weights[k] for k in ("w1", "w2", "w3", "b3")))
+        self.block = abi.gated_heads(*(self.weights[k] for k in ("w1", "w2", "w3", "b3")))
         self.grad = {k: torch.zeros_like(v) for k, v in self.param.items()}
         self.loss = torch.zeros(n, device=device)
         self.count = torch.zeros(1, dtype=torch.int32, device=device)
@@ -167,17 +167,25 @@ class GatedFit:
         self.config = abi.adamw_config(lr, state_bits=state_bits, step_dev=self.count)
         self.ws, self.rooms = None, []
 
+    @property
+    def heads(self) -> abi.ks_heads:
+        """The heads for the evaluation (of a fit with categories: ``heads_for``, since what
+        the evaluation puts beside 16 features is their squares)."""
+        if self.categories:
+            raise ValueError("a fit with categories: heads_for(category)")
+        return self.block
+
     def workspace(self, data: Measurements) -> int:
         """Room for a step on these rows; called by ``step``, and before a capture.
         Smaller rooms are kept: captured steps go on using them."""
         import torch
         like = self.weights["w1"]
-        if data.x.device != like.device or data.x.dtype != like.dtype or data.x.shape[1] != self.heads.in_dim:
+        if data.x.device != like.device or data.x.dtype != like.dtype or data.x.shape[1] != self.block.in_dim:
             raise ValueError(f"rows are {data.x.dtype} [{data.x.shape[1]}] on {data.x.device}, "
-                             f"not {like.dtype} [{self.heads.in_dim}] on {like.device}")
+                             f"not {like.dtype} [{self.block.in_dim}] on {like.device}")
         if data.categories != self.categories:
             raise ValueError(f"rows of {data.categories} categories for a fit of {self.categories}")
-        need = abi.ks_gated_workspace_bytes(self.heads, data.rows)
+        need = abi.ks_gated_workspace_bytes(self.block, data.rows)
         if need == 0:
             raise abi.KsError(abi.KS_EINVAL, abi.ks_last_error())
         if self.ws is None or self.ws.numel() < need:
@@ -199,15 +207,15 @@ class GatedFit:
                 rows = data.noisy_rows
                 abi.ks_dropout(self.feature_drop, *data.noise_pair, s)
             if not self.categories:
-                abi.ks_gated_loss(self.heads, rows, data.target, self.loss.data_ptr(), None, self.grad_struct, ws, need, s)
+                abi.ks_gated_loss(self.block, rows, data.target, self.loss.data_ptr(), None, self.grad_struct, ws, need, s)
                 return self.loss
             columns, dz = data.columns if rows is data.rows else data.noisy_columns, data.dz.data_ptr()
             abi.ks_embed(self.table, 1.0, data.ids.data_ptr(), self.drop, columns, s)
-            abi.ks_gated_forward(self.heads, rows, dz, s)
+            abi.ks_gated_forward(self.block, rows, dz, s)
             abi.ks_eta_loss(data.fam_off, dz, data.target, self.loss.data_ptr(), dz, data.loss_ws.data_ptr(),
                             data.loss_ws.numel(), s)
-            abi.ks_gated_backward(self.heads, rows, dz, self.grad_struct, ws, need, s)
-            abi.ks_gated_backward(self.heads, rows, dz, data.rows_grad, ws, need, s)
+            abi.ks_gated_backward(self.block, rows, dz, self.grad_struct, ws, need, s)
+            abi.ks_gated_backward(self.block, rows, dz, data.rows_grad, ws, need, s)
             abi.ks_embed_backward(data.order, 1.0, data.columns_grad, self.drop, self.table_grad, data.back_ws.data_ptr(),
                                   data.back_ws.numel(), s)
         return self.loss

@@ -367,7 +367,9 @@ def test_fit_refuses_rows_that_do_not_go_together():
         with pytest.raises(ValueError):
             fit.GatedFit(16, 8, device="cpu", **bad)
     plain, learned = fit.GatedFit(32, 8, device="cpu"), fit.GatedFit(16, 8, device="cpu", categories=2)
-    assert learned.heads.in_dim == 32
+    assert learned.block.in_dim == 32 and plain.heads is plain.block
+    with pytest.raises(ValueError):
+        learned.heads
     with pytest.raises(ValueError):
         learned.workspace(fit.Measurements(torch.zeros(6, 32), off, eta))
     with pytest.raises(ValueError):
