@@ -160,6 +160,8 @@ OrderRoom room_of(const ks::OrderParams &p) {
 // (4099 rows of 16 columns: 11 us with 4, 13 with 8, 19 with 16).  More workgroups leave
 // more sums of ids that go on for the join: 16,381 rows of 2048 columns 90 us with 512, 96
 // with 1024, 125 with 2048; 300,007 of 67 columns 33, 31, 32; 2,000,003 of 16 65, 64, 62.
+// Up to twelve places where they make one workgroup, and no join: 1000 rows of 16 columns
+// 8 us, 10 with the join; 1400 9 and 10; with sixteen places 2000 rows 12 and 10.
 void plan(ks::EmbedBackParams &p, const ks_id_order *o, int64_t n_cols) {
   std::memset(&p, 0, sizeof p);
   p.n_rows = o->n_rows;
@@ -171,6 +173,7 @@ void plan(ks::EmbedBackParams &p, const ks_id_order *o, int64_t n_cols) {
   const int64_t fill = ks::kBackThreads * ks::kBackFill, groups = ks::kBackThreads / p.wide, most = 1024 * 4 * groups;
   p.fill_wgs = (o->n_ids * (int64_t)p.quads.blocks + fill - 1) / fill;
   p.each = (uint32_t)std::min<int64_t>(4 * std::max<int64_t>(1, (o->n_rows * p.tiles + most - 1) / most), 4096);
+  if (o->n_rows <= 12 * groups) p.each = std::max<uint32_t>((uint32_t)((o->n_rows + groups - 1) / groups), 4);
   p.run = p.each * (uint32_t)groups;
   p.runs = (uint32_t)((o->n_rows + p.run - 1) / p.run);
 }

@@ -292,11 +292,11 @@ def test_gradient_widths(t, dim, drop):
         check_back(n, v, dim, t, pad, shift, 1.3, drop)
 
 
-@pytest.mark.parametrize("n", [0, 1, 2, 127, 128, 129, 130, 2047, 2048, 2049, 4099, 33_333, 300_007])
+@pytest.mark.parametrize("n", [0, 1, 2, 127, 128, 129, 130, 513, 1536, 1537, 2047, 2048, 2049, 4099, 33_333, 300_007])
 @pytest.mark.parametrize("v,dim", [(1, 16), (67, 16), (3000, 5), (5, 67)])
 def test_gradient_lengths(n, v, dim):
-    """On both sides of the length from which ids are summed by workgroups, and ids that
-    begin and end inside, at and across the parts of the order."""
+    """Ids that begin and end inside, at and across the groups and parts of the order; one
+    part and more."""
     check_back(n, v, dim)
 
 
