@@ -49,6 +49,7 @@ struct EmbedBackParams {
   Drop drop;
   uint32_t wide, each, run, runs, tiles;   // runs parts of the order, tiles of `wide` blocks
   int64_t fill_wgs;                  // ... and for the ids without rows
+  bool past;                         // their zeros are not kept in the caches
   float *part;                       // [runs][2][8 blocks]
   uint32_t mix;                      // (set by the launch, as the rest)
   int64_t wg0, fill_wg0, fill_row0;  // of a launch (set by it): its first workgroup, the first

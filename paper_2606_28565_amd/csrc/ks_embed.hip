@@ -265,9 +265,12 @@ __global__ __launch_bounds__(kBackThreads) void k_embed_back(EmbedBackParams a) 
       const int64_t v = a.fill_row0 + row_in(a.quads, a.fill_quad0 + l + u * kBackThreads, q);
       if (v >= a.n_ids || a.off[v] < a.off[v + 1]) continue;
       float *o = a.grad + v * a.grad_ld + 4 * (int64_t)q;
-      if (a.quads.rem == 0 || q + 1 < a.quads.blocks) *(any_f32x4 *)o = f32x4{};
-      else
+      if (a.quads.rem == 0 || q + 1 < a.quads.blocks) {
+        if (a.past) __builtin_nontemporal_store(f32x4{}, (f32x4 *)o);
+        else *(any_f32x4 *)o = f32x4{};
+      } else {
         for (uint32_t j = 0; j < a.quads.rem; ++j) o[j] = 0.0f;
+      }
     }
     return;
   }

@@ -620,6 +620,29 @@ def test_gradient_of_a_far_table():
         assert (grad[lo:lo + 10_000] == want[lo:lo + 10_000, None]).all()
 
 
+@pytest.mark.parametrize("dim,ld,shift", [(128, 128, 0), (127, 128, 0), (126, 132, 4), (129, 129, 0), (128, 128, 1)])
+def test_gradient_of_a_large_table(dim, ld, shift):
+    """Over 128 MiB, on the 16-byte grid and off it: all ids' rows and nothing else."""
+    import torch
+    v, n = 300_000, 2000
+    g = torch.Generator().manual_seed(6)
+    ids = torch.randint(0, v, (n,), generator=g).to(torch.int32)
+    ids[:3] = torch.tensor([0, v - 1, v])
+    ids = ids.cuda()
+    dy = rnd(n, dim, dim, 0, "f32")
+    order = run_order(ids, v)
+    buf, grad = columns(v, dim, ld, shift, "f32")
+    run_back(order, dy, grad)
+    seen = torch.unique(ids[ids < v].long())
+    want, bound = o.embed_back(ids.cpu().numpy(), v, f64(dy), 1.0)
+    at = seen.cpu().numpy()
+    assert (np.abs(f64(grad[seen]) - want[at]) <= bound[at]).all()
+    rest = torch.ones(v, dtype=torch.bool, device="cuda")
+    rest[seen] = False
+    assert (grad[rest] == 0).all()
+    assert untouched(buf, grad)
+
+
 def test_tables_of_more_than_32_bits():
     """A table of more than 2^32 elements."""
     import torch
