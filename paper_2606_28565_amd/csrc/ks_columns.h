@@ -51,7 +51,6 @@ struct EmbedBackParams {
   int64_t fill_wgs;                  // ... and for the ids without rows
   bool past;                         // their zeros are not kept in the caches
   float *part;                       // [runs][2][8 blocks]
-  uint32_t mix;                      // (set by the launch, as the rest)
   int64_t wg0, fill_wg0, fill_row0;  // of a launch (set by it): its first workgroup, the first
   uint32_t fill_quad0;               // for ids without rows, and where that one begins
 };

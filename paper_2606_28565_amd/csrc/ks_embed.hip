@@ -249,16 +249,11 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams a) {
 // with the join.
 template <bool B16, bool DROP, int KIND>
 __global__ __launch_bounds__(kBackThreads) void k_embed_back(EmbedBackParams a) {
-  // a workgroup of places and a.mix for ids without rows in turn, then the rest of the latter
+  const int64_t wg = a.wg0 + blockIdx.x;
   const uint32_t n = min(a.off[a.n_ids], (uint32_t)a.n_rows);   // (behind: rows without an id)
-  const int64_t wg = a.wg0 + blockIdx.x, parts = (int64_t)a.runs * a.tiles;
-  const uint32_t turn = a.mix + 1;
-  const bool mixed = wg < parts * turn;
-  const uint32_t place = mixed ? (uint32_t)wg / turn : 0, rest = mixed ? (uint32_t)wg % turn : 1;
-  if (rest > 0) {
+  if (wg >= (int64_t)a.runs * a.tiles) {
     // ids without rows
-    const int64_t fill = mixed ? (int64_t)place * a.mix + rest - 1 : wg - parts;
-    const uint32_t l = (uint32_t)(fill - a.fill_wg0) * (kBackThreads * kBackFill) + threadIdx.x;
+    const uint32_t l = (uint32_t)(wg - a.fill_wg0) * (kBackThreads * kBackFill) + threadIdx.x;
 #pragma unroll
     for (int u = 0; u < kBackFill; ++u) {
       uint32_t q;
@@ -278,7 +273,7 @@ __global__ __launch_bounds__(kBackThreads) void k_embed_back(EmbedBackParams a) 
   __shared__ float val[kBackThreads][8];
   __shared__ uint32_t stop[kBackThreads];
   const uint32_t step = DROP ? step_of(a.drop) : 0;
-  const uint32_t part = place / a.tiles, tile = place % a.tiles, lo = part * a.run;
+  const uint32_t part = (uint32_t)(wg / a.tiles), tile = (uint32_t)(wg % a.tiles), lo = part * a.run;
   if (lo >= n) return;
   const uint32_t wide = a.wide, groups = kBackThreads / wide;
   const uint32_t g = threadIdx.x / wide, b = tile * wide + threadIdx.x % wide;
@@ -467,13 +462,6 @@ hipError_t in_launches(int64_t wgs, F &&launch) {
   return hipSuccess;
 }
 
-// Workgroups for ids without rows after each one of places, so that gathering and writing
-// run beside each other; an even number, since workgroups go to the eight dies in turn.
-// 16,381 rows of 2048 bf16 columns, 32,000 ids, with the join: 94 us with none, 90, 88, 86,
-// 85, 90 with 2, 4, 6, 8, 16 (135 with 3: two dies had all places); of 4096 columns 174 with
-// none, 166 with 8, 158 with 16.
-constexpr int64_t kMix = 8;
-
 int kind_of(const Cols &c) { return c.rem == 0 ? kWhole : c.blocks > 1 ? kPart : kFew; }
 
 template <bool LOOKUP, bool S16, bool D16, bool DROP, int KIND>
@@ -508,13 +496,10 @@ template <bool B16, bool DROP>
 hipError_t embed_back_parts(EmbedBackParams p, hipStream_t s) {
   const int kind = kind_of(p.cols);
   const int64_t parts = (int64_t)p.runs * p.tiles;
-  p.mix = parts ? (uint32_t)(p.fill_wgs / parts < kMix ? p.fill_wgs / parts : kMix) & ~1u : 0;
-  const int64_t turn = p.mix + 1;
   return in_launches(parts + p.fill_wgs, [&](int64_t at, uint32_t wgs) {
     p.wg0 = at;
-    // the launch's first workgroup for ids without rows
-    p.fill_wg0 = at < parts * turn ? at / turn * p.mix + (at % turn ? at % turn - 1 : 0) : at - parts;
-    const int64_t quads = p.fill_wg0 * (kBackThreads * kBackFill);
+    p.fill_wg0 = at > parts ? at : parts;   // the launch's first one for ids without rows
+    const int64_t quads = (p.fill_wg0 - parts) * (kBackThreads * kBackFill);
     p.fill_row0 = quads / p.quads.blocks;
     p.fill_quad0 = (uint32_t)(quads % p.quads.blocks);
     if (kind == kWhole) hipLaunchKernelGGL((k_embed_back<B16, DROP, kWhole>), dim3(wgs), dim3(kBackThreads), 0, s, p);
