@@ -155,11 +155,12 @@ OrderRoom room_of(const ks::OrderParams &p) {
   return r;
 }
 
-// Four places of the order for each group of lanes, more where that is over 1024 workgroups,
+// Four places of the order for each group of lanes, more where that is over `most` places,
 // 4096 at most (64 runs of 64 additions).  Few places are a short way through a small call
 // (4099 rows of 16 columns: 11 us with 4, 13 with 8, 19 with 16).  More workgroups leave
-// more sums of ids that go on for the join: 16,381 rows of 2048 columns 90 us with 512, 96
-// with 1024, 125 with 2048; 300,007 of 67 columns 33, 31, 32; 2,000,003 of 16 65, 64, 62.
+// more sums of ids that go on for the join, wide ones above all; fewer do not fill the card:
+// with 512, 1024, 2048 workgroups 16,381 rows of 2048 bf16 columns 67, 72, 75 us (of 1024 44,
+// 46, 50), 300,007 of 256 38, 36, 40, of 67 28, 27, 27, 2,000,003 of 16 fp32 57, 52, 49.
 // Up to twelve places where they make one workgroup, and no join: 1000 rows of 16 columns
 // 8 us, 10 with the join; 1400 9 and 10; with sixteen places 2000 rows 12 and 10.
 void plan(ks::EmbedBackParams &p, const ks_id_order *o, int64_t n_cols) {
@@ -170,18 +171,19 @@ void plan(ks::EmbedBackParams &p, const ks_id_order *o, int64_t n_cols) {
   p.quads = cols_of(n_cols, 4);
   p.wide = std::min<uint32_t>(p.cols.blocks, ks::kBackThreads);
   p.tiles = (p.cols.blocks + p.wide - 1) / p.wide;
-  const int64_t fill = ks::kBackThreads * ks::kBackFill, groups = ks::kBackThreads / p.wide, most = 1024 * 4 * groups;
+  const int64_t fill = ks::kBackThreads * ks::kBackFill, groups = ks::kBackThreads / p.wide;
+  const int64_t most = (p.wide > 64 ? 512 : p.wide > 4 ? 1024 : 2048) * 4 * groups;
   p.fill_wgs = (o->n_ids * (int64_t)p.quads.blocks + fill - 1) / fill;
   p.each = (uint32_t)std::min<int64_t>(4 * std::max<int64_t>(1, (o->n_rows * p.tiles + most - 1) / most), 4096);
   if (o->n_rows <= 12 * groups) p.each = std::max<uint32_t>((uint32_t)((o->n_rows + groups - 1) / groups), 4);
   p.run = p.each * (uint32_t)groups;
   p.runs = (uint32_t)((o->n_rows + p.run - 1) / p.run);
 }
+
 // Nontemporal stores for the zeros of a gradient that the caches do not keep for its reader
-// anyway.  With an AdamW step that reads the gradient: 262 MB of rows on the
-// 16-byte grid 397 us, with ordinary stores 406 (by itself 16,381 rows of 2048 bf16 columns
-// 55 and 76 us); but 51 MB 74 and 73, 8 MB 29 and 28, and off the grid a fill of 1,000,000 x 67
-// 61 and 58.
+// anyway.  With an AdamW step that reads the gradient, 262 MB on the 16-byte grid 397 us, with
+// ordinary stores 406 (16,381 rows of 2048 bf16 columns by themselves 72 and 85); but
+// 51 MB 74 and 73, 8 MB 29 and 28, and off the grid zeros for 1,000,000 x 67 61 and 58.
 constexpr int64_t kPast = int64_t(1) << 27;
 bool past_caches(const ks_matrix *grad) {
   return grad->n_rows * grad->n_cols * (int64_t)sizeof(float) > kPast && (uintptr_t)grad->p % 16 == 0 && grad->ld % 4 == 0;
