@@ -242,7 +242,7 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams a) {
 //
 // A thread's sum: 64 additions in a row, then one for each such run.
 //
-// 2,000,003 rows of 16 fp32 columns in rows of 32, 67 ids: 52 us (318 MB fetched, 6.1 TB/s)
+// 2,000,003 rows of 16 fp32 columns in rows of 32, 67 ids: 52 us (291 MB fetched, 5.6 TB/s)
 // and the join 6.  16,381 rows of 2048 bf16 columns, 32,000 ids: 60 us (334 MB, most of
 // them zeros for ids without rows, 5.6 TB/s) and the join 6.  By ids instead of places (a
 // group for an id of up to 128 rows, workgroups for longer ones) they were 152 and 147 us
