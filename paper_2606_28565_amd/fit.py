@@ -231,8 +231,9 @@ class GatedFit:
     def heads_for(self, category: int | None = None, bounded=None, grid=None) -> abi.ks_heads:
         """Heads of 16 features for one category (None: its learned columns are 0, as for
         rows without one): feature 15 is 1, so what the learned columns e add to gates and
-        ups, W[:, 16:] e, goes to their column 15.  The weights as of now, in tensors that
-        stay with the struct (``weights``); bounded, grid: as for ``abi.gated_heads``."""
+        ups, W[:, 16:] e, goes to their column 15: formed in fp32, for bf16 heads rounded once
+        more, as those are bf16 throughout.  The weights as of now, in tensors that stay with
+        the struct (``weights``); bounded, grid: as for ``abi.gated_heads``."""
         if not self.categories:
             raise ValueError("a fit without categories: its heads are ``heads``")
         if category is not None and not 0 <= category < self.categories:
