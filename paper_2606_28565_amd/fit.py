@@ -104,7 +104,7 @@ class Measurements:
         """Rows for a fit that drops features: theirs but the constant one are written by
         each step."""
         if self.noisy is None:
-            features = (FEATURES if self.categories else self.x.shape[1]) - 1
+            features = FEATURES - 1
             self.noisy = self.x.clone()
             self.noisy_rows = abi.feature_rows(self.noisy, list(self.rows.fam_off))
             self.noisy_columns = abi.matrix(self.noisy[:, FEATURES:]) if self.categories else None
@@ -115,7 +115,8 @@ class GatedFit:
     """Gated heads under AdamW: fp32 parameters, states of ``state_bits`` (32 or 8),
     and for precision "bf16" the bf16 copies that the heads read.  categories: how many
     there are learned columns for (0: none; else in_dim is 32); dropout: of their
-    elements, feature_dropout: of the features but the constant one."""
+    elements, feature_dropout: of the features but the constant one (not with in_dim 32
+    and no categories: no dropout keeps both a feature's expected value and its square's)."""
 
     def __init__(self, in_dim: int = 16, hidden: int = 64, precision: str = "f32", seed: int = 0, lr: float = 3e-3,
                  weight_decay: float = 0.0, state_bits: int = 32, device="cuda", categories: int = 0, dropout: float = 0.0,
@@ -125,6 +126,8 @@ class GatedFit:
             raise ValueError(f"{categories} categories, dropout of learned columns {dropout}")
         if not (0.0 <= dropout < 1.0 and 0.0 <= feature_dropout < 1.0):
             raise ValueError(f"dropout {dropout} or feature_dropout {feature_dropout} outside [0, 1)")
+        if feature_dropout and in_dim != FEATURES and not categories:
+            raise ValueError(f"feature_dropout of {in_dim} inputs: features would be dropped without their squares")
         in_dim = 2 * FEATURES if categories else in_dim
         g = torch.Generator().manual_seed(seed)
         n = abi.NFAM
