@@ -26,6 +26,7 @@ and ks_adamw.  Dropout (of learned columns; of features: ``feature_dropout``) dr
 every step, in replays of a captured one too."""
 from __future__ import annotations
 
+import weakref
 from types import SimpleNamespace
 
 from . import abi
@@ -63,7 +64,8 @@ class Measurements:
             raise ValueError(f"eta is {tuple(eta.shape)}, not one per row of {tuple(x.shape)}")
         if any(t is not None and t.device != x.device for t in (eta, weight, ids)):
             raise ValueError("x, eta, weight and ids are not on one device")
-        self.ids, self.categories, self.noisy = ids, 0, None
+        self.ids, self.categories = ids, 0
+        self.noisy = None   # the rows that the last step which drops features has written
         if ids is not None:
             if ids.dtype != torch.int32 or ids.shape != eta.shape or not ids.is_contiguous():
                 raise ValueError(f"ids are {ids.dtype} {tuple(ids.shape)}, not int32 {tuple(eta.shape)}")
@@ -101,14 +103,12 @@ class Measurements:
                               abi.current_stream())
 
     def noise(self):
-        """Rows for a fit that drops features: theirs but the constant one are written by
+        """Rows for one fit that drops features: theirs but the constant one are written by
         each step."""
-        if self.noisy is None:
-            features = FEATURES - 1
-            self.noisy = self.x.clone()
-            self.noisy_rows = abi.feature_rows(self.noisy, list(self.rows.fam_off))
-            self.noisy_columns = abi.matrix(self.noisy[:, FEATURES:]) if self.categories else None
-            self.noise_pair = abi.matrix(self.x[:, :features]), abi.matrix(self.noisy[:, :features])
+        x, features = self.x.clone(), FEATURES - 1
+        return SimpleNamespace(x=x, rows=abi.feature_rows(x, list(self.rows.fam_off)),
+                               columns=abi.matrix(x[:, FEATURES:]) if self.categories else None,
+                               pair=(abi.matrix(self.x[:, :features]), abi.matrix(x[:, :features])))
 
 
 class GatedFit:
@@ -169,6 +169,7 @@ class GatedFit:
         self.tensors = abi.adamw_tensors(tensors)
         self.config = abi.adamw_config(lr, state_bits=state_bits, step_dev=self.count)
         self.ws, self.rooms = None, []
+        self.noise = weakref.WeakKeyDictionary()   # Measurements -> the rows to drop features in
 
     @property
     def heads(self) -> abi.ks_heads:
@@ -179,8 +180,9 @@ class GatedFit:
         return self.block
 
     def workspace(self, data: Measurements) -> int:
-        """Room for a step on these rows; called by ``step``, and before a capture.
-        Smaller rooms are kept: captured steps go on using them."""
+        """Room for a step on these rows; called by ``step``, and before a capture (of a fit
+        that drops features on the steps' stream, or one that it waits for: a copy of the rows
+        is made).  Smaller rooms are kept: captured steps go on using them."""
         import torch
         like = self.weights["w1"]
         if data.x.device != like.device or data.x.dtype != like.dtype or data.x.shape[1] != self.block.in_dim:
@@ -195,7 +197,9 @@ class GatedFit:
             self.ws = torch.empty(need, dtype=torch.uint8, device=self.loss.device)
             self.rooms.append(self.ws)
         if self.feature_drop is not None:
-            data.noise()
+            if data not in self.noise:
+                self.noise[data] = data.noise()
+            data.noisy = self.noise[data].x
         return need
 
     def gradients(self, data: Measurements):
@@ -205,14 +209,14 @@ class GatedFit:
         need = self.workspace(data)
         with torch.cuda.device(self.loss.device):
             s, ws = abi.current_stream(), self.ws.data_ptr()
-            rows = data.rows
-            if self.feature_drop is not None:
-                rows = data.noisy_rows
-                abi.ks_dropout(self.feature_drop, *data.noise_pair, s)
+            noise = None if self.feature_drop is None else self.noise[data]
+            rows = data.rows if noise is None else noise.rows
+            if noise is not None:
+                abi.ks_dropout(self.feature_drop, *noise.pair, s)
             if not self.categories:
                 abi.ks_gated_loss(self.block, rows, data.target, self.loss.data_ptr(), None, self.grad_struct, ws, need, s)
                 return self.loss
-            columns, dz = data.columns if rows is data.rows else data.noisy_columns, data.dz.data_ptr()
+            columns, dz = data.columns if noise is None else noise.columns, data.dz.data_ptr()
             abi.ks_embed(self.table, 1.0, data.ids.data_ptr(), self.drop, columns, s)
             abi.ks_gated_forward(self.block, rows, dz, s)
             abi.ks_eta_loss(data.fam_off, dz, data.target, self.loss.data_ptr(), dz, data.loss_ws.data_ptr(),

@@ -30,3 +30,20 @@ def test_the_constant_is_not_among_the_features_to_drop():
     d = measurements()
     fit.GatedFit(16, 8, device="cpu", feature_dropout=0.1).workspace(d)
     assert d.noisy.shape == d.x.shape and (d.noisy == d.x).all()
+
+
+def test_each_fit_drops_features_in_rows_of_its_own():
+    """Fits on the same rows may step at the same time, on streams or in graphs of their own:
+    none writes what another one reads."""
+    d, other = measurements(), measurements(9)
+    a, b = (fit.GatedFit(16, 8, device="cpu", seed=s, feature_dropout=0.1) for s in (1, 2))
+    seen = []
+    for ft in (a, b):
+        for data in (d, other):
+            ft.workspace(data)
+            seen.append(data.noisy)
+    assert len({t.data_ptr() for t in seen + [d.x, other.x]}) == 6
+    # ... and keeps them: a captured step goes on using them
+    for ft, data, rows in zip((a, a, b, b), (d, other) * 2, seen):
+        ft.workspace(data)
+        assert data.noisy is rows
