@@ -193,11 +193,16 @@ class GatedFit:
         need = abi.ks_gated_workspace_bytes(self.block, data.rows)
         if need == 0:
             raise abi.KsError(abi.KS_EINVAL, abi.ks_last_error())
+        new = self.feature_drop is not None and data not in self.noise
+        if new and data.x.is_cuda:
+            with torch.cuda.device(data.x.device):
+                if torch.cuda.is_current_stream_capturing():   # (eager steps would lack the copy until a replay)
+                    raise RuntimeError("a fit that drops features: workspace(rows) before a capture")
         if self.ws is None or self.ws.numel() < need:
             self.ws = torch.empty(need, dtype=torch.uint8, device=self.loss.device)
             self.rooms.append(self.ws)
         if self.feature_drop is not None:
-            if data not in self.noise:
+            if new:
                 self.noise[data] = data.noise()
             data.noisy = self.noise[data].x
         return need
