@@ -86,9 +86,12 @@ __device__ __forceinline__ float eta_of(float z) {
 // logarithm (within 2^-23 relative, the logarithm near 1 too): the exponent's
 // rounding is put back to first order, and the logarithm of the rounded 1 + e
 // corrected for that rounding, which keeps it exact relative to a small e.
+// sigma(-z) is within |z| 2^-24 relative, as if of a z rounded once more: enough where z comes
+// out of a block.  EXACT: from e, within 2^-21, for a z that is given.
 struct EtaTerm {
   float loss, dz;
 };
+template <bool EXACT = false>
 __device__ __forceinline__ EtaTerm eta_term(float z, float eta, float weight, float huber) {
   constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
   const float t = fabsf(z) * -kLog2e, lo = fmaf(fabsf(z), -kLog2e, -t) - fabsf(z) * 1.92596299e-8f;
@@ -96,14 +99,16 @@ __device__ __forceinline__ EtaTerm eta_term(float z, float eta, float weight, fl
   e = fmaf(e * kLn2, lo, e);
   if (!(fabsf(z) < 126.0f)) e = z == z ? 0.0f : z;   // (below the normal range; t - t is no number at infinity)
   const float w = 1.0f + e;
-  const float log1 = fmaf(__builtin_amdgcn_logf(w), kLn2, (e - (w - 1.0f)) * __builtin_amdgcn_rcpf(w));
+  const float rw = __builtin_amdgcn_rcpf(w);
+  const float log1 = fmaf(__builtin_amdgcn_logf(w), kLn2, (e - (w - 1.0f)) * rw);
   const float at = eta < 0x1p-126f ? eta * 0x1p32f : eta;   // (the logarithm takes normal numbers)
   const float res = fmaxf(-z, 0.0f) + log1 - (__builtin_amdgcn_logf(at) - (eta < 0x1p-126f ? 32.0f : 0.0f)) * kLn2;
   const float size = fabsf(res);
   const bool far = size > huber;   // (a NaN stays one)
   const float rho = far ? huber * (size - 0.5f * huber) : 0.5f * res * res;
   const float slope = far ? copysignf(huber, res) : res;
-  return {weight * rho, -weight * slope * sigmoid(-z)};   // d log(1 + e^-z) / dz = -sigma(-z)
+  const float sigma = EXACT ? (z > 0.0f ? e : 1.0f) * rw : sigmoid(-z);   // (e, w are NaN where z is)
+  return {weight * rho, -weight * slope * sigma};   // d log(1 + e^-z) / dz = -sigma(-z)
 }
 
 // HID: the widest block that fits the LDS room (any narrower one too)

@@ -1,6 +1,6 @@
 """More of the learned columns on the GPU against the fp64 oracle: launches that begin inside a
-row, digits of ten bits, three digits, what is not finite beside what is, widths whose blocks do
-not divide a workgroup, and fits that drop features on the same rows."""
+row, digits of ten bits, three digits, what is not finite beside what is, widths whose blocks do not
+divide a workgroup, the loss at far z, and fits that drop features on the same rows."""
 from __future__ import annotations
 
 import numpy as np
@@ -9,8 +9,8 @@ import pytest
 from oracle import ks_columns as o
 from paper_2606_28565_amd import fit
 from tests.test_columns_fit_gpu import data
-from tests.test_columns_gpu import (SEED, check_back, columns, f64, make_ids, near, rnd, run_back, run_dropout, run_embed, run_order,
-                                    untouched)
+from tests.test_columns_gpu import (SEED, check_back, check_eta, columns, f64, family_split, make_ids, rnd, run_back,
+                                    run_dropout, run_embed, run_eta, run_order, untouched)
 
 pytestmark = pytest.mark.gpu
 
@@ -173,3 +173,22 @@ def test_gradient_of_widths_off_the_workgroup(t, dim):
 def test_gradient_of_one_id_and_wide_rows(dim):
     """All rows are one id's: its sum goes on through every workgroup."""
     check_back(9001, 3, dim, "bf16", kind="one", positive=True)
+
+
+# ------------------------------------------------------------------ the loss at given z
+@pytest.mark.parametrize("n", [5000, 60_001])
+@pytest.mark.parametrize("huber", [0.3, 1e3, float("inf")])
+@pytest.mark.parametrize("around", [0, 20, 45, 70])
+def test_dz_of_far_z(n, huber, around):
+    """sigma(-z) down to 1e-32 keeps its precision, whatever its size; eta near and far from
+    what z says."""
+    import torch
+    g = torch.Generator().manual_seed(around + n)
+    z = around + 5 * torch.rand(n, generator=g)
+    z = torch.where(torch.rand(n, generator=g) < 0.1, -z, z)
+    eta = torch.exp(torch.rand(n, generator=g) * torch.tensor([1e-3, 1.0, 30.0])[torch.randint(0, 3, (n,), generator=g)])
+    weight = 0.5 + torch.rand(n, generator=g)
+    z, eta, weight = z.cuda(), eta.cuda(), weight.cuda()
+    off = family_split(n)
+    check_eta(z, eta, weight, off, huber, run_eta(z, eta, weight, off, huber))
+    check_eta(z, eta, None, off, huber, run_eta(z, eta, None, off, huber))
