@@ -9,8 +9,9 @@ learn log eta from dimensionless features).
     abi.ks_eval_steps(..., fit.heads, ...)    # the fitted heads price records
 
 A step is ks_gated_loss (loss and gradients) and ks_adamw (all tensors in one
-launch); it allocates nothing and can be captured into a graph.  Argument
-marshalling only, as in ``abi``: the arithmetic is in libks.so.
+launch); it allocates nothing and can be captured into a graph.  A step is argument
+marshalling, as in ``abi``: its arithmetic is in libks.so.  (``heads_for`` forms what a
+category's learned columns add to its heads in torch, once for fitted heads.)
 
 Rows measured on different devices (library versions, element types) carry a category
 each, whose learned columns stand beside their 16 features:
@@ -56,7 +57,8 @@ class Measurements:
     (None: 1 each), kept on the device.  ids: an int32 category below ``categories`` for
     each row of 16 features (others, as -1: none).  x is then a copy whose columns behind the
     features are the learned ones, written by each step, and the ids' order is found once:
-    one fit at a time steps on such rows."""
+    one fit at a time steps on such rows.  (Without ids several may, each on a stream or in
+    a graph of its own.)"""
 
     def __init__(self, x, fam_off, eta, weight=None, huber: float = float("inf"), ids=None, categories: int = 0):
         import torch
